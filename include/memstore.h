@@ -67,7 +67,9 @@ enum {
   MS_REQ_BAD_BLOCK_ID = 8,      /* table entry < 0 or >= num_blocks: token skipped */
   MS_REQ_POSITION_OVERFLOW = 16, /* pos >= max_position: token skipped */
   MS_REQ_KERNEL_TIMEOUT = 32,    /* a bounded wait inside the copy kernel ran out: the cache contents of this call are incomplete */
-  MS_REQ_BAD_START = 64          /* start_pos < 0: no token of the request is placed */
+  MS_REQ_BAD_START = 64,         /* start_pos < 0: no token of the request is placed */
+  MS_REQ_NO_BLOCKS = 128,        /* memstore_grow_blocks / memstore_release_blocks: the free list cannot serve the request */
+  MS_REQ_BAD_LENGTH = 256        /* a negative number of tokens, or token rows outside the call's token arrays */
 };
 
 enum { MS_DTYPE_F32 = 0, MS_DTYPE_F16 = 1, MS_DTYPE_BF16 = 2 };
@@ -392,6 +394,121 @@ ms_status memstore_retrieve_inject(memstore_t* store, const void* queries, const
 ms_status memstore_serve_host(memstore_t* store, const void* query, int32_t user, int32_t k, int32_t start_pos,
                               const int32_t* block_table, int32_t max_blocks, const ms_paged_cache* cache, uint32_t flags,
                               int32_t* out_ids, int32_t* out_n_tokens, int32_t* out_status, ms_stream stream);
+
+/*
+ * ---- the serving step around the cache -------------------------------------------------------------------------------
+ * Injection fills a request's paged blocks; the calls below are what a serving loop does with them next, all on the
+ * device: memstore_grow_blocks gives every request blocks for its new tokens and lists their positions and slots,
+ * memstore_append rotates the new tokens' queries and keys and writes their K/V into the cache of one layer,
+ * memstore_attend lets the new tokens attend to everything their request has in the cache of that layer, and
+ * memstore_release_blocks takes the blocks of finished requests back.  New tokens of all requests are packed one request
+ * after another along the token axis (q_start).  These calls use no scratch of the store: memstore_attend works in a
+ * workspace that the caller gives, so calls on different streams or in different CUDA graphs do not disturb one another
+ * as long as their arguments differ.  They run on the store's device whichever device is current, and may be captured
+ * from their first call on.
+ */
+
+/* A [tokens][heads][head_dim] bf16 array: element (t, h, d) at base[t * token_stride + h * head_stride + d].  base 16-byte
+ * aligned, strides in elements, non-negative multiples of 8 (a slice of a fused projection's output has token_stride
+ * (n_q_heads + 2 n_kv_heads) * head_dim); in arrays that a call writes, head_dim or more where there is more than one. */
+typedef struct {
+  void* base;
+  int64_t token_stride, head_stride;
+} ms_heads;
+
+/*
+ * Block tables and slot maps from request lengths.  Request r holds start_lens[r] tokens in the blocks
+ * table[r][0 .. ceil(start/bs) - 1] and gets new_lens[r] more at positions start .. start + new - 1.  It needs
+ *   need_r = ceil((start + new) / bs) - ceil(start / bs)
+ * further blocks, taken in request order from the free list: free_blocks[*n_taken .. n_free - 1] are free, earlier entries
+ * are in use.  Request r is served when it needs no block or when *n_taken + (the needs of requests 0 .. r) <= n_free: no
+ * request overtakes one that was refused before it.  A refused request gets nothing (all or none): its length stays, its
+ * tokens have position and slot -1.
+ *   start_lens, new_lens  device int32 [nreq]
+ *   block_tables          device int32 [nreq][max_blocks]: entries ceil(start/bs) .. of served requests are written
+ *   cache                 geometry only: block_size and num_blocks are read
+ *   free_blocks           device int32 [n_free]; n_taken: device int32 [1], entries taken so far
+ *   token_capacity        entries of out_positions and out_slots; entries behind the last token are set to -1
+ *   out_q_start           device int32 [nreq + 1]: prefix sums of new_lens (negative ones count as 0), at most token_capacity
+ *   out_seq_lens          device int32 [nreq]: start + new when served, else start; may be start_lens itself
+ *   out_positions         device int32 [token_capacity] or NULL;  out_slots  device int64 [token_capacity] or NULL:
+ *                         slot = table[r][pos / bs] * bs + pos % bs, -1 where the block id is not in [0, num_blocks)
+ *   out_n_taken           device int32 [1]: *n_taken + the blocks given out; may be n_taken itself
+ *   out_status            device int32 [nreq]: MS_REQ_NO_BLOCKS, MS_REQ_BAD_START (start < 0), MS_REQ_BAD_LENGTH (new < 0,
+ *                         or its tokens end behind token_capacity), MS_REQ_POSITION_OVERFLOW (start + new > max_position),
+ *                         MS_REQ_BLOCK_TABLE_SHORT (more than max_blocks blocks): refused.  MS_REQ_BAD_BLOCK_ID: the table
+ *                         or the free list names a block outside the cache: the tokens of that block get slot -1 (a table
+ *                         entry from the free list is then written as -1).
+ * An *n_taken outside [0, n_free] serves no request that needs blocks.  Calls that share tables or a free list are ordered
+ * by the caller.
+ */
+ms_status memstore_grow_blocks(memstore_t* store, const int32_t* start_lens, const int32_t* new_lens, int32_t nreq,
+                               int32_t* block_tables, int32_t max_blocks, const ms_paged_cache* cache, const int32_t* free_blocks,
+                               int32_t n_free, const int32_t* n_taken, int32_t token_capacity, int32_t* out_q_start,
+                               int32_t* out_seq_lens, int32_t* out_positions, int64_t* out_slots, int32_t* out_n_taken,
+                               int32_t* out_status, ms_stream stream);
+
+/*
+ * Take back the blocks of finished requests: for every request with release[r] != 0 (release == NULL: all) the blocks
+ * table[r][0 .. ceil(seq_len/bs) - 1] return to the free list (those of the first such request directly in front of
+ * free_blocks[*n_taken], those of the next in front of them, and *n_taken falls by their number), those table entries become -1 and
+ * seq_lens[r] 0.  Entries that name no block of the cache are dropped (MS_REQ_BAD_BLOCK_ID in out_status,
+ * device int32 [nreq] or NULL); a request whose blocks do not fit in front of *n_taken keeps them (MS_REQ_NO_BLOCKS), and so
+ * do all later ones with blocks to return.  A block that two tables share would be returned twice: keep shared blocks out of tables that are
+ * released.
+ */
+ms_status memstore_release_blocks(memstore_t* store, const int32_t* release, int32_t* seq_lens, int32_t nreq, int32_t* block_tables,
+                                  int32_t max_blocks, const ms_paged_cache* cache, int32_t* free_blocks, int32_t n_free,
+                                  int32_t* n_taken, int32_t* out_status, ms_stream stream);
+
+/*
+ * Rotate the queries and keys of n_tokens new tokens at their positions (the rotation of memstore_inject: same angles, fp32
+ * arithmetic, one rounding to bf16) and write keys and values into layer `layer` of the cache at their slots (bf16, or e4m3
+ * by the rule of ms_paged_cache).
+ *   q          [n_tokens][n_q_heads][head_dim], rotated into q_out, which may be q itself (same base and strides); n_q_heads
+ *              == 0: keys and values only (q and q_out are not looked at)
+ *   k, v       [n_tokens][n_kv_heads][head_dim], the heads of the store
+ *   positions  device int32 [n_tokens]; a token whose position is not in [0, max_position) is left out altogether
+ *   slots      device int64 [n_tokens]; a token whose slot is not in [0, num_blocks * block_size) writes nothing into the cache
+ *   out_status device int32 [n_tokens] or NULL: 0, MS_REQ_BAD_START (position < 0), MS_REQ_POSITION_OVERFLOW,
+ *              MS_REQ_BAD_BLOCK_ID (slot)
+ * Two tokens with one slot race (last writer wins, undetected).
+ */
+ms_status memstore_append(memstore_t* store, int32_t layer, const ms_heads* q, int32_t n_q_heads, const ms_heads* k, const ms_heads* v,
+                          const int32_t* positions, const int64_t* slots, int32_t n_tokens, const ms_paged_cache* cache,
+                          const ms_heads* q_out, int32_t* out_status, ms_stream stream);
+
+/*
+ * Attention of every request's new tokens over its tokens in layer `layer` of the paged cache.  The new tokens of request r are
+ * the rows q_start[r] .. q_start[r+1] - 1 of q and the LAST tokens of its seq_lens[r] cached ones (memstore_append has written
+ * them): row i is at position p = seq_len - n_new + i and attends to the keys at positions 0 .. p.  With g = n_q_heads /
+ * n_kv_heads query heads per K/V head, for query head h:
+ *   s_j = scale * q . K[j][h / g],  out = sum_j exp(s_j - lse) V[j][h / g],  lse = ln sum_j exp(s_j)      (j = 0 .. p)
+ * Scores, maxima, sums and accumulators are fp32; the weights are rounded to the type of the matrix product (bf16, or fp16
+ * with an 8-bit cache).  A row without keys (p < 0) gives zeros and lse = -infinity.  Whatever the cache holds behind a
+ * row's last key, NaN and infinities included, does not reach that row.
+ *   q, out        bf16 [n_tokens][n_q_heads][head_dim] (rotated queries); rows outside every request are neither read nor written.
+ *                 out must not overlap q unless it is q itself (same base and strides)
+ *   q_start       device int32 [nreq + 1], non-decreasing, within [0, n_tokens]
+ *   seq_lens      device int32 [nreq]: tokens in the cache, the new ones included
+ *   cache         as for memstore_inject; the strides of an 8-bit cache are multiples of 16 here (MS_ERR_UNSUPPORTED)
+ *   block_tables  device int32 [nreq][max_blocks]; keys whose block the table does not name (too short, or an id outside
+ *                 [0, num_blocks)) are left out
+ *   scale         > 0 and finite, or 0 for 1 / sqrt(head_dim)
+ *   max_q_len     an upper bound of the requests' new tokens if the host knows one, else 0: it steers the choice of kernels, no
+ *                 result depends on it being right
+ *   out_lse       device fp32 [n_tokens][n_q_heads] or NULL
+ *   out_status    device int32 [nreq] or NULL: MS_REQ_BAD_LENGTH (q_start[r] .. q_start[r+1] is no range of rows, or seq_len is not in
+ *                 [0, 2^30]: the request is left out), MS_REQ_BLOCK_TABLE_SHORT, MS_REQ_BAD_BLOCK_ID, MS_REQ_KERNEL_TIMEOUT
+ *   workspace     device, 256-byte aligned, memstore_attend_workspace() bytes or more; its contents need not be kept or
+ *                 cleared between calls, but calls that may overlap on the GPU need workspaces of their own
+ */
+ms_status memstore_attend(memstore_t* store, int32_t layer, const ms_heads* q, int32_t n_q_heads, int32_t n_tokens, const int32_t* q_start,
+                          const int32_t* seq_lens, int32_t nreq, const int32_t* block_tables, int32_t max_blocks,
+                          const ms_paged_cache* cache, float scale, int32_t max_q_len, const ms_heads* out, float* out_lse,
+                          int32_t* out_status, void* workspace, size_t workspace_bytes, ms_stream stream);
+/* Bytes of workspace that any memstore_attend call of this store needs (it depends on the GPU and head_dim, not on lengths). */
+size_t memstore_attend_workspace(memstore_t* store);
 
 /* Counters since creation (host side; bytes are the algorithmic ones, not measured traffic).  Reading
  * kernel_timeouts synchronises the device. */

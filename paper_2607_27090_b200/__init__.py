@@ -6,7 +6,7 @@ be imported on its own.
 """
 import importlib
 
-_BINDING_NAMES = ("MemStore", "PagedCache", "MemStoreError")
+_BINDING_NAMES = ("MemStore", "PagedCache", "MemStoreError", "GrownBlocks")
 
 
 def __getattr__(name):

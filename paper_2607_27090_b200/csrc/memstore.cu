@@ -23,6 +23,9 @@
 #include "retrieve.cuh"
 #include "score_gemm.cuh"
 #include "ann.cuh"
+#include "append.cuh"
+#include "attend.cuh"
+#include "blocks.cuh"
 
 using namespace ms;
 
@@ -1873,5 +1876,7 @@ ms_status memstore_set_profile_events(memstore_t* s, void* before_copy, void* af
 }
 
 const char* memstore_last_error(memstore_t* s) { return s ? s->err.c_str() : "null store"; }
+
+#include "serving_host.cuh"
 
 }  // extern "C"

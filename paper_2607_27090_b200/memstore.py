@@ -10,6 +10,7 @@ from __future__ import annotations
 import ctypes as C
 from dataclasses import dataclass
 from pathlib import Path
+from typing import NamedTuple
 
 import torch
 
@@ -31,6 +32,7 @@ CACHE_BF16, CACHE_FP8_E4M3 = 0, 1
 STORE_TMA_COPY_PATH = 1
 REQ_KERNEL_TIMEOUT = 32
 REQ_BAD_START = 64
+REQ_NO_BLOCKS, REQ_BAD_LENGTH = 128, 256
 
 
 class MemStoreError(RuntimeError):
@@ -58,6 +60,10 @@ class _PagedCache(C.Structure):
     ]  # fmt: skip
 
 
+class _Heads(C.Structure):
+    _fields_ = [("base", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
 class _AnnParams(C.Structure):
     _fields_ = [("beam", C.c_int32), ("parents", C.c_int32), ("n_entry", C.c_int32), ("max_iters", C.c_int32)]
 
@@ -76,7 +82,8 @@ EXPORTS = (
     "memstore_retrieve_inject", "memstore_add_facts_host", "memstore_set_prefix", "memstore_rope_table_llama3",
     "memstore_build_graph", "memstore_set_graph", "memstore_get_graph", "memstore_retrieve_ann", "memstore_graph_append",
     "memstore_test_hooks", "memstore_reserve", "memstore_compose_cache", "memstore_remove_fact", "memstore_set_graph_user",
-    "memstore_get_graph_user", "memstore_retrieve_ann_users",
+    "memstore_get_graph_user", "memstore_retrieve_ann_users", "memstore_grow_blocks", "memstore_release_blocks",
+    "memstore_append", "memstore_attend", "memstore_attend_workspace",
 )  # fmt: skip
 
 _lib = None
@@ -146,6 +153,17 @@ def load_library() -> C.CDLL:
     L.memstore_serve_host.argtypes = [vp, vp, i32, i32, i32, vp, i32, C.POINTER(_PagedCache), u32, vp, vp, vp, vp]
     L.memstore_inject.restype = i32
     L.memstore_inject.argtypes = [vp, vp, i32, i32, vp, vp, i32, C.POINTER(_PagedCache), vp, vp, vp, i64, u32, vp]
+    hp = C.POINTER(_Heads)
+    L.memstore_grow_blocks.restype = i32
+    L.memstore_grow_blocks.argtypes = [vp, vp, vp, i32, vp, i32, C.POINTER(_PagedCache), vp, i32, vp, i32, vp, vp, vp, vp, vp, vp, vp]
+    L.memstore_release_blocks.restype = i32
+    L.memstore_release_blocks.argtypes = [vp, vp, vp, i32, vp, i32, C.POINTER(_PagedCache), vp, i32, vp, vp, vp]
+    L.memstore_append.restype = i32
+    L.memstore_append.argtypes = [vp, i32, hp, i32, hp, hp, vp, vp, i32, C.POINTER(_PagedCache), hp, vp, vp]
+    L.memstore_attend.restype = i32
+    L.memstore_attend.argtypes = [vp, i32, hp, i32, i32, vp, vp, i32, vp, i32, C.POINTER(_PagedCache), C.c_float, i32, hp, vp, vp, vp, C.c_size_t, vp]
+    L.memstore_attend_workspace.restype = C.c_size_t
+    L.memstore_attend_workspace.argtypes = [vp]
     L.memstore_stats.restype = i32
     L.memstore_stats.argtypes = [vp, C.POINTER(_Stats)]
     L.memstore_set_profile_events.restype = i32
@@ -174,6 +192,17 @@ def _stream_ptr(stream) -> C.c_void_p:
     if stream is None:
         stream = torch.cuda.current_stream()
     return C.c_void_p(stream.cuda_stream)
+
+
+class GrownBlocks(NamedTuple):
+    """What ``MemStore.grow_blocks`` returns (see ``memstore_grow_blocks``)."""
+
+    q_start: torch.Tensor
+    seq_lens: torch.Tensor
+    positions: torch.Tensor
+    slots: torch.Tensor
+    n_taken: torch.Tensor
+    status: torch.Tensor
 
 
 def rope_table_llama3(rotary_dim, rope_theta, factor=8.0, low_freq_factor=1.0, high_freq_factor=4.0, original_max_position=8192):
@@ -525,6 +554,132 @@ class MemStore:
     def set_profile_repeats(self, n: int):
         """Measurement aid: launches of the copy kernel per inject call while profile events are set (see the header)."""
         self._check(self._lib.memstore_set_profile_repeats(self._h, int(n)))
+
+    # -- the serving step around the cache -----------------------------------------------------------
+    def _on(self, t: torch.Tensor | None, dtype, name: str, shape: tuple | None = None):
+        """Pointer of a contiguous tensor on the store's device."""
+        if t is None:
+            return None
+        ptr = _dev_ptr(t, dtype, name)
+        if t.device != self.device:
+            raise ValueError(f"{name} is on {t.device}, the store on {self.device}")
+        if shape is not None and tuple(t.shape) != shape:
+            raise ValueError(f"{name} must have shape {shape}, got {tuple(t.shape)}")
+        return ptr
+
+    def _heads(self, t: torch.Tensor, n_tokens: int, n_heads: int, name: str) -> _Heads:
+        """[n_tokens, n_heads, head_dim] bf16, contiguous in its last dimension, any strides in front of it."""
+        if not t.is_cuda or t.dtype != torch.bfloat16:
+            raise TypeError(f"{name} must be a CUDA bfloat16 tensor")
+        if t.device != self.device:
+            raise ValueError(f"{name} is on {t.device}, the store on {self.device}")
+        if tuple(t.shape) != (n_tokens, n_heads, self.head_dim):
+            raise ValueError(f"{name} must have shape {(n_tokens, n_heads, self.head_dim)}, got {tuple(t.shape)}")
+        if t.numel() and t.stride(2) != 1:
+            raise ValueError(f"{name} must be contiguous in its last dimension")
+        # (strides of dimensions of one element, which torch leaves arbitrary, are not used)
+        return _Heads(t.data_ptr(), t.stride(0) if n_tokens > 1 else 0, t.stride(1) if n_heads > 1 else 0)
+
+    def _cache(self, cache: PagedCache) -> _PagedCache:
+        for t, n in ((cache.k, "k"), (cache.v, "v")):
+            if t.device != self.device:
+                raise ValueError(f"cache.{n} is on {t.device}, the store on {self.device}")
+        return cache._struct()
+
+    def _stream(self, stream) -> torch.cuda.Stream:
+        return torch.cuda.current_stream(self.device) if stream is None else stream
+
+    def grow_blocks(self, start_lens, new_lens, block_tables, cache: PagedCache, free_blocks, n_taken, token_capacity: int,
+                    out: GrownBlocks | None = None, stream=None) -> GrownBlocks:  # fmt: skip
+        """Give every request blocks for ``new_lens`` more tokens and list the new tokens' positions and slots
+        (``block_tables`` is written in place; ``out`` takes buffers of an earlier result, in which ``seq_lens`` may be
+        ``start_lens`` itself and ``n_taken`` the counter itself)."""
+        nreq, cap = start_lens.shape[0], int(token_capacity)
+        stream = self._stream(stream)
+        if out is None:
+            with torch.cuda.stream(stream):
+                e = lambda n, dt=torch.int32: torch.empty((n,), dtype=dt, device=self.device)  # noqa: E731
+                out = GrownBlocks(e(nreq + 1), e(nreq), e(cap), e(cap, torch.int64), e(1), e(nreq))
+        if block_tables.dim() != 2 or block_tables.shape[0] != nreq:
+            raise ValueError(f"block_tables must have shape ({nreq}, max_blocks), got {tuple(block_tables.shape)}")
+        i32 = torch.int32
+        rc = self._lib.memstore_grow_blocks(
+            self._h, self._on(start_lens, i32, "start_lens", (nreq,)), self._on(new_lens, i32, "new_lens", (nreq,)), nreq,
+            self._on(block_tables, i32, "block_tables"), block_tables.shape[1], C.byref(self._cache(cache)),
+            self._on(free_blocks, i32, "free_blocks"), free_blocks.numel(), self._on(n_taken, i32, "n_taken", (1,)), cap,
+            self._on(out.q_start, i32, "out.q_start", (nreq + 1,)), self._on(out.seq_lens, i32, "out.seq_lens", (nreq,)),
+            self._on(out.positions, i32, "out.positions", (cap,)), self._on(out.slots, torch.int64, "out.slots", (cap,)),
+            self._on(out.n_taken, i32, "out.n_taken", (1,)), self._on(out.status, i32, "out.status", (nreq,)),
+            C.c_void_p(stream.cuda_stream))  # fmt: skip
+        self._check(rc)
+        return out
+
+    def release_blocks(self, seq_lens, block_tables, cache: PagedCache, free_blocks, n_taken, release=None, out_status=None,
+                       stream=None) -> None:  # fmt: skip
+        """Return the blocks of the requests with ``release[r] != 0`` (None: all) to the free list; their table entries
+        become -1 and their lengths 0, all in place."""
+        nreq, i32 = seq_lens.shape[0], torch.int32
+        if block_tables.dim() != 2 or block_tables.shape[0] != nreq:
+            raise ValueError(f"block_tables must have shape ({nreq}, max_blocks), got {tuple(block_tables.shape)}")
+        rc = self._lib.memstore_release_blocks(
+            self._h, self._on(release, i32, "release", (nreq,)), self._on(seq_lens, i32, "seq_lens", (nreq,)), nreq,
+            self._on(block_tables, i32, "block_tables"), block_tables.shape[1], C.byref(self._cache(cache)),
+            self._on(free_blocks, i32, "free_blocks"), free_blocks.numel(), self._on(n_taken, i32, "n_taken", (1,)),
+            self._on(out_status, i32, "out_status", (nreq,)), C.c_void_p(self._stream(stream).cuda_stream))  # fmt: skip
+        self._check(rc)
+
+    def append(self, layer: int, q, k, v, positions, slots, cache: PagedCache, q_out=None, out_status=None, stream=None):
+        """Rotate ``q`` [T, n_q_heads, d] (or None) and ``k`` [T, h, d] at ``positions`` (int32) and write K and V into
+        ``layer`` of the cache at ``slots`` (int64, negative: not written).  Returns the rotated queries (``q_out``, a new
+        tensor unless given; it may be ``q`` itself, in place)."""
+        T = k.shape[0]
+        stream = self._stream(stream)
+        n_q = 0
+        hq = ho = None
+        if q is not None:
+            n_q = q.shape[1]
+            hq = self._heads(q, T, n_q, "q")
+            if q_out is None:
+                with torch.cuda.stream(stream):
+                    q_out = torch.empty((T, n_q, self.head_dim), dtype=torch.bfloat16, device=self.device)
+            ho = self._heads(q_out, T, n_q, "q_out")
+        rc = self._lib.memstore_append(
+            self._h, layer, C.byref(hq) if hq is not None else None, n_q, C.byref(self._heads(k, T, self.n_kv_heads, "k")),
+            C.byref(self._heads(v, T, self.n_kv_heads, "v")), self._on(positions, torch.int32, "positions", (T,)),
+            self._on(slots, torch.int64, "slots", (T,)), T, C.byref(self._cache(cache)), C.byref(ho) if ho is not None else None,
+            self._on(out_status, torch.int32, "out_status", (T,)), C.c_void_p(stream.cuda_stream))  # fmt: skip
+        self._check(rc)
+        return q_out
+
+    def attend_workspace_bytes(self) -> int:
+        """Bytes of workspace of an ``attend`` call of this store."""
+        return int(self._lib.memstore_attend_workspace(self._h))
+
+    def attend(self, layer: int, q, cache: PagedCache, q_start, seq_lens, block_tables, scale: float = 0.0, max_q_len: int = 0, out=None,
+               want_lse: bool = False, out_lse=None, out_status=None, workspace=None, stream=None):  # fmt: skip
+        """Attention of the new tokens ``q`` [T, n_q_heads, d] (rows ``q_start[r] .. q_start[r+1] - 1`` are the last tokens
+        of request r's ``seq_lens[r]`` cached ones) over ``layer`` of the cache.  Returns (out, lse or None, out_status).
+        ``workspace``: a uint8 tensor of ``attend_workspace_bytes()``; by default one comes from torch's allocator for
+        every call, so calls on different streams or in different CUDA graphs have their own."""
+        T, n_q, nreq, i32 = q.shape[0], q.shape[1], seq_lens.shape[0], torch.int32
+        if block_tables.dim() != 2 or block_tables.shape[0] != nreq:
+            raise ValueError(f"block_tables must have shape ({nreq}, max_blocks), got {tuple(block_tables.shape)}")
+        stream = self._stream(stream)
+        with torch.cuda.stream(stream):
+            if out is None:
+                out = torch.empty((T, n_q, self.head_dim), dtype=torch.bfloat16, device=self.device)
+            if out_lse is None and want_lse:
+                out_lse = torch.empty((T, n_q), dtype=torch.float32, device=self.device)
+            if workspace is None:
+                workspace = torch.empty((self.attend_workspace_bytes(),), dtype=torch.uint8, device=self.device)
+        rc = self._lib.memstore_attend(
+            self._h, layer, C.byref(self._heads(q, T, n_q, "q")), n_q, T, self._on(q_start, i32, "q_start", (nreq + 1,)),
+            self._on(seq_lens, i32, "seq_lens", (nreq,)), nreq, self._on(block_tables, i32, "block_tables"), block_tables.shape[1],
+            C.byref(self._cache(cache)), float(scale), int(max_q_len), C.byref(self._heads(out, T, n_q, "out")),
+            self._on(out_lse, torch.float32, "out_lse", (T, n_q)), self._on(out_status, i32, "out_status", (nreq,)),
+            self._on(workspace, torch.uint8, "workspace"), workspace.numel(), C.c_void_p(stream.cuda_stream))  # fmt: skip
+        self._check(rc)
+        return out, out_lse, out_status
 
     def stats(self) -> dict:
         st = _Stats()
