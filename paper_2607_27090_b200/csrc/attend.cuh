@@ -578,73 +578,74 @@ __global__ void __launch_bounds__(kAttnThreads, AttnCfg<D, FP8>::kCtasPerSm) att
   }
 }
 
-// Joins the parts of units that CTA borders cut, and reports on the requests.  Block b - 1 < ctas - 1 looks at the border in front of
-// CTA b's share: the block whose border is the first one inside a unit joins that unit.  The blocks behind them check tables.
+// Joins the parts of a unit that CTA borders cut: block b looks at the border in front of CTA b's share and joins the unit there when
+// that border is the unit's first.
 constexpr int kCombineThreads = 128;
 template <int D>
-__global__ void __launch_bounds__(kCombineThreads) attend_combine_kernel(const AttendParams p, const int ctas) {  // ctas of the rows kernel
-  __shared__ int64_t s_warp[32], s_found[2];
-  grid_launch_dependents();
+__device__ __forceinline__ void rows_join(const AttendParams& p, int b, int ctas, int64_t* s_warp, int64_t* s_found) {
   const int tid = threadIdx.x;
-  // (every path waits for the kernels before this one, so that whatever waits for this kernel has waited for them)
-  if ((int)blockIdx.x < ctas - 1) {
-    const int b = blockIdx.x + 1;
-    const int64_t total = attn_total<kCombineThreads>(p, s_warp);
-    const int64_t share = attn_share(total, ctas, p.min_share);
-    const int64_t off = b * share;
-    int64_t req_start = 0;
-    const int r = off < total ? attn_locate<kCombineThreads>(p, off, s_warp, s_found, &req_start) : -1;
-    grid_dependency_wait();
-    if (r < 0) return;
-    const AttnReq rq = attn_request(p, r);
-    const int tiles = attn_tiles(rq), n_rt = (rq.rows + kAttnRows - 1) / kAttnRows;
-    const int t0 = (int)((off - req_start) % tiles);
-    if (t0 == 0 || off - share > off - t0) return;  // no unit is cut here, or an earlier border is the unit's first
-    const int64_t u = (off - req_start) / tiles;
-    const int rt = (int)(u % n_rt), kvh = (int)(u / n_rt);
-    const int64_t u_end = off - t0 + tiles;
-    const int c_last = (int)((u_end - 1) / share);
-    const int row0 = rt * kAttnRows, rows = min(kAttnRows, rq.rows - row0);
-    for (int e = tid; e < rows * (D / 2); e += kCombineThreads) {
-      const int row = e / (D / 2), d = 2 * (e % (D / 2));
-      float m = -INFINITY, l = 0.f, y0 = 0.f, y1 = 0.f;
-      for (int c = b - 1; c <= c_last; ++c) {
-        const int64_t at = ((int64_t)c * 2 + (c == b - 1 ? 1 : 0)) * kAttnRows + row;
-        const float2 ml = p.part_ml[at];
-        const float2 x = *reinterpret_cast<const float2*>(p.part_o + at * D + d);
-        const float n = fmaxf(m, ml.x);
-        const float fa = m == -INFINITY ? 1.f : ex2(m - n), fb = ml.x == -INFINITY ? 1.f : ex2(ml.x - n);
-        l = l * fa + ml.y * fb;
-        y0 = y0 * fa + x.x * fb;
-        y1 = y1 * fa + x.y * fb;
-        m = n;
-      }
-      const int R = row0 + row, tok = rq.q0 + R / p.group, head = kvh * p.group + R % p.group;
-      const float inv = l == 0.f ? 0.f : p.v_scale / l;
-      *reinterpret_cast<uint32_t*>(p.out + tok * p.o_ts + head * p.o_hs + d) = pack_bf16(y0 * inv, y1 * inv);
-      if (p.lse && d == 0) p.lse[(int64_t)tok * p.n_q + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+  const int64_t total = attn_total<kCombineThreads>(p, s_warp);
+  const int64_t share = attn_share(total, ctas, p.min_share);
+  const int64_t off = b * share;
+  int64_t req_start = 0;
+  const int r = off < total ? attn_locate<kCombineThreads>(p, off, s_warp, s_found, &req_start) : -1;
+  grid_dependency_wait();
+  if (r < 0) return;
+  const AttnReq rq = attn_request(p, r);
+  const int tiles = attn_tiles(rq), n_rt = (rq.rows + kAttnRows - 1) / kAttnRows;
+  const int t0 = (int)((off - req_start) % tiles);
+  if (t0 == 0 || share < t0) return;  // no unit is cut here, or an earlier border is the unit's first
+  const int64_t u = (off - req_start) / tiles;
+  const int rt = (int)(u % n_rt), kvh = (int)(u / n_rt);
+  const int c_last = (int)((off - t0 + tiles - 1) / share);
+  const int row0 = rt * kAttnRows, rows = min(kAttnRows, rq.rows - row0);
+  for (int e = tid; e < rows * (D / 2); e += kCombineThreads) {
+    const int row = e / (D / 2), d = 2 * (e % (D / 2));
+    float m = -INFINITY, l = 0.f, y0 = 0.f, y1 = 0.f;
+    for (int c = b - 1; c <= c_last; ++c) {
+      const int64_t at = ((int64_t)c * 2 + (c == b - 1 ? 1 : 0)) * kAttnRows + row;
+      const float2 ml = p.part_ml[at];
+      const float2 x = *reinterpret_cast<const float2*>(p.part_o + at * D + d);
+      const float n = fmaxf(m, ml.x);
+      const float fa = m == -INFINITY ? 1.f : ex2(m - n), fb = ml.x == -INFINITY ? 1.f : ex2(ml.x - n);
+      l = l * fa + ml.y * fb;
+      y0 = y0 * fa + x.x * fb;
+      y1 = y1 * fa + x.y * fb;
+      m = n;
     }
-  } else {
-    grid_dependency_wait();
-    const int r = ((int)blockIdx.x - (ctas - 1)) * (kCombineThreads / 32) + (tid >> 5), lane = tid & 31;
-    if (!p.status || r >= p.nreq) return;
-    const int32_t q0 = p.q_start[r], q1 = p.q_start[r + 1], len = p.seq_lens[r];
-    int st = 0;
-    if (q0 < 0 || q1 < q0 || q1 > p.n_tokens || len < 0 || len > kAttnMaxLen) {
-      st = kReqBadLength;
-    } else {
-      const int64_t blocks = ((int64_t)len + p.block_size - 1) / p.block_size;
-      if (blocks > p.max_blocks) st = kReqTableShort;
-      const int n = (int)min(blocks, (int64_t)p.max_blocks);
-      bool bad = false;
-      for (int b = lane; b < n; b += 32) {
-        const int32_t x = p.tables[(int64_t)r * p.max_blocks + b];
-        bad = bad || x < 0 || x >= p.num_blocks;
-      }
-      if (__any_sync(0xffffffffu, bad)) st |= kReqBadBlock;
-    }
-    if (lane == 0) p.status[r] = st;
+    const int R = row0 + row, tok = rq.q0 + R / p.group, head = kvh * p.group + R % p.group;
+    const float inv = l == 0.f ? 0.f : p.v_scale / l;
+    *reinterpret_cast<uint32_t*>(p.out + tok * p.o_ts + head * p.o_hs + d) = pack_bf16(y0 * inv, y1 * inv);
+    if (p.lse && d == 0) p.lse[(int64_t)tok * p.n_q + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
   }
+}
+
+// The status words of four requests, a warp each; errors: time-outs of the chunk kernel's CTAs (it serves requests of more than
+// min_rows rows), or nullptr.
+__device__ __forceinline__ void attend_report(const AttendParams& p, int block, const int32_t* errors, int n_errors, int min_rows) {
+  const int r = block * (kCombineThreads / 32) + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+  if (!p.status || r >= p.nreq) return;
+  const int32_t q0 = p.q_start[r], q1 = p.q_start[r + 1], len = p.seq_lens[r];
+  int st = 0;
+  if (q0 < 0 || q1 < q0 || q1 > p.n_tokens || len < 0 || len > kAttnMaxLen) {
+    st = kReqBadLength;
+  } else {
+    const int64_t blocks = ((int64_t)len + p.block_size - 1) / p.block_size;
+    if (blocks > p.max_blocks) st = kReqTableShort;
+    const int n = (int)min(blocks, (int64_t)p.max_blocks);
+    bool bad = false;
+    for (int b = lane; b < n; b += 32) {
+      const int32_t x = p.tables[(int64_t)r * p.max_blocks + b];
+      bad = bad || x < 0 || x >= p.num_blocks;
+    }
+    if (__any_sync(0xffffffffu, bad)) st |= kReqBadBlock;
+    if (errors && (q1 - q0) * p.group > min_rows) {
+      bool late = false;
+      for (int i = lane; i < n_errors; i += 32) late = late || errors[i] != 0;
+      if (__any_sync(0xffffffffu, late)) st |= kReqTimeout;
+    }
+  }
+  if (lane == 0) p.status[r] = st;
 }
 
 }  // namespace ms

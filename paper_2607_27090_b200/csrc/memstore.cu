@@ -25,6 +25,7 @@
 #include "ann.cuh"
 #include "append.cuh"
 #include "attend.cuh"
+#include "attend_chunk.cuh"
 #include "blocks.cuh"
 
 using namespace ms;

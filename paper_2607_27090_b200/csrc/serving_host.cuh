@@ -183,6 +183,35 @@ ms_status memstore_append(memstore_t* s, int32_t layer, const ms_heads* q, int32
 }
 
 // ---- attention --------------------------------------------------------------------------------------------------------
+// Requests with more rows (new tokens x query heads per K/V head) than this go to the tensor-core kernel, when head_dim allows it.
+constexpr int kChunkMinRows = kAttnRows;
+
+// The workspace: unfinished rows of the rows kernel (two CTAs per SM at most) and their statistics, then those of the chunk kernel
+// (one CTA per SM) and its error words.  It depends on the GPU and head_dim alone.
+struct AttendLayout {
+  size_t rows_o, rows_ml, chunk_o, chunk_ml, errors, bytes;
+};
+static bool attend_has_chunks(int head_dim) { return head_dim == 64 || head_dim == 128; }
+static AttendLayout attend_layout(const memstore* s) {
+  const size_t d = (size_t)s->cfg.head_dim, sms = (size_t)s->sm_count;
+  AttendLayout w{};
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    const size_t here = at;
+    at += (bytes + 255) & ~(size_t)255;
+    return here;
+  };
+  w.rows_o = take(sms * 2 * 2 * kAttnRows * d * 4);
+  w.rows_ml = take(sms * 2 * 2 * kAttnRows * 8);
+  if (attend_has_chunks(s->cfg.head_dim)) {
+    w.chunk_o = take(sms * 2 * kChunkRows * d * 4);
+    w.chunk_ml = take(sms * 2 * kChunkRows * 8);
+    w.errors = take(sms * 4);
+  }
+  w.bytes = at;
+  return w;
+}
+
 extern "C++" {
 // Shared-memory limits of the attention kernels, raised once per device.
 template <int D, bool FP8>
@@ -191,27 +220,48 @@ static cudaError_t attend_prepare(int device) {
   static bool done[64] = {false};
   std::lock_guard<std::mutex> lock(mu);
   if (done[device & 63]) return cudaSuccess;
-  const cudaError_t e = cudaFuncSetAttribute(attend_rows_kernel<D, FP8>, cudaFuncAttributeMaxDynamicSharedMemorySize, AttnCfg<D, FP8>::kSmemBytes);
+  cudaError_t e = cudaFuncSetAttribute(attend_rows_kernel<D, FP8>, cudaFuncAttributeMaxDynamicSharedMemorySize, AttnCfg<D, FP8>::kSmemBytes);
+  if constexpr (D == 64 || D == 128)
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(attend_chunk_kernel<D, FP8>, cudaFuncAttributeMaxDynamicSharedMemorySize, ChunkCfg<D>::kSmemBytes);
   if (e == cudaSuccess) done[device & 63] = true;
   return e;
 }
 
 template <int D, bool FP8>
-static ms_status attend_launch(memstore* s, AttendParams& p, cudaStream_t st) {
+static ms_status attend_launch(memstore* s, ChunkParams& c, int64_t max_rows, cudaStream_t st) {
   MS_CUDA(s, (attend_prepare<D, FP8>(s->cfg.device)));
-  const int ctas = s->sm_count * AttnCfg<D, FP8>::kCtasPerSm;
-  MS_CUDA(s, launch_dependent(attend_rows_kernel<D, FP8>, dim3((unsigned)ctas), dim3(kAttnThreads), AttnCfg<D, FP8>::kSmemBytes, st, p));
+  AttendParams& p = c.a;
+  // Which kernels: the chunk kernel when a request may have more rows than the rows kernel serves well, the rows kernel when a
+  // request may have fewer.  A single request whose rows are probably many goes to the chunk kernel whatever it turns out to be,
+  // and one kernel is saved.
+  bool chunks = (D == 64 || D == 128) && max_rows > kChunkMinRows;
+  const bool rows = !chunks || p.nreq > 1;
+  c.min_rows = rows ? kChunkMinRows : 0;
+  p.max_rows = chunks ? c.min_rows : 0x7fffffff;
+  int chunk_ctas = 0, rows_ctas = 0;
+  if constexpr (D == 64 || D == 128) {
+    if (chunks) {
+      chunk_ctas = s->sm_count;
+      MS_CUDA(s, launch_dependent(attend_chunk_kernel<D, FP8>, dim3((unsigned)chunk_ctas), dim3(kChunkThreads), ChunkCfg<D>::kSmemBytes, st, c));
+      s->kernels_launched++;
+    }
+  }
+  if (rows) {
+    rows_ctas = s->sm_count * AttnCfg<D, FP8>::kCtasPerSm;
+    MS_CUDA(s, launch_dependent(attend_rows_kernel<D, FP8>, dim3((unsigned)rows_ctas), dim3(kAttnThreads), AttnCfg<D, FP8>::kSmemBytes, st, p));
+    s->kernels_launched++;
+  }
   const int checks = p.status ? (p.nreq + kCombineThreads / 32 - 1) / (kCombineThreads / 32) : 0;
-  MS_CUDA(s, launch_dependent(attend_combine_kernel<D>, dim3((unsigned)(ctas - 1 + checks)), dim3(kCombineThreads), 0, st, p, ctas));
-  s->kernels_launched += 2;
+  const int joins = (chunk_ctas > 1 ? (chunk_ctas - 1) * (kChunkRows / kChunkJoinRows) : 0) + (rows_ctas > 1 ? rows_ctas - 1 : 0);
+  if (joins + checks > 0) {
+    MS_CUDA(s, launch_dependent(attend_join_kernel<D>, dim3((unsigned)(joins + checks)), dim3(kCombineThreads), 0, st, c, chunk_ctas, rows_ctas));
+    s->kernels_launched++;
+  }
   return MS_OK;
 }
 }  // extern "C++"
 
-// CTAs of the rows kernel that the workspace has room for (two per SM), and its layout: unfinished rows, then their statistics.
-static size_t attend_rows_bytes(const memstore* s) { return (size_t)s->sm_count * 2 * 2 * kAttnRows * ((size_t)s->cfg.head_dim * 4 + 8); }
-
-size_t memstore_attend_workspace(memstore_t* s) { return s ? (attend_rows_bytes(s) + 255) & ~(size_t)255 : 0; }
+size_t memstore_attend_workspace(memstore_t* s) { return s ? attend_layout(s).bytes : 0; }
 
 ms_status memstore_attend(memstore_t* s, int32_t layer, const ms_heads* q, int32_t n_q_heads, int32_t n_tokens, const int32_t* q_start,
                           const int32_t* seq_lens, int32_t nreq, const int32_t* block_tables, int32_t max_blocks, const ms_paged_cache* cache,
@@ -239,7 +289,8 @@ ms_status memstore_attend(memstore_t* s, int32_t layer, const ms_heads* q, int32
   DeviceGuard g(c.device);
   const bool fp8 = cache->dtype == MS_CACHE_FP8_E4M3;
   const int64_t esz = fp8 ? 1 : 2;
-  AttendParams p{};
+  ChunkParams cp{};
+  AttendParams& p = cp.a;
   p.q = (const __nv_bfloat16*)q->base;
   p.q_ts = q->token_stride;
   p.q_hs = q->head_stride;
@@ -267,16 +318,24 @@ ms_status memstore_attend(memstore_t* s, int32_t layer, const ms_heads* q, int32
   p.v_scale = fp8 ? cache->v_scale : 1.f;
   p.lse = out_lse;
   p.status = out_status;
-  p.max_rows = 0x7fffffff;
   p.min_share = 2;
-  p.part_o = (float*)workspace;
-  p.part_ml = (float2*)((float*)workspace + (size_t)s->sm_count * 2 * 2 * kAttnRows * c.head_dim);
+  const AttendLayout w = attend_layout(s);
+  char* base = (char*)workspace;
+  p.part_o = (float*)(base + w.rows_o);
+  p.part_ml = (float2*)(base + w.rows_ml);
+  cp.min_share = 2;
+  cp.part_o = (float*)(base + w.chunk_o);
+  cp.part_ml = (float2*)(base + w.chunk_ml);
+  cp.errors = (int32_t*)(base + w.errors);
+  cp.spin_limit = s->test_spin_limit;
+  cp.mute_producer = s->test_mute_producers;
+  const int64_t max_rows = (int64_t)(max_q_len > 0 && max_q_len < n_tokens ? max_q_len : n_tokens) * group;
   cudaStream_t st = (cudaStream_t)stream;
   switch (c.head_dim) {
-    case 16: return fp8 ? attend_launch<16, true>(s, p, st) : attend_launch<16, false>(s, p, st);
-    case 32: return fp8 ? attend_launch<32, true>(s, p, st) : attend_launch<32, false>(s, p, st);
-    case 64: return fp8 ? attend_launch<64, true>(s, p, st) : attend_launch<64, false>(s, p, st);
-    case 128: return fp8 ? attend_launch<128, true>(s, p, st) : attend_launch<128, false>(s, p, st);
-    default: return fp8 ? attend_launch<256, true>(s, p, st) : attend_launch<256, false>(s, p, st);
+    case 16: return fp8 ? attend_launch<16, true>(s, cp, max_rows, st) : attend_launch<16, false>(s, cp, max_rows, st);
+    case 32: return fp8 ? attend_launch<32, true>(s, cp, max_rows, st) : attend_launch<32, false>(s, cp, max_rows, st);
+    case 64: return fp8 ? attend_launch<64, true>(s, cp, max_rows, st) : attend_launch<64, false>(s, cp, max_rows, st);
+    case 128: return fp8 ? attend_launch<128, true>(s, cp, max_rows, st) : attend_launch<128, false>(s, cp, max_rows, st);
+    default: return fp8 ? attend_launch<256, true>(s, cp, max_rows, st) : attend_launch<256, false>(s, cp, max_rows, st);
   }
 }
