@@ -8,14 +8,16 @@
 // of a group.  Two halves of 128 rows work in turn: while the tensor cores multiply for one half, the other half's warps form its
 // weights.  Scores go to TMEM, a thread owns one row (no shuffles), the weights return to TMEM in the type of V over the scores'
 // columns and are the A operand of the second product, whose accumulator stays in TMEM for the whole unit.
-//   warps 0-3, 4-7  weights of rows 0-127, 128-255, and the epilogue
-//   warps 8-11      loads: queries (scaled to fp16 for an 8-bit cache), then K and V tiles of 128 keys through a ring of 5 buffers,
-//                   gathered through the block table with cp.async (8-bit: loaded, converted to fp16 exactly, stored)
-//   warp 12         TMEM allocation, tcgen05.mma issue
+//   warps 0-7, 8-15  weights of rows 0-127, 128-255, and the epilogue: two threads share a row, 64 of the tile's keys each (16 warps: a
+//                    single warp per scheduler cannot keep the exponentials' unit busy)
+//   warps 16-19      loads: queries (scaled to fp16 for an 8-bit cache), then K and V tiles of 128 keys through a ring of 5 buffers,
+//                    gathered through the block table with cp.async (8-bit: loaded, converted to fp16 exactly, stored)
+//   warp 20          TMEM allocation, tcgen05.mma issue by one elected lane (warps 21-23 complete its warpgroup)
 // Work split: as in attend.cuh, the tiles of all units (causal: only as many as a unit's last row sees) form one line of which every
 // CTA takes an equal share, so 64 units on 148 SMs balance as well as 6400.
-// Running maximum: the weights are formed with the maximum of the tiles before, and formed again only when a tile's maximum exceeds it
-// by more than 2^8 (then the accumulator is rescaled too): fp32 sums and weights of up to 256 lose nothing.
+// Running maximum: the weights are formed with the maximum of the tiles before; no maximum is looked for unless the sum of a thread's 64
+// weights passes 2^14, when the row takes a new maximum, its weights are formed again and its accumulator is rescaled.  fp32 sums, and
+// weights of up to 2^14 in bf16 or fp16, lose nothing by that.
 // Every wait is bounded; when one runs out the CTA reports it, frees its tensor memory and leaves.
 #pragma once
 #include "attend.cuh"
@@ -26,10 +28,12 @@ namespace ms {
 constexpr int kChunkRows = 256;
 constexpr int kChunkKeys = 128;
 constexpr int kChunkStages = 5;
-constexpr int kChunkLag = 2;          // tiles that a loading thread keeps in flight behind the one it issues
-constexpr int kChunkThreads = 13 * 32;
+constexpr int kChunkThreads = 24 * 32;
+constexpr int kChunkRegsWeights = 88, kChunkRegsLoads = 72, kChunkRegsIssue = 56;
+static_assert(4 * kChunkRegsWeights + kChunkRegsLoads + kChunkRegsIssue <= 6 * 80, "six warpgroups share the 80 registers a thread of the launch");
 constexpr int kChunkMaskRing = 8;     // (a tile's masks are read at most three tiles after the loader wrote them)
-constexpr float kChunkSlack = 8.f;    // log2 of the growth of the maximum that is tolerated without rescaling
+constexpr uint32_t kChunkSpinLimit = 1u << 26;  // polls (a second or more)
+constexpr float kChunkMaxSum = 16384.f;  // sum of 64 weights (and so a weight) that is tolerated without taking a new maximum
 
 template <int D>
 struct ChunkCfg {
@@ -37,7 +41,8 @@ struct ChunkCfg {
   static constexpr int kTileBytes = kChunkKeys * D * 2;              // K or V tile, 16 bits per element
   static constexpr int kQBytes = kChunkRows * D * 2;
   static constexpr int kRingBytes = kChunkStages * kTileBytes;
-  static constexpr int kSmemBytes = 1024 + kQBytes + kRingBytes + 1536;  // + alignment, barriers, masks
+  static constexpr int kSmemBytes = 1024 + kQBytes + kRingBytes + 1984;  // alignment, tiles, barriers and small arrays
+  static_assert(kSmemBytes <= 232448, "shared memory of a CTA");
   static constexpr int kColO = 2 * kChunkKeys;                       // TMEM: S0, S1 (128 columns each), O0, O1 (D columns each)
   static constexpr int kTmemCols = 512;
 };
@@ -137,27 +142,44 @@ __device__ __forceinline__ bool chunk_next(const ChunkParams& c, ChunkSeg* seg) 
 }
 
 // ---- tcgen05 forms that the scoring kernel does not use
-// Shared-memory descriptor of V as the B operand whose N dimension (head_dim) is contiguous: rows of 128 bytes (64 elements of one
-// key), 128-byte swizzled; 8-key groups are 1 KiB apart (stride offset), blocks of 64 elements one tile column apart (leading offset).
-__device__ __forceinline__ uint64_t umma_desc_mn_sw128(uint32_t smem_addr, uint32_t block_bytes) {
-  uint64_t d = 0;
-  d |= (uint64_t)((smem_addr & 0x3FFFFu) >> 4);
-  d |= (uint64_t)(block_bytes >> 4) << 16;
-  d |= (uint64_t)(1024 >> 4) << 32;
-  d |= (uint64_t)1 << 46;
-  d |= (uint64_t)2 << 61;
-  return d;
-}
-// A from tensor memory (lane = row, two 16-bit elements per column).
-__device__ __forceinline__ void umma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+// Shared-memory descriptors, low and high words.  All tiles have rows of 128 bytes (64 elements), 128-byte swizzled, in groups of 8
+// rows 1 KiB apart (the stride offset).  Q and K are K-major.  V as the B operand has its N dimension (head_dim) contiguous: blocks of
+// 64 elements are one column block (16 KiB) apart, the leading offset.  Shared addresses fit the 14 bits of the address field (units of
+// 16 bytes), so an advance is an addition to the low word.
+constexpr uint32_t kDescHi = (uint32_t)(1024 >> 4) | (1u << 14) | (2u << 29);  // stride offset, version, 128-byte swizzle
+__device__ __forceinline__ uint32_t desc_lo_k(uint32_t smem_addr) { return (smem_addr >> 4) | (1u << 16); }
+__device__ __forceinline__ uint32_t desc_lo_mn(uint32_t smem_addr) { return (smem_addr >> 4) | ((uint32_t)(16384 >> 4) << 16); }
+// (the whole warp comes here, so that operands stay in uniform registers; the lane with `lead` issues)
+__device__ __forceinline__ void umma_ss(bool lead, uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
       "{\n\t"
-      ".reg .pred p;\n\t"
+      ".reg .pred p, e;\n\t"
+      ".reg .b64 a, b;\n\t"
       "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, {%5, %6, %7, %8}, p;\n\t"
+      "setp.ne.b32 e, %6, 0;\n\t"
+      "mov.b64 a, {%1, %5};\n\t"
+      "mov.b64 b, {%2, %5};\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n\t"
       "}\n" ::"r"(d_tmem),
-      "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(0u), "r"(0u), "r"(0u), "r"(0u)
+      "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(accumulate), "r"(kDescHi), "r"((uint32_t)lead)
       : "memory");
+}
+// A from tensor memory (lane = row, two 16-bit elements per column)
+__device__ __forceinline__ void umma_ts(bool lead, uint32_t d_tmem, uint32_t a_tmem, uint32_t b_lo, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t"
+      ".reg .pred p, e;\n\t"
+      ".reg .b64 b;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "setp.ne.b32 e, %6, 0;\n\t"
+      "mov.b64 b, {%2, %5};\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p;\n\t"
+      "}\n" ::"r"(d_tmem),
+      "r"(a_tmem), "r"(b_lo), "r"(idesc), "r"(accumulate), "r"(kDescHi), "r"((uint32_t)lead)
+      : "memory");
+}
+__device__ __forceinline__ void umma_commit_if(bool lead, uint64_t* bar) {
+  asm volatile("{ .reg .pred e; setp.ne.b32 e, %1, 0; @e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0]; }" ::"r"(smem_u32(bar)), "r"((uint32_t)lead) : "memory");
 }
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* r) {
   asm volatile(
@@ -166,16 +188,78 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* r) {
       "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
       : "memory");
 }
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, float* r) {
+  uint32_t* u = reinterpret_cast<uint32_t*>(r);
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7]), "=r"(u[8]), "=r"(u[9]), "=r"(u[10]),
+        "=r"(u[11]), "=r"(u[12]), "=r"(u[13]), "=r"(u[14]), "=r"(u[15])
+      : "r"(taddr)
+      : "memory");
+}
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
+template <int N>
+__device__ __forceinline__ void regs_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N>
+__device__ __forceinline__ void regs_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+
+// Bounded wait without pauses between the polls (a hundred nanoseconds between a barrier and its waiter would show in every tile).
+__device__ __forceinline__ bool chunk_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag, uint32_t limit) {
+  const uint32_t addr = smem_u32(bar);
+  for (uint32_t spin = 0; spin < limit; ++spin) {
+    uint32_t ok;
+    asm volatile(
+        "{ .reg .pred p; mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }"
+        : "=r"(ok)
+        : "r"(addr), "r"(parity)
+        : "memory");
+    if (ok) return true;
+    if ((spin & 63u) == 63u && *abort_flag) return false;
+  }
+  *abort_flag = 1;
+  return false;
+}
+__device__ __forceinline__ bool elect_one() {
+  uint32_t p;
+  asm volatile("{ .reg .pred q; elect.sync _|q, 0xffffffff; selp.u32 %0, 1, 0, q; }" : "=r"(p));
+  return p != 0u;
+}
+// Barrier of the two warps that share 32 rows, and the same with the disjunction of a predicate.
+__device__ __forceinline__ void pair_sync(int id) { asm volatile("barrier.cta.sync %0, 64;" ::"r"(id) : "memory"); }
+__device__ __forceinline__ bool pair_any(int id, bool v) {
+  uint32_t r;
+  asm volatile("{ .reg .pred p, q; setp.ne.u32 p, %2, 0; barrier.cta.red.or.pred q, %1, 64, p; selp.u32 %0, 1, 0, q; }" : "=r"(r) : "r"(id), "r"((uint32_t)v) : "memory");
+  return r != 0u;
+}
+
+// ---- pairs of fp32 (the packed instructions round each half as the scalar ones do)
+typedef unsigned long long f2;
+__device__ __forceinline__ f2 f2_make(float a, float b) { return pack_f32x2(a, b); }
+__device__ __forceinline__ void f2_split(f2 v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ f2 f2_fma(f2 a, f2 b, f2 c) {
+  f2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ f2 f2_add(f2 a, f2 b) {
+  f2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
 // byte offset of 16-byte chunk c of row r in a [rows][64 elements] block with 128-byte swizzle
 __device__ __forceinline__ int chunk_swz(int r, int c) { return r * 128 + ((c ^ (r & 7)) << 4); }
 
-// The 32 columns of a row that the bits of `see` keep; the others become minus infinity.
+// The 16 scores that the low bits of `see` keep; the others become minus infinity.
 __device__ __forceinline__ void chunk_mask(float* s, uint32_t see) {
 #pragma unroll
-  for (int e = 0; e < 32; ++e)
+  for (int e = 0; e < 16; ++e)
     if (!((see >> e) & 1u)) s[e] = -INFINITY;
 }
 // Bits of 32 keys from key k0 on that a row with last key lim may see, out of those that exist.
@@ -183,6 +267,13 @@ __device__ __forceinline__ uint32_t chunk_see(uint32_t there, int k0, int lim) {
   const int n = lim - k0;  // keys k0 .. k0 + n are seen
   return n >= 31 ? there : n < 0 ? 0u : there & ((2u << n) - 1u);
 }
+
+struct ChunkYes {
+  static constexpr bool value = true;
+};
+struct ChunkNo {
+  static constexpr bool value = false;
+};
 
 template <int D, bool FP8>
 __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const ChunkParams c) {
@@ -204,9 +295,11 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   uint32_t* s_masks = tmem_slot + 4;           // [kChunkMaskRing][4]: keys of the tile that the table names
   uint32_t* s_bad = s_masks + 4 * kChunkMaskRing;  // [kChunkMaskRing][4]: a loading warp's part of the V tile holds values that are not
-                                                   // finite (looked for in causal tiles only)
-  float* s_qscale = reinterpret_cast<float*>(s_bad + 4 * kChunkMaskRing);  // [256], 8-bit cache: the rows' powers of two, inverted
-  __shared__ int64_t s_warp[32], s_found[2];
+                                                   // finite // finite (looked for
+  float* s_pair = reinterpret_cast<float*>(s_bad + 4 * kChunkMaskRing);  // [256]: exchange between the two threads of a row
+  uint8_t* s_qexp = reinterpret_cast<uint8_t*>(s_pair + kChunkRows);  // [256], 8-bit cache: exponent fields of the rows' inverse powers of two
+  int64_t* s_warp = reinterpret_cast<int64_t*>(s_qexp + kChunkRows);  // [32]
+  int64_t* s_found = s_warp + 32;                                      // [2]
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
@@ -218,7 +311,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
     }
     for (int h = 0; h < 2; ++h) {
       mbar_init(&s_full[h], 1);
-      mbar_init(&p_full[h], 4);
+      mbar_init(&p_full[h], 8);
       mbar_init(&o_full[h], 1);
     }
     *abort_flag = 0;
@@ -227,15 +320,15 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
   }
   grid_dependency_wait();  // (before tensor memory is taken: a kernel before this one may still hold it)
   grid_launch_dependents();
-  if (warp == 12) {
+  if (warp == 20) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(C::kTmemCols) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = *tmem_slot;
-  const uint32_t limit = c.spin_limit ? c.spin_limit : kSpinLimit;
+  const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_slot, 0);
+  const uint32_t limit = c.spin_limit ? c.spin_limit : kChunkSpinLimit;
 
   const int64_t total = chunk_total<kChunkThreads>(c, s_warp);
   const int64_t share = attn_share(total, gridDim.x, c.min_share);
@@ -256,15 +349,16 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
     return end <= 0 ? 0 : seg.t1 - seg.t0;
   };
 
-  if (warp >= 8 && warp < 12) {
+  if (warp >= 16 && warp < 20) {
     // ------------------------------------------------------------------ loads
-    const int w = warp - 8, lt = tid - 8 * 32;
+    regs_down<kChunkRegsLoads>();
+    const int w = warp - 16, lt = tid - 16 * 32;
     bool ok = !c.mute_producer;
     uint32_t q_ph = 1;
-    int stage = 0, unpublished = 0, pub = 0, mask_at = 0;
+    int stage = 0, pub = 0, unpublished = 0, mask_at = 0;
     uint32_t ph = 1;
+    // the oldest tile's copies have landed: make them visible to the tensor cores, then count the warp in
     auto publish = [&] {
-      // this thread's copies into the stage have landed: make them visible to the tensor cores, then count the warp in
       fence_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(&kv_full[pub]);
@@ -279,54 +373,46 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
       const int row0 = seg.rt * kChunkRows, rows = min(kChunkRows, q.rows - row0);
       const int pos0 = q.len - q.n;
       const int key_end = min(q.keys, pos0 + (row0 + rows - 1) / p.group + 1), lim_min = pos0 + row0 / p.group;
-      // everything in flight becomes visible before this warp waits for the unit before to end
-      if (!FP8) cp_async_wait<0>();
-      while (unpublished > 0) publish();
-      ok = mbar_wait(q_empty, q_ph, abort_flag, limit);
-      q_ph ^= 1u;
-      if (!ok) break;
-      // ---- queries: a warp takes 64 rows, 32 lanes a row (D / 32 elements each)
-      {
-        constexpr int kE = D / 32;  // 2 or 4 elements per lane
-#pragma unroll 4
-        for (int i = 0; i < kChunkRows / 4; ++i) {
-          const int row = w * (kChunkRows / 4) + i;
-          uint32_t x[kE / 2];
+      // ---- queries, once the products of the unit before have read theirs: a warp takes 64 rows, 16 bytes a lane
+      auto load_queries = [&] {
+        ok = chunk_wait(q_empty, q_ph, abort_flag, limit);
+        q_ph ^= 1u;
+        if (!ok) return;
+        constexpr int kLanes = D / 8, kPerWarp = 32 / kLanes, kBatch = 4;  // lanes of a row, rows of a load, loads in flight
+        const int ql = lane % kLanes;
+#pragma unroll 1
+        for (int i0 = 0; i0 < kChunkRows / 4 / kPerWarp; i0 += kBatch) {
+          uint4 x[kBatch];
 #pragma unroll
-          for (int e = 0; e < kE / 2; ++e) x[e] = 0u;
-          if (row < rows) {
-            const int R = row0 + row;
-            const __nv_bfloat16* src = p.q + (int64_t)(q.q0 + R / p.group) * p.q_ts + (int64_t)(seg.kvh * p.group + R % p.group) * p.q_hs + lane * kE;
-            if constexpr (kE == 4) {
-              const uint2 y = *reinterpret_cast<const uint2*>(src);
-              x[0] = y.x, x[1] = y.y;
-            } else {
-              x[0] = *reinterpret_cast<const uint32_t*>(src);
+          for (int i = 0; i < kBatch; ++i) {
+            const int row = w * (kChunkRows / 4) + (i0 + i) * kPerWarp + lane / kLanes, R = row0 + row;
+            x[i] = make_uint4(0u, 0u, 0u, 0u);
+            if (row < rows)
+              x[i] = *reinterpret_cast<const uint4*>(p.q + (int64_t)(q.q0 + R / p.group) * p.q_ts + (int64_t)(seg.kvh * p.group + R % p.group) * p.q_hs + ql * 8);
+          }
+#pragma unroll
+          for (int i = 0; i < kBatch; ++i) {
+            const int row = w * (kChunkRows / 4) + (i0 + i) * kPerWarp + lane / kLanes;
+            uint32_t y[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+            if constexpr (FP8) {  // to fp16 by a power of two per row (see attend.cuh)
+              float m = 0.f;
+#pragma unroll
+              for (int e = 0; e < 4; ++e) m = fmaxf(m, fmaxf(fabsf(bf16lo(y[e])), fabsf(bf16hi(y[e]))));
+#pragma unroll
+              for (int o = kLanes / 2; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+              const int ex = min(max(268 - (int)(__float_as_uint(m) >> 23), 13), 227);
+              const float f = __uint_as_float((uint32_t)ex << 23);
+              if (ql == 0) s_qexp[row] = (uint8_t)(254 - ex);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) y[e] = pack_half(bf16lo(y[e]) * f, bf16hi(y[e]) * f);
             }
+            *reinterpret_cast<uint4*>(q_smem + (row >> 7) * (C::kQBytes / 2) + (ql >> 3) * 16384 + chunk_swz(row & 127, ql & 7)) = make_uint4(y[0], y[1], y[2], y[3]);
           }
-          if constexpr (FP8) {  // to fp16 by a power of two per row (see attend.cuh)
-            float m = 0.f;
-#pragma unroll
-            for (int e = 0; e < kE / 2; ++e) m = fmaxf(m, fmaxf(fabsf(bf16lo(x[e])), fabsf(bf16hi(x[e]))));
-#pragma unroll
-            for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-            const int ex = min(max(268 - (int)(__float_as_uint(m) >> 23), 13), 227);
-            const float f = __uint_as_float((uint32_t)ex << 23);
-            if (lane == 0) s_qscale[row] = __uint_as_float((uint32_t)(254 - ex) << 23);
-#pragma unroll
-            for (int e = 0; e < kE / 2; ++e) x[e] = pack_half(bf16lo(x[e]) * f, bf16hi(x[e]) * f);
-          }
-          const int byte = lane * kE * 2, blk = byte >> 7, in = byte & 127;
-          uint8_t* dst = q_smem + (row >> 7) * (C::kQBytes / 2) + blk * 16384 + chunk_swz(row & 127, in >> 4) + (in & 15);
-          if constexpr (kE == 4)
-            *reinterpret_cast<uint2*>(dst) = make_uint2(x[0], x[1]);
-          else
-            *reinterpret_cast<uint32_t*>(dst) = x[0];
         }
         fence_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive(q_full);
-      }
+      };
       // ---- tiles: K, V, K, V ...; a thread looks up key lt of the tile, a warp copies its own 32 keys
       const int32_t* table = p.tables + (int64_t)seg.r * p.max_blocks;
       auto entry_of = [&](int t) {
@@ -345,7 +431,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
         if (lane == 0) s_masks[mask_at * 4 + w] = mask;
         bool bad = false;
         for (int kv = 0; kv < 2; ++kv) {
-          ok = mbar_wait(&kv_empty[stage], ph, abort_flag, limit);
+          ok = chunk_wait(&kv_empty[stage], ph, abort_flag, limit);
           if (!ok) break;
           uint8_t* dst = ring + stage * C::kTileBytes;
           const uint8_t* base = kv ? p.v_cache : p.k_cache;
@@ -359,7 +445,6 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
 #pragma unroll
               for (int b = 0; b < C::kHalves; ++b) cp_async16(du + b * 16384 + chunk_swz(row, ch), base + ro + b * 128 + ch * 16, there);
             }
-            cp_async_commit();
           } else {
             constexpr int kLoads = 32 * D / 512;  // 16-byte loads per lane: the warp's 32 rows of D bytes
             uint4 x[kLoads];
@@ -389,57 +474,64 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
               *reinterpret_cast<uint4*>(d + chunk_swz(row, 2 * (ch & 3) + 1)) = hi;
             }
           }
+          if (!FP8) cp_async_commit();
           ++unpublished;
-          const int here = stage;
+          if (kv && causal) {
+            if constexpr (!FP8) {
+              // (the last tiles of a unit) wait for the copies and look at the values: one that is not finite would reach rows that
+              // must not see it as 0 * inf.  It becomes zero here, and the epilogue adds it to the rows that see it.
+              asm volatile("cp.async.wait_all;" ::: "memory");
+#pragma unroll
+              for (int i = 0; i < 8; ++i) {
+                const int row = w * 32 + i * 4 + (lane >> 3), ch = lane & 7;
+#pragma unroll
+                for (int b = 0; b < C::kHalves; ++b) {
+                  uint4* at16 = reinterpret_cast<uint4*>(dst + b * 16384 + chunk_swz(row, ch));
+                  const uint4 z = *at16;
+                  const uint32_t y[4] = {z.x, z.y, z.z, z.w};
+                  uint32_t keep[4];
+                  bool some = false;
+#pragma unroll
+                  for (int e = 0; e < 4; ++e) {
+                    keep[e] = ((y[e] & 0x7f80u) == 0x7f80u ? 0u : 0xffffu) | ((y[e] & 0x7f800000u) == 0x7f800000u ? 0u : 0xffff0000u);
+                    some = some || keep[e] != 0xffffffffu;
+                  }
+                  if (some) {
+                    *at16 = make_uint4(y[0] & keep[0], y[1] & keep[1], y[2] & keep[2], y[3] & keep[3]);
+                    bad = true;
+                  }
+                }
+              }
+            }
+            bad = __any_sync(0xffffffffu, bad);
+          }
+          if (kv && lane == 0) s_bad[mask_at * 4 + w] = bad;
+          if (FP8 || (kv && causal)) {
+            while (unpublished > 0) publish();
+          } else if (unpublished > 1) {  // (this one is on its way, the one before has had the time of a tile)
+            cp_async_wait<1>();
+            publish();
+          }
           if (++stage == kChunkStages) {
             stage = 0;
             ph ^= 1u;
           }
-          if constexpr (FP8) {
-            if (kv) {
-              const bool any = __any_sync(0xffffffffu, bad);
-              if (lane == 0) s_bad[mask_at * 4 + w] = any;
-            }
-            publish();
-          } else {
-            if (kv && !causal && lane == 0) s_bad[mask_at * 4 + w] = 0u;
-            if (kv && causal) {
-              // (the last tiles of a unit) wait for the copies and look at the values: one that is not finite would reach rows that
-              // must not see it as 0 * inf.  It becomes zero here, and the epilogue adds it to the rows that see it.
-              cp_async_wait<0>();
-#pragma unroll 1
-              for (int i = 0; i < 8; ++i) {
-                const int row = w * 32 + i * 4 + (lane >> 3), ch = lane & 7;
-                for (int b = 0; b < C::kHalves; ++b) {
-                  uint32_t* z = reinterpret_cast<uint32_t*>(ring + here * C::kTileBytes + b * 16384 + chunk_swz(row, ch));
-                  for (int e = 0; e < 4; ++e) {
-                    uint32_t m = 0u;
-                    if ((z[e] & 0x7f80u) == 0x7f80u) m |= 0xffffu;
-                    if ((z[e] & 0x7f800000u) == 0x7f800000u) m |= 0xffff0000u;
-                    if (m) {
-                      z[e] &= ~m;
-                      bad = true;
-                    }
-                  }
-                }
-              }
-              const bool any = __any_sync(0xffffffffu, bad);
-              if (lane == 0) s_bad[mask_at * 4 + w] = any;
-              while (unpublished > 0) publish();
-            } else if (unpublished > kChunkLag) {
-              cp_async_wait<kChunkLag>();
-              publish();
-            }
+          if (kv == 0 && t == seg.t0) {  // the first K tile is on its way
+            // (and everything before it is published: the unit before can end)
+            load_queries();
+            if (!ok) break;
           }
         }
         if (++mask_at == kChunkMaskRing) mask_at = 0;
       }
     }
-    if (!FP8) cp_async_wait<0>();
+    cp_async_wait<0>();
     while (unpublished > 0) publish();
-  } else if (warp == 12) {
+  } else if (warp >= 20) {
     // ------------------------------------------------------------------ tensor-core issue
-    if (lane == 0) {
+    regs_down<kChunkRegsIssue>();
+    if (warp == 20) {
+      const bool lead = elect_one();
       constexpr uint32_t kTypes = FP8 ? 0u : (1u << 7) | (1u << 10);  // fp16 or bf16 operands
       constexpr uint32_t kIdescS = (1u << 4) | kTypes | ((uint32_t)(kChunkKeys >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
       constexpr uint32_t kIdescO = (1u << 4) | kTypes | (1u << 16) | ((uint32_t)(D >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
@@ -453,45 +545,43 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
         const int nt = n_tiles();
         if (nt == 0) continue;
         const int halves = min(kChunkRows, seg.q.rows - seg.rt * kChunkRows) > 128 ? 2 : 1;
-        ok = mbar_wait(q_full, q_ph, abort_flag, limit);
+        ok = chunk_wait(q_full, q_ph, abort_flag, limit);
         q_ph ^= 1u;
         int v_stage = 0;
         uint32_t v_ph = 0;
         for (int j = 0; ok && j <= nt; ++j) {
           int k_stage = stage;
           if (j < nt) {
-            ok = mbar_wait(&kv_full[stage], ph, abort_flag, limit);
+            ok = chunk_wait(&kv_full[stage], ph, abort_flag, limit);
             if (!ok) break;
           }
           for (int h = 0; ok && h < halves; ++h) {
             if (j > 0) {  // O += P V of the tile before
-              if (h == 0) ok = mbar_wait(&kv_full[v_stage], v_ph, abort_flag, limit);
-              if (ok) ok = mbar_wait(&p_full[h], p_ph[h], abort_flag, limit);
+              if (h == 0) ok = chunk_wait(&kv_full[v_stage], v_ph, abort_flag, limit);
+              if (ok) ok = chunk_wait(&p_full[h], p_ph[h], abort_flag, limit);
               if (!ok) break;
               p_ph[h] ^= 1u;
               tc_fence_after();
-              const uint64_t vd = umma_desc_mn_sw128(ring_u + v_stage * C::kTileBytes, 16384);
+              const uint32_t vd = desc_lo_mn(ring_u + v_stage * C::kTileBytes);
 #pragma unroll
               for (int k = 0; k < kChunkKeys / 16; ++k)  // 16 keys are two 1 KiB groups
-                umma_f16_ts(tmem + C::kColO + h * D, tmem + h * kChunkKeys + k * 8, vd + (uint64_t)(k * 128), kIdescO, (j > 1 || k > 0) ? 1u : 0u);
-              if (h == halves - 1) umma_commit(&kv_empty[v_stage]);
-              if (j == nt) umma_commit(&o_full[h]);
+                umma_ts(lead, tmem + C::kColO + h * D, tmem + h * kChunkKeys + k * 8, vd + k * 128, kIdescO, (j > 1 || k > 0) ? 1u : 0u);
+              if (h == halves - 1) umma_commit_if(lead, &kv_empty[v_stage]);
+              if (j == nt) umma_commit_if(lead, &o_full[h]);
             }
             if (j < nt) {  // S = Q K^T
               tc_fence_after();
+              const uint32_t qd = desc_lo_k(q_u + h * (C::kQBytes / 2)), kd = desc_lo_k(ring_u + k_stage * C::kTileBytes);
 #pragma unroll
-              for (int k = 0; k < D / 16; ++k) {
-                const uint64_t qd = umma_desc_k_sw128(q_u + h * (C::kQBytes / 2) + (k >> 2) * 16384) + (uint64_t)(2 * (k & 3));
-                const uint64_t kd = umma_desc_k_sw128(ring_u + k_stage * C::kTileBytes + (k >> 2) * 16384) + (uint64_t)(2 * (k & 3));
-                umma_f16(tmem + h * kChunkKeys, qd, kd, kIdescS, k > 0 ? 1u : 0u);
-              }
-              umma_commit(&s_full[h]);
+              for (int k = 0; k < D / 16; ++k)  // 16 elements are 32 bytes of a row, 64 a column block
+                umma_ss(lead, tmem + h * kChunkKeys, qd + (k >> 2) * 1024 + 2 * (k & 3), kd + (k >> 2) * 1024 + 2 * (k & 3), kIdescS, k > 0 ? 1u : 0u);
+              umma_commit_if(lead, &s_full[h]);
             }
           }
           if (!ok) break;
           if (j < nt) {
-            umma_commit(&kv_empty[k_stage]);
-            if (j == nt - 1) umma_commit(q_empty);
+            umma_commit_if(lead, &kv_empty[k_stage]);
+            if (j == nt - 1) umma_commit_if(lead, q_empty);
             if (++stage == kChunkStages) {
               stage = 0;
               ph ^= 1u;
@@ -509,9 +599,24 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
     __syncwarp();
   } else {
     // ------------------------------------------------------------------ weights, epilogue
-    const int h = warp >> 2, row = tid;  // row of the unit (0 .. 255)
+    regs_up<kChunkRegsWeights>();
+    const int h = warp >> 3, part = (warp >> 2) & 1;     // half of the rows; half of a tile's keys and of the accumulator's columns
+    const int row = h * 128 + (warp & 3) * 32 + lane;    // of the unit
+    const int pair = 1 + h * 4 + (warp & 3);             // barrier of the two warps that share these rows
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-    const uint32_t ts = tmem + lanes + h * kChunkKeys, to = tmem + lanes + C::kColO + h * D;
+    const uint32_t ts = tmem + lanes + h * kChunkKeys, to = tmem + lanes + C::kColO + h * D + part * (D / 2);
+    // both threads of a row get what `join` makes of their values
+    auto pair_join = [&](float v, auto join) {
+      if (part) s_pair[row] = v;
+      pair_sync(pair);
+      if (!part) {
+        v = join(v, s_pair[row]);
+        s_pair[row] = v;
+      }
+      pair_sync(pair);
+      if (part) v = s_pair[row];
+      return v;
+    };
     bool ok = true;
     uint32_t s_ph = 0, o_ph = 0;
     int mask_at = 0;
@@ -520,102 +625,130 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
       const int nt = n_tiles();
       const AttnReq& q = seg.q;
       const int row0 = seg.rt * kChunkRows, rows = min(kChunkRows, q.rows - row0);
-      const bool active = h == 0 || rows > 128;
-      const int pos0 = q.len - q.n;
-      const int lim = pos0 + (row0 + min(row, rows - 1)) / p.group, lim_min = pos0 + row0 / p.group;
-      if (!active) {
+      if (h == 1 && rows <= 128) {
         mask_at = (mask_at + nt) % kChunkMaskRing;
         continue;
       }
+      const int pos0 = q.len - q.n;
+      const int lim = pos0 + (row0 + min(row, rows - 1)) / p.group, lim_min = pos0 + row0 / p.group;
       float m = -INFINITY, l = 0.f, sc = p.scale_log2;
       bool any_bad = false;
       int v_at = 0;
+      bool v_causal = false;  // the tile before was a causal one
       auto look_at_v = [&] {
         const uint4 b = *reinterpret_cast<const uint4*>(s_bad + v_at * 4);
         any_bad = any_bad || (b.x | b.y | b.z | b.w) != 0u;
       };
       for (int j = 0; j < nt; ++j) {
-        ok = mbar_wait(&s_full[h], s_ph, abort_flag, limit);
+        ok = chunk_wait(&s_full[h], s_ph, abort_flag, limit);
         s_ph ^= 1u;
-        if (!ok) break;
         tc_fence_after();
-        if (FP8 && j == 0) sc = p.scale_log2 * s_qscale[row];
-        const int k0 = (seg.t0 + j) * kChunkKeys;
-        const uint4 there = *reinterpret_cast<const uint4*>(s_masks + mask_at * 4);
-        if (j > 0) look_at_v();  // (of the tile before: its product with V was issued before these scores)
+        if (FP8 && j == 0) sc = p.scale_log2 * __uint_as_float((uint32_t)s_qexp[row] << 23);
+        const int k0 = (seg.t0 + j) * kChunkKeys + part * 64;
+        const uint2 there = *reinterpret_cast<const uint2*>(s_masks + mask_at * 4 + part * 2);
+        if (v_causal) look_at_v();  // (of the tile before: its product with V was issued before these scores)
         v_at = mask_at;
+        v_causal = (seg.t0 + j) * kChunkKeys + kChunkKeys - 1 > lim_min;
         if (++mask_at == kChunkMaskRing) mask_at = 0;
-        const uint32_t tw[4] = {there.x, there.y, there.z, there.w};
-        const bool masked = k0 + kChunkKeys - 1 > lim_min || (there.x & there.y & there.z & there.w) != 0xffffffffu;
-        uint32_t pk[kChunkKeys / 2];
-        float sum = 0.f, mx = -INFINITY;
-        // weights with maximum `mm` of the 128 scores, packed; their sum and the scores' maximum
-        auto form = [&](float mm) {
-          const float sub = mm == -INFINITY ? 0.f : mm;
-          float s0 = 0.f, s1 = 0.f, x0 = -INFINITY, x1 = -INFINITY;
+        const bool masked = k0 + 63 > lim_min || (there.x & there.y) != 0xffffffffu;
+        uint32_t pk[32];
+        float sum = 0.f;
+        // weights of the 64 scores with maximum `mm`, packed, and their sum
+        auto form = [&](float mm, auto with_mask) {
+          const float sub = mm == -INFINITY ? 0.f : -mm;
+          const f2 sc2 = f2_make(sc, sc), sub2 = f2_make(sub, sub);
+          f2 total2 = 0ull;
 #pragma unroll
           for (int b = 0; b < 4; ++b) {
-            float s[32];
-            tmem_ld32(ts + b * 32, s);
+            float s[16];
+            tmem_ld16(ts + part * 64 + b * 16, s);
             tmem_ld_wait();
-            if (masked) chunk_mask(s, chunk_see(tw[b], k0 + b * 32, lim));
+            if (with_mask.value) chunk_mask(s, chunk_see(b >= 2 ? there.y : there.x, k0 + (b >> 1) * 32, lim) >> ((b & 1) * 16));
 #pragma unroll
-            for (int e = 0; e < 32; e += 2) {
-              x0 = fmaxf(x0, s[e]);
-              x1 = fmaxf(x1, s[e + 1]);
-              const float w0 = ex2(fmaf(s[e], sc, -sub)), w1 = ex2(fmaf(s[e + 1], sc, -sub));
-              s0 += w0;
-              s1 += w1;
-              pk[b * 16 + e / 2] = FP8 ? pack_half(w0, w1) : pack_bf16(w0, w1);
+            for (int e = 0; e < 16; e += 2) {
+              float w0, w1;
+              f2_split(f2_fma(f2_make(s[e], s[e + 1]), sc2, sub2), w0, w1);
+              w0 = ex2(w0);
+              w1 = ex2(w1);
+              total2 = f2_add(total2, f2_make(w0, w1));
+              pk[b * 8 + e / 2] = FP8 ? pack_half(w0, w1) : pack_bf16(w0, w1);
             }
           }
-          sum = s0 + s1;
-          mx = fmaxf(x0, x1);
+          float a, b;
+          f2_split(total2, a, b);
+          sum = a + b;
         };
-        form(m);
-        const float top = mx * sc;
-        if (__any_sync(0xffffffffu, top > m + kChunkSlack)) {  // (always in a unit's first tile)
-          const float n = top > m + kChunkSlack ? top : m;
+        auto form_any = [&](float mm) {
+          if (masked)
+            form(mm, ChunkYes{});
+          else
+            form(mm, ChunkNo{});
+        };
+        if (ok) form_any(m);
+        // (always in a segment's first tile, rarely later; also the point from which both warps have read their scores, over which
+        // the weights are stored)
+        const bool renew = sum > kChunkMaxSum || m == -INFINITY;
+        if (pair_any(pair, !ok || renew)) {
+          if (pair_any(pair, !ok)) {  // a wait ran out: both warps leave together, neither is left at a barrier
+            ok = false;
+            break;
+          }
+          float mx = -INFINITY;
+#pragma unroll 1
+          for (int b = 0; b < 4; ++b) {
+            float s[16];
+            tmem_ld16(ts + part * 64 + b * 16, s);
+            tmem_ld_wait();
+            if (masked) chunk_mask(s, chunk_see(b >= 2 ? there.y : there.x, k0 + (b >> 1) * 32, lim) >> ((b & 1) * 16));
+#pragma unroll
+            for (int e = 0; e < 16; e += 2) mx = max3(mx, s[e], s[e + 1]);
+          }
+          // (a row's maximum changes by its own scores alone, so that a row does not depend on its neighbours)
+          mx = pair_join(mx, [](float a, float b) { return fmaxf(a, b); });
+          const bool own = pair_join(renew ? 1.f : 0.f, [](float a, float b) { return fmaxf(a, b); }) != 0.f;
+          const float n = own ? fmaxf(m, mx * sc) : m;
           const float f = n == -INFINITY || m == n ? 1.f : ex2(m - n);
           if (j > 0) {
             // the accumulator holds the tiles before this one (the commit that signalled these scores follows their product)
 #pragma unroll 1
-            for (int b = 0; b < D / 32; ++b) {
-              float o[32];
-              tmem_ld32(to + b * 32, o);
+            for (int b = 0; b < D / 2; b += 16) {
+              float o[16];
+              tmem_ld16(to + b, o);
               tmem_ld_wait();
 #pragma unroll
-              for (int e = 0; e < 32; ++e) o[e] *= f;
-              tmem_st16(to + b * 32, reinterpret_cast<const uint32_t*>(o));
-              tmem_st16(to + b * 32 + 16, reinterpret_cast<const uint32_t*>(o) + 16);
+              for (int e = 0; e < 16; ++e) o[e] *= f;
+              tmem_st16(to + b, reinterpret_cast<const uint32_t*>(o));
             }
           }
           l *= f;
           m = n;
-          form(m);
+          form_any(m);
+          pair_sync(pair);
         }
         l += sum;
-#pragma unroll
-        for (int b = 0; b < 4; ++b) tmem_st16(ts + b * 16, pk + b * 16);
+        tmem_st16(ts + part * 32, pk);
+        tmem_st16(ts + part * 32 + 16, pk + 16);
         tmem_st_wait();
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(&p_full[h]);
       }
       if (ok && nt > 0) {
-        ok = mbar_wait(&o_full[h], o_ph, abort_flag, limit);
+        ok = chunk_wait(&o_full[h], o_ph, abort_flag, limit);
         o_ph ^= 1u;
         tc_fence_after();
-        look_at_v();
+        if (v_causal) look_at_v();
+        ok = !pair_any(pair, !ok);
       }
       if (!ok) break;
-      // ---- epilogue: this thread's row
+      // ---- epilogue: this thread's half of its row
+      if (nt > 0) l = pair_join(l, [](float a, float b) { return a + b; });
       const bool whole = seg.t0 == 0 && seg.t1 == seg.tiles;
       const bool mine = row < rows;
       const int R = row0 + min(row, rows - 1), tok = q.q0 + R / p.group, head = seg.kvh * p.group + R % p.group;
       const float inv = l == 0.f ? 0.f : p.v_scale / l;
       const int64_t slot = (int64_t)blockIdx.x * 2 + (seg.t0 == 0 ? 1 : 0);
-      if (mine) {
+      if (mine && part == 0) {
         if (whole) {
           if (p.lse) p.lse[(int64_t)tok * p.n_q + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
         } else {
@@ -623,14 +756,15 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
         }
       }
 #pragma unroll 1
-      for (int b = 0; b < D / 32; ++b) {
-        float o[32];
+      for (int b = 0; b < D / 2; b += 16) {
+        const int col = part * (D / 2) + b;
+        float o[16];
         if (nt > 0) {
-          tmem_ld32(to + b * 32, o);
+          tmem_ld16(to + b, o);
           tmem_ld_wait();
         } else {
 #pragma unroll
-          for (int e = 0; e < 32; ++e) o[e] = 0.f;
+          for (int e = 0; e < 16; ++e) o[e] = 0.f;
         }
         if (any_bad) {
           // values that are not finite, at the keys of this segment's causal tiles that the row sees: their weight is positive, so
@@ -643,11 +777,11 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
             if (blk < 0 || blk >= p.num_blocks) continue;
             const uint8_t* v = p.v_cache + blk * p.block_stride + (key % p.block_size) * p.token_stride + seg.kvh * p.head_stride;
 #pragma unroll
-            for (int e = 0; e < 32; ++e) {
+            for (int e = 0; e < 16; ++e) {
               if (FP8) {
-                if ((v[b * 32 + e] & 0x7f) == 0x7f) o[e] = NAN;
+                if ((v[col + e] & 0x7f) == 0x7f) o[e] = NAN;
               } else {
-                const uint32_t x = (uint32_t)reinterpret_cast<const uint16_t*>(v)[b * 32 + e] << 16;
+                const uint32_t x = (uint32_t)reinterpret_cast<const uint16_t*>(v)[col + e] << 16;
                 if ((x & 0x7f800000u) == 0x7f800000u) o[e] += __uint_as_float(x);
               }
             }
@@ -655,15 +789,15 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
         }
         if (mine) {
           if (whole) {
-            __nv_bfloat16* dst = p.out + tok * p.o_ts + head * p.o_hs + b * 32;
+            __nv_bfloat16* dst = p.out + tok * p.o_ts + head * p.o_hs + col;
 #pragma unroll
-            for (int e = 0; e < 32; e += 8)
+            for (int e = 0; e < 16; e += 8)
               *reinterpret_cast<uint4*>(dst + e) = make_uint4(pack_bf16(o[e] * inv, o[e + 1] * inv), pack_bf16(o[e + 2] * inv, o[e + 3] * inv),
                                                               pack_bf16(o[e + 4] * inv, o[e + 5] * inv), pack_bf16(o[e + 6] * inv, o[e + 7] * inv));
           } else {
 #pragma unroll
-            for (int e = 0; e < 32; e += 4)
-              *reinterpret_cast<float4*>(c.part_o + ((slot * (D / 4) + b * 8 + e / 4) * kChunkRows + row) * 4) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+            for (int e = 0; e < 16; e += 4)
+              *reinterpret_cast<float4*>(c.part_o + ((slot * (D / 4) + (col + e) / 4) * kChunkRows + row) * 4) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
           }
         }
       }
@@ -677,7 +811,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
     for (int w = 0; w < 4096; ++w) __nanosleep(256);  // let products and copies that may still be in flight end
   }
   if (tid == 0) c.errors[blockIdx.x] = *abort_flag;
-  if (warp == 12) {
+  if (warp == 20) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(C::kTmemCols) : "memory");
   }
