@@ -313,6 +313,7 @@ class MemStore:
                       kv_arena.numel() * kv_arena.element_size() if kv_arena is not None else 0, max_host_kv_tokens,
                       rotary_dim, 0)  # fmt: skip
         self.n_layers, self.n_kv_heads, self.head_dim, self.emb_dim = n_layers, n_kv_heads, head_dim, emb_dim
+        self._index, self._workspace_bytes = self.device.index, None
         rc = self._lib.memstore_create(C.byref(cfg), C.byref(self._h))
         if rc != MS_OK:
             self._h = C.c_void_p()
@@ -556,104 +557,107 @@ class MemStore:
         self._check(self._lib.memstore_set_profile_repeats(self._h, int(n)))
 
     # -- the serving step around the cache -----------------------------------------------------------
-    def _on(self, t: torch.Tensor | None, dtype, name: str, shape: tuple | None = None):
-        """Pointer of a contiguous tensor on the store's device."""
-        if t is None:
-            return None
-        ptr = _dev_ptr(t, dtype, name)
-        if t.device != self.device:
+    # (these calls are made once per layer and token: every check below is one comparison, and a failed one is explained afterwards)
+    def _ptr(self, t: torch.Tensor, dtype, name: str, shape: tuple | None = None) -> int:
+        """Address of a contiguous tensor on the store's device."""
+        if t.dtype is dtype and t.get_device() == self._index and t.is_contiguous() and (shape is None or t.shape == shape):
+            return t.data_ptr()
+        _dev_ptr(t, dtype, name)
+        if t.get_device() != self._index:
             raise ValueError(f"{name} is on {t.device}, the store on {self.device}")
-        if shape is not None and tuple(t.shape) != shape:
-            raise ValueError(f"{name} must have shape {shape}, got {tuple(t.shape)}")
-        return ptr
+        raise ValueError(f"{name} must have shape {shape}, got {tuple(t.shape)}")
 
     def _heads(self, t: torch.Tensor, n_tokens: int, n_heads: int, name: str) -> _Heads:
         """[n_tokens, n_heads, head_dim] bf16, contiguous in its last dimension, any strides in front of it."""
-        if not t.is_cuda or t.dtype != torch.bfloat16:
+        if t.dtype is not torch.bfloat16 or not t.is_cuda:
             raise TypeError(f"{name} must be a CUDA bfloat16 tensor")
-        if t.device != self.device:
+        if t.get_device() != self._index:
             raise ValueError(f"{name} is on {t.device}, the store on {self.device}")
-        if tuple(t.shape) != (n_tokens, n_heads, self.head_dim):
+        if t.shape != (n_tokens, n_heads, self.head_dim):
             raise ValueError(f"{name} must have shape {(n_tokens, n_heads, self.head_dim)}, got {tuple(t.shape)}")
-        if t.numel() and t.stride(2) != 1:
+        st, sh, sd = t.stride()
+        if sd != 1 and t.numel():
             raise ValueError(f"{name} must be contiguous in its last dimension")
         # (strides of dimensions of one element, which torch leaves arbitrary, are not used)
-        return _Heads(t.data_ptr(), t.stride(0) if n_tokens > 1 else 0, t.stride(1) if n_heads > 1 else 0)
+        return _Heads(t.data_ptr(), st if n_tokens > 1 else 0, sh if n_heads > 1 else 0)
 
-    def _cache(self, cache: PagedCache) -> _PagedCache:
-        for t, n in ((cache.k, "k"), (cache.v, "v")):
-            if t.device != self.device:
-                raise ValueError(f"cache.{n} is on {t.device}, the store on {self.device}")
-        return cache._struct()
+    def _paged(self, cache: PagedCache):
+        c = cache._struct()
+        if cache.k.get_device() != self._index or cache.v.get_device() != self._index:
+            raise ValueError(f"the cache is on {cache.k.device}, the store on {self.device}")
+        return C.byref(c)
 
-    def _stream(self, stream) -> torch.cuda.Stream:
-        return torch.cuda.current_stream(self.device) if stream is None else stream
+    def _raw_stream(self, stream) -> int:
+        """The stream's handle; default: the current stream of the store's device."""
+        return torch._C._cuda_getCurrentRawStream(self._index) if stream is None else stream.cuda_stream
+
+    def _empty(self, stream, *specs):
+        """New tensors (shape, dtype) on the store's device, in the pool of the stream that they are used on."""
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                return [torch.empty(s, dtype=d, device=self.device) for s, d in specs]
+        return [torch.empty(s, dtype=d, device=self.device) for s, d in specs]
 
     def grow_blocks(self, start_lens, new_lens, block_tables, cache: PagedCache, free_blocks, n_taken, token_capacity: int,
                     out: GrownBlocks | None = None, stream=None) -> GrownBlocks:  # fmt: skip
         """Give every request blocks for ``new_lens`` more tokens and list the new tokens' positions and slots
         (``block_tables`` is written in place; ``out`` takes buffers of an earlier result, in which ``seq_lens`` may be
         ``start_lens`` itself and ``n_taken`` the counter itself)."""
-        nreq, cap = start_lens.shape[0], int(token_capacity)
-        stream = self._stream(stream)
-        if out is None:
-            with torch.cuda.stream(stream):
-                e = lambda n, dt=torch.int32: torch.empty((n,), dtype=dt, device=self.device)  # noqa: E731
-                out = GrownBlocks(e(nreq + 1), e(nreq), e(cap), e(cap, torch.int64), e(1), e(nreq))
+        nreq, cap, i32, ptr = start_lens.shape[0], int(token_capacity), torch.int32, self._ptr
         if block_tables.dim() != 2 or block_tables.shape[0] != nreq:
             raise ValueError(f"block_tables must have shape ({nreq}, max_blocks), got {tuple(block_tables.shape)}")
-        i32 = torch.int32
-        rc = self._lib.memstore_grow_blocks(
-            self._h, self._on(start_lens, i32, "start_lens", (nreq,)), self._on(new_lens, i32, "new_lens", (nreq,)), nreq,
-            self._on(block_tables, i32, "block_tables"), block_tables.shape[1], C.byref(self._cache(cache)),
-            self._on(free_blocks, i32, "free_blocks"), free_blocks.numel(), self._on(n_taken, i32, "n_taken", (1,)), cap,
-            self._on(out.q_start, i32, "out.q_start", (nreq + 1,)), self._on(out.seq_lens, i32, "out.seq_lens", (nreq,)),
-            self._on(out.positions, i32, "out.positions", (cap,)), self._on(out.slots, torch.int64, "out.slots", (cap,)),
-            self._on(out.n_taken, i32, "out.n_taken", (1,)), self._on(out.status, i32, "out.status", (nreq,)),
-            C.c_void_p(stream.cuda_stream))  # fmt: skip
-        self._check(rc)
+        if out is None:
+            ints, slots = self._empty(stream, (3 * nreq + 2 + max(cap, 0), i32), (max(cap, 0), torch.int64))
+            q_start, lens, status, taken, positions = ints.split_with_sizes((nreq + 1, nreq, nreq, 1, max(cap, 0)))
+            out = GrownBlocks(q_start, lens, positions, slots, taken, status)
+            at = ints.data_ptr()
+            outs = (at, at + 4 * (nreq + 1), at + 4 * (3 * nreq + 2), slots.data_ptr(), at + 4 * (3 * nreq + 1), at + 4 * (2 * nreq + 1))
+        else:
+            outs = (ptr(out.q_start, i32, "out.q_start", (nreq + 1,)), ptr(out.seq_lens, i32, "out.seq_lens", (nreq,)),
+                    None if out.positions is None else ptr(out.positions, i32, "out.positions", (cap,)),
+                    None if out.slots is None else ptr(out.slots, torch.int64, "out.slots", (cap,)),
+                    ptr(out.n_taken, i32, "out.n_taken", (1,)), ptr(out.status, i32, "out.status", (nreq,)))  # fmt: skip
+        self._check(self._lib.memstore_grow_blocks(
+            self._h, ptr(start_lens, i32, "start_lens", (nreq,)), ptr(new_lens, i32, "new_lens", (nreq,)), nreq,
+            ptr(block_tables, i32, "block_tables"), block_tables.shape[1], self._paged(cache), ptr(free_blocks, i32, "free_blocks"),
+            free_blocks.numel(), ptr(n_taken, i32, "n_taken", (1,)), cap, *outs, self._raw_stream(stream)))  # fmt: skip
         return out
 
     def release_blocks(self, seq_lens, block_tables, cache: PagedCache, free_blocks, n_taken, release=None, out_status=None,
                        stream=None) -> None:  # fmt: skip
         """Return the blocks of the requests with ``release[r] != 0`` (None: all) to the free list; their table entries
         become -1 and their lengths 0, all in place."""
-        nreq, i32 = seq_lens.shape[0], torch.int32
+        nreq, i32, ptr = seq_lens.shape[0], torch.int32, self._ptr
         if block_tables.dim() != 2 or block_tables.shape[0] != nreq:
             raise ValueError(f"block_tables must have shape ({nreq}, max_blocks), got {tuple(block_tables.shape)}")
-        rc = self._lib.memstore_release_blocks(
-            self._h, self._on(release, i32, "release", (nreq,)), self._on(seq_lens, i32, "seq_lens", (nreq,)), nreq,
-            self._on(block_tables, i32, "block_tables"), block_tables.shape[1], C.byref(self._cache(cache)),
-            self._on(free_blocks, i32, "free_blocks"), free_blocks.numel(), self._on(n_taken, i32, "n_taken", (1,)),
-            self._on(out_status, i32, "out_status", (nreq,)), C.c_void_p(self._stream(stream).cuda_stream))  # fmt: skip
-        self._check(rc)
+        self._check(self._lib.memstore_release_blocks(
+            self._h, None if release is None else ptr(release, i32, "release", (nreq,)), ptr(seq_lens, i32, "seq_lens", (nreq,)), nreq,
+            ptr(block_tables, i32, "block_tables"), block_tables.shape[1], self._paged(cache), ptr(free_blocks, i32, "free_blocks"),
+            free_blocks.numel(), ptr(n_taken, i32, "n_taken", (1,)), None if out_status is None else ptr(out_status, i32, "out_status", (nreq,)),
+            self._raw_stream(stream)))  # fmt: skip
 
     def append(self, layer: int, q, k, v, positions, slots, cache: PagedCache, q_out=None, out_status=None, stream=None):
         """Rotate ``q`` [T, n_q_heads, d] (or None) and ``k`` [T, h, d] at ``positions`` (int32) and write K and V into
         ``layer`` of the cache at ``slots`` (int64, negative: not written).  Returns the rotated queries (``q_out``, a new
         tensor unless given; it may be ``q`` itself, in place)."""
-        T = k.shape[0]
-        stream = self._stream(stream)
-        n_q = 0
-        hq = ho = None
+        T, n_q, hq, ho = k.shape[0], 0, None, None
         if q is not None:
             n_q = q.shape[1]
             hq = self._heads(q, T, n_q, "q")
             if q_out is None:
-                with torch.cuda.stream(stream):
-                    q_out = torch.empty((T, n_q, self.head_dim), dtype=torch.bfloat16, device=self.device)
-            ho = self._heads(q_out, T, n_q, "q_out")
-        rc = self._lib.memstore_append(
-            self._h, layer, C.byref(hq) if hq is not None else None, n_q, C.byref(self._heads(k, T, self.n_kv_heads, "k")),
-            C.byref(self._heads(v, T, self.n_kv_heads, "v")), self._on(positions, torch.int32, "positions", (T,)),
-            self._on(slots, torch.int64, "slots", (T,)), T, C.byref(self._cache(cache)), C.byref(ho) if ho is not None else None,
-            self._on(out_status, torch.int32, "out_status", (T,)), C.c_void_p(stream.cuda_stream))  # fmt: skip
-        self._check(rc)
+                (q_out,) = self._empty(stream, ((T, n_q, self.head_dim), torch.bfloat16))
+            ho = hq if q_out is q else self._heads(q_out, T, n_q, "q_out")
+        self._check(self._lib.memstore_append(
+            self._h, layer, hq, n_q, self._heads(k, T, self.n_kv_heads, "k"), self._heads(v, T, self.n_kv_heads, "v"),
+            self._ptr(positions, torch.int32, "positions", (T,)), self._ptr(slots, torch.int64, "slots", (T,)), T, self._paged(cache), ho,
+            None if out_status is None else self._ptr(out_status, torch.int32, "out_status", (T,)), self._raw_stream(stream)))  # fmt: skip
         return q_out
 
     def attend_workspace_bytes(self) -> int:
         """Bytes of workspace of an ``attend`` call of this store."""
-        return int(self._lib.memstore_attend_workspace(self._h))
+        if self._workspace_bytes is None:
+            self._workspace_bytes = int(self._lib.memstore_attend_workspace(self._h))
+        return self._workspace_bytes
 
     def attend(self, layer: int, q, cache: PagedCache, q_start, seq_lens, block_tables, scale: float = 0.0, max_q_len: int = 0, out=None,
                want_lse: bool = False, out_lse=None, out_status=None, workspace=None, stream=None):  # fmt: skip
@@ -661,24 +665,22 @@ class MemStore:
         of request r's ``seq_lens[r]`` cached ones) over ``layer`` of the cache.  Returns (out, lse or None, out_status).
         ``workspace``: a uint8 tensor of ``attend_workspace_bytes()``; by default one comes from torch's allocator for
         every call, so calls on different streams or in different CUDA graphs have their own."""
-        T, n_q, nreq, i32 = q.shape[0], q.shape[1], seq_lens.shape[0], torch.int32
+        (T, n_q, _), nreq, i32, ptr = q.shape, seq_lens.shape[0], torch.int32, self._ptr
         if block_tables.dim() != 2 or block_tables.shape[0] != nreq:
             raise ValueError(f"block_tables must have shape ({nreq}, max_blocks), got {tuple(block_tables.shape)}")
-        stream = self._stream(stream)
-        with torch.cuda.stream(stream):
-            if out is None:
-                out = torch.empty((T, n_q, self.head_dim), dtype=torch.bfloat16, device=self.device)
-            if out_lse is None and want_lse:
-                out_lse = torch.empty((T, n_q), dtype=torch.float32, device=self.device)
-            if workspace is None:
-                workspace = torch.empty((self.attend_workspace_bytes(),), dtype=torch.uint8, device=self.device)
-        rc = self._lib.memstore_attend(
-            self._h, layer, C.byref(self._heads(q, T, n_q, "q")), n_q, T, self._on(q_start, i32, "q_start", (nreq + 1,)),
-            self._on(seq_lens, i32, "seq_lens", (nreq,)), nreq, self._on(block_tables, i32, "block_tables"), block_tables.shape[1],
-            C.byref(self._cache(cache)), float(scale), int(max_q_len), C.byref(self._heads(out, T, n_q, "out")),
-            self._on(out_lse, torch.float32, "out_lse", (T, n_q)), self._on(out_status, i32, "out_status", (nreq,)),
-            self._on(workspace, torch.uint8, "workspace"), workspace.numel(), C.c_void_p(stream.cuda_stream))  # fmt: skip
-        self._check(rc)
+        hq = self._heads(q, T, n_q, "q")
+        if out is None:
+            (out,) = self._empty(stream, ((T, n_q, self.head_dim), torch.bfloat16))
+        if out_lse is None and want_lse:
+            (out_lse,) = self._empty(stream, ((T, n_q), torch.float32))
+        if workspace is None:
+            (workspace,) = self._empty(stream, (self.attend_workspace_bytes(), torch.uint8))
+        self._check(self._lib.memstore_attend(
+            self._h, layer, hq, n_q, T, ptr(q_start, i32, "q_start", (nreq + 1,)), ptr(seq_lens, i32, "seq_lens", (nreq,)), nreq,
+            ptr(block_tables, i32, "block_tables"), block_tables.shape[1], self._paged(cache), scale, max_q_len,
+            hq if out is q else self._heads(out, T, n_q, "out"), None if out_lse is None else ptr(out_lse, torch.float32, "out_lse", (T, n_q)),
+            None if out_status is None else ptr(out_status, i32, "out_status", (nreq,)), ptr(workspace, torch.uint8, "workspace"),
+            workspace.numel(), self._raw_stream(stream)))  # fmt: skip
         return out, out_lse, out_status
 
     def stats(self) -> dict:
