@@ -26,6 +26,8 @@ constexpr int kAttnWarps = 4;
 constexpr int kAttnThreads = kAttnWarps * 32;
 constexpr int kAttnWarpKeys = 16;  // keys of a warp in a tile
 constexpr int kAttnTileKeys = kAttnWarps * kAttnWarpKeys;
+constexpr int kAttnMaxGroup = 1024;
+constexpr int kAttnMaxCtasPerSm = 3;
 constexpr int32_t kAttnMaxLen = 1 << 30;  // (key numbers stay inside 32 bits)
 
 struct AttendParams {
@@ -33,7 +35,8 @@ struct AttendParams {
   int64_t q_ts, q_hs;
   __nv_bfloat16* out;
   int64_t o_ts, o_hs;
-  int32_t n_q, n_kv, group;  // heads, and query heads per K/V head
+  int32_t n_q, n_kv, group;  // heads, and query heads per K/V head (at most kAttnMaxGroup)
+  uint32_t group_magic;      // floor(2^32 / group) + 1, 0 for group == 1
   int32_t n_tokens;
   const int32_t* q_start;
   const int32_t* seq_lens;
@@ -43,7 +46,7 @@ struct AttendParams {
   const uint8_t *k_cache, *v_cache;                    // of the layer
   int64_t block_stride, token_stride, head_stride;     // bytes
   int64_t num_blocks;
-  int32_t block_size;
+  int32_t block_size, block_shift;  // block_shift: log2 of the block size, or -1
   float scale_log2;  // scale * log2(e) (* k_scale)
   float v_scale;     // 1 for a bf16 cache
   float* lse;        // [n_tokens][n_q] or nullptr
@@ -79,42 +82,104 @@ __device__ __forceinline__ int64_t attn_cost(const AttendParams& p, const AttnRe
   return (int64_t)((a.rows + kAttnRows - 1) / kAttnRows) * p.n_kv * attn_tiles(a);
 }
 
-// All tiles of the call, by the whole block.
-template <int THREADS>
-__device__ __forceinline__ int64_t attn_total(const AttendParams& p, int64_t* s_warp) {
-  int64_t sum = 0;
-  for (int r = threadIdx.x; r < p.nreq; r += THREADS) sum += attn_cost(p, attn_request(p, r));
-  int64_t total;
-  block_scan<THREADS>(sum, s_warp, &total);
-  return total;
+// a / b and a % b; 64-bit division only where it is needed
+__device__ __forceinline__ int64_t attn_div(int64_t a, int64_t b, int64_t* rem) {
+  if (((a | b) >> 32) == 0) {
+    const uint32_t q = (uint32_t)a / (uint32_t)b;
+    *rem = (uint32_t)a - q * (uint32_t)b;
+    return q;
+  }
+  const int64_t q = a / b;
+  *rem = a - q * b;
+  return q;
 }
+// x / group for x < 2^20 (exact: the product's error x * group / 2^32 stays below 1 / group)
+__device__ __forceinline__ int group_div(const AttendParams& p, int x) { return p.group_magic ? (int)__umulhi((uint32_t)x, p.group_magic) : x; }
+
+// The line of all tiles of a call.  Up to 128 requests every warp holds the line by itself, four requests a lane (one round of loads,
+// no barrier); more requests are scanned by the block, a pass per THREADS requests.
+constexpr int kLinePerLane = 4;
+template <int THREADS>
+struct AttnLine {
+  int64_t cost[kLinePerLane], before;  // of this lane's requests, and of all requests before them
+  int64_t total;
+
+  template <typename F>
+  __device__ __forceinline__ void init(int nreq, F cost_of, int64_t* s_warp) {
+    if (nreq <= 32 * kLinePerLane) {
+      const int lane = threadIdx.x & 31;
+      int64_t own = 0;
+#pragma unroll
+      for (int i = 0; i < kLinePerLane; ++i) {
+        const int r = lane * kLinePerLane + i;
+        cost[i] = r < nreq ? cost_of(r) : 0;
+        own += cost[i];
+      }
+      int64_t v = own;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int64_t u = __shfl_up_sync(0xffffffffu, v, o);
+        if (lane >= o) v += u;
+      }
+      before = v - own;
+      total = __shfl_sync(0xffffffffu, v, 31);
+    } else {
+      int64_t sum = 0;
+      for (int r = threadIdx.x; r < nreq; r += THREADS) sum += cost_of(r);
+      block_scan<THREADS>(sum, s_warp, &total);
+    }
+  }
+  // Request that tile `off` belongs to, and the offset of the request's first tile; -1 when off lies behind the line.  All threads
+  // of the block come here with the same off.
+  template <typename F>
+  __device__ __forceinline__ int locate(int nreq, F cost_of, int64_t off, int64_t* s_warp, int64_t* s_found, int64_t* start) const {
+    if (off >= total) return -1;
+    if (nreq <= 32 * kLinePerLane) {
+      int64_t at = before;
+      int found = -1;
+      int64_t found_at = 0;
+#pragma unroll
+      for (int i = 0; i < kLinePerLane; ++i) {
+        if (off >= at && off < at + cost[i]) {
+          found = (int)(threadIdx.x & 31) * kLinePerLane + i;
+          found_at = at;
+        }
+        at += cost[i];
+      }
+      const int src = __ffs(__ballot_sync(0xffffffffu, found >= 0)) - 1;
+      *start = __shfl_sync(0xffffffffu, found_at, src);
+      return __shfl_sync(0xffffffffu, found, src);
+    }
+    int64_t before_pass = 0;
+    for (int r0 = 0; r0 < nreq; r0 += THREADS) {
+      const int r = r0 + threadIdx.x;
+      const int64_t c = r < nreq ? cost_of(r) : 0;
+      int64_t pass;
+      const int64_t end = before_pass + block_scan<THREADS>(c, s_warp, &pass);
+      if (off < before_pass + pass) {  // uniform
+        if (c > 0 && off >= end - c && off < end) {
+          s_found[0] = r;
+          s_found[1] = end - c;
+        }
+        __syncthreads();
+        *start = s_found[1];
+        return (int)s_found[0];
+      }
+      before_pass += pass;
+    }
+    return -1;
+  }
+};
 __device__ __forceinline__ int64_t attn_share(int64_t total, int ctas, int min_share) {
-  const int64_t s = (total + ctas - 1) / ctas;
+  int64_t rem;
+  const int64_t s = attn_div(total + ctas - 1, ctas, &rem);
   return s > min_share ? s : min_share;
 }
 
-// Request that tile `off` of the line belongs to, and the offset of the request's first tile; by the whole block.
-template <int THREADS>
-__device__ __forceinline__ int attn_locate(const AttendParams& p, int64_t off, int64_t* s_warp, int64_t* s_found, int64_t* start) {
-  int64_t before = 0;
-  for (int r0 = 0; r0 < p.nreq; r0 += THREADS) {
-    const int r = r0 + threadIdx.x;
-    const int64_t c = r < p.nreq ? attn_cost(p, attn_request(p, r)) : 0;
-    int64_t total;
-    const int64_t end = before + block_scan<THREADS>(c, s_warp, &total);
-    if (off < before + total) {  // uniform
-      if (c > 0 && off >= end - c && off < end) {
-        s_found[0] = r;
-        s_found[1] = end - c;
-      }
-      __syncthreads();
-      *start = s_found[1];
-      return (int)s_found[0];
-    }
-    before += total;
-  }
-  *start = 0;
-  return -1;  // (off lies behind the line: callers check)
+// block of the table that a key lies in, and its place there
+__device__ __forceinline__ int attn_page(const AttendParams& p, int key) { return p.block_shift >= 0 ? key >> p.block_shift : key / p.block_size; }
+__device__ __forceinline__ int attn_in_page(const AttendParams& p, int key) {
+  return p.block_shift >= 0 ? key & (p.block_size - 1) : key % p.block_size;
 }
 
 __device__ __forceinline__ uint32_t attn_smem(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -145,10 +210,9 @@ __device__ __forceinline__ float ex2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-// two e4m3 codes (low half of `u`) as two fp16: exact
-__device__ __forceinline__ uint32_t e4m3x2_half2(uint32_t u) {
-  const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(u & 0xffffu), __NV_E4M3);
-  return (uint32_t)h.x | ((uint32_t)h.y << 16);
+// four e4m3 codes as four fp16 (exact), two to a word
+__device__ __forceinline__ void e4m3x4_half2(uint32_t u, uint32_t& lo, uint32_t& hi) {
+  asm("{ .reg .b16 a, b; mov.b32 {a, b}, %2; cvt.rn.f16x2.e4m3x2 %0, a; cvt.rn.f16x2.e4m3x2 %1, b; }" : "=r"(lo), "=r"(hi) : "r"(u));
 }
 __device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
   const __half2 h = __floats2half2_rn(lo, hi);
@@ -197,13 +261,16 @@ __global__ void __launch_bounds__(kAttnThreads, AttnCfg<D, FP8>::kCtasPerSm) att
   grid_launch_dependents();
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t4 = lane & 3;
 
-  const int64_t total = attn_total<kAttnThreads>(p, s_warp);
+  auto cost_of = [&](int i) { return attn_cost(p, attn_request(p, i)); };
+  AttnLine<kAttnThreads> line;
+  line.init(p.nreq, cost_of, s_warp);
+  const int64_t total = line.total;
   const int64_t share = attn_share(total, gridDim.x, p.min_share);
   int64_t off = blockIdx.x * share;
   const int64_t off_end = min(total, off + share);
   if (off >= off_end) return;
   int64_t req_start;
-  int r = attn_locate<kAttnThreads>(p, off, s_warp, s_found, &req_start);
+  int r = line.locate(p.nreq, cost_of, off, s_warp, s_found, &req_start);
   if (r < 0) return;
   AttnReq rq = attn_request(p, r);
 
@@ -213,29 +280,70 @@ __global__ void __launch_bounds__(kAttnThreads, AttnCfg<D, FP8>::kCtasPerSm) att
   while (off < off_end) {
     // ---- the unit that tile `off` belongs to
     const int tiles = attn_tiles(rq), n_rt = (rq.rows + kAttnRows - 1) / kAttnRows;
-    const int64_t in_req = off - req_start;
-    const int t0 = (int)(in_req % tiles);
-    const int64_t u = in_req / tiles;  // row tile fastest, so that the row tiles of a K/V head follow one another
-    const int rt = (int)(u % n_rt), kvh = (int)(u / n_rt);
+    int64_t rem;
+    const int64_t u = attn_div(off - req_start, tiles, &rem);  // row tile fastest, so that the row tiles of a K/V head follow one another
+    const int t0 = (int)rem;
+    const int kvh = (int)attn_div(u, n_rt, &rem), rt = (int)rem;
     const int t1 = (int)min((int64_t)tiles, t0 + (off_end - off));
     const bool whole = t0 == 0 && t1 == tiles;
     const int row0 = rt * kAttnRows;
     const int rows = min(kAttnRows, rq.rows - row0);
+    const int tok0 = row0 / p.group, sub0 = row0 - tok0 * p.group;  // new token and query head of the group of row 0
     const int pos0 = rq.len - rq.n;  // position of the request's first new token
-    const int last_pos = pos0 + (row0 + rows - 1) / p.group;
+    const int last_pos = pos0 + tok0 + group_div(p, sub0 + rows - 1);
     const int key_end = min(rq.keys, last_pos + 1);  // keys that any row of the unit may see
     const int n_it = min(t1, (key_end + kAttnTileKeys - 1) / kAttnTileKeys) - t0;  // <= 0: nothing to read
     // last key of this thread's two rows (rows behind the unit's last follow the last one)
-    const int lim0 = pos0 + (row0 + min(g, rows - 1)) / p.group, lim1 = pos0 + (row0 + min(g + 8, rows - 1)) / p.group;
-    const int lim_min = pos0 + row0 / p.group;
+    const int lim0 = pos0 + tok0 + group_div(p, sub0 + min(g, rows - 1)), lim1 = pos0 + tok0 + group_div(p, sub0 + min(g + 8, rows - 1));
+    const int lim_min = pos0 + tok0;
 
+    const int32_t* table = p.tables + (int64_t)r * p.max_blocks;
+    const uint8_t* kh = p.k_cache + kvh * p.head_stride;
+    const uint8_t* vh = p.v_cache + kvh * p.head_stride;
+    // lane's key of iteration i, and its table entry (fetched one iteration before it is needed)
+    auto key_of = [&](int i) { return (t0 + i) * kAttnTileKeys + warp * kAttnWarpKeys + (lane & 15); };
+    auto entry_of = [&](int i) {
+      const int key = key_of(i);
+      return i < n_it && key < key_end ? __ldg(table + attn_page(p, key)) : -1;
+    };
+    auto issue = [&](int i, int32_t blk) {
+      if (i < n_it) {
+        const int key = key_of(i);
+        const bool live = blk >= 0 && blk < p.num_blocks;
+        const int64_t at = live ? blk * p.block_stride + attn_in_page(p, key) * p.token_stride : 0;
+        const uint32_t mask = __ballot_sync(0xffffffffu, live) & 0xffffu;
+        const int st = i % C::kStages;
+        if (lane == 0) s_mask[warp][st] = mask;
+        const uint32_t dst = ring_u + st * C::kStageBytes;
+        constexpr int kPer = kAttnWarpKeys * C::kChunks / 32 > 0 ? kAttnWarpKeys * C::kChunks / 32 : 1;
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) {
+          const int idx = j * 32 + lane, row = (idx / C::kChunks) & 15, ch = idx % C::kChunks;
+          const int64_t ro = __shfl_sync(0xffffffffu, at, row);
+          const bool ok = (mask >> row) & 1u;
+          if (kAttnWarpKeys * C::kChunks >= 32 || idx < kAttnWarpKeys * C::kChunks) {
+            cp_async16(dst + attn_swz<C::kChunks, FP8, false>(row, ch), kh + ro + ch * 16, ok);
+            cp_async16(dst + C::kTileBytes + attn_swz<C::kChunks, FP8, true>(row, ch), vh + ro + ch * 16, ok);
+          }
+        }
+      }
+      cp_async_commit();
+    };
+
+    int32_t nxt = entry_of(0);
+#pragma unroll 1
+    for (int i = 0; i < C::kStages - 1; ++i) {
+      const int32_t blk = nxt;
+      nxt = entry_of(i + 1);
+      issue(i, blk);
+    }
     // ---- queries: A fragments of the 16 rows, zero behind the last
     uint32_t qf[kSteps][4];
     float sc0 = p.scale_log2, sc1 = p.scale_log2;
     {
-      const int ra = row0 + g, rb = row0 + g + 8;
-      const __nv_bfloat16* qa = p.q + (int64_t)(rq.q0 + ra / p.group) * p.q_ts + (int64_t)(kvh * p.group + ra % p.group) * p.q_hs;
-      const __nv_bfloat16* qb = p.q + (int64_t)(rq.q0 + rb / p.group) * p.q_ts + (int64_t)(kvh * p.group + rb % p.group) * p.q_hs;
+      const int ta = group_div(p, sub0 + g), tb = group_div(p, sub0 + g + 8);
+      const __nv_bfloat16* qa = p.q + (int64_t)(rq.q0 + tok0 + ta) * p.q_ts + (int64_t)(kvh * p.group + sub0 + g - ta * p.group) * p.q_hs;
+      const __nv_bfloat16* qb = p.q + (int64_t)(rq.q0 + tok0 + tb) * p.q_ts + (int64_t)(kvh * p.group + sub0 + g + 8 - tb * p.group) * p.q_hs;
       const bool la = g < rows, lb = g + 8 < rows;
 #pragma unroll
       for (int k = 0; k < kSteps; ++k) {
@@ -280,46 +388,6 @@ __global__ void __launch_bounds__(kAttnThreads, AttnCfg<D, FP8>::kCtasPerSm) att
     for (int n = 0; n < kNT; ++n) o[n][0] = o[n][1] = o[n][2] = o[n][3] = 0.f;
     float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;
 
-    const int32_t* table = p.tables + (int64_t)r * p.max_blocks;
-    const uint8_t* kh = p.k_cache + kvh * p.head_stride;
-    const uint8_t* vh = p.v_cache + kvh * p.head_stride;
-    // lane's key of iteration i, and its table entry (fetched one iteration before it is needed)
-    auto key_of = [&](int i) { return (t0 + i) * kAttnTileKeys + warp * kAttnWarpKeys + (lane & 15); };
-    auto entry_of = [&](int i) {
-      const int key = key_of(i);
-      return i < n_it && key < key_end ? __ldg(table + key / p.block_size) : -1;
-    };
-    auto issue = [&](int i, int32_t blk) {
-      if (i < n_it) {
-        const int key = key_of(i);
-        const bool live = blk >= 0 && blk < p.num_blocks;
-        const int64_t at = live ? blk * p.block_stride + (key % p.block_size) * p.token_stride : 0;
-        const uint32_t mask = __ballot_sync(0xffffffffu, live) & 0xffffu;
-        const int st = i % C::kStages;
-        if (lane == 0) s_mask[warp][st] = mask;
-        const uint32_t dst = ring_u + st * C::kStageBytes;
-        constexpr int kPer = kAttnWarpKeys * C::kChunks / 32 > 0 ? kAttnWarpKeys * C::kChunks / 32 : 1;
-#pragma unroll
-        for (int j = 0; j < kPer; ++j) {
-          const int idx = j * 32 + lane, row = (idx / C::kChunks) & 15, ch = idx % C::kChunks;
-          const int64_t ro = __shfl_sync(0xffffffffu, at, row);
-          const bool ok = (mask >> row) & 1u;
-          if (kAttnWarpKeys * C::kChunks >= 32 || idx < kAttnWarpKeys * C::kChunks) {
-            cp_async16(dst + attn_swz<C::kChunks, FP8, false>(row, ch), kh + ro + ch * 16, ok);
-            cp_async16(dst + C::kTileBytes + attn_swz<C::kChunks, FP8, true>(row, ch), vh + ro + ch * 16, ok);
-          }
-        }
-      }
-      cp_async_commit();
-    };
-
-    int32_t nxt = entry_of(0);
-#pragma unroll 1
-    for (int i = 0; i < C::kStages - 1; ++i) {
-      const int32_t blk = nxt;
-      nxt = entry_of(i + 1);
-      issue(i, blk);
-    }
 #pragma unroll 1
     for (int i = 0; i < n_it; ++i) {
       cp_async_wait<C::kStages - 2>();
@@ -366,7 +434,11 @@ __global__ void __launch_bounds__(kAttnThreads, AttnCfg<D, FP8>::kCtasPerSm) att
               w[0] = *reinterpret_cast<const uint32_t*>(src);
             }
 #pragma unroll
-            for (int q = 0; q < C::kSPB; ++q) mma16816<true>(s[nt], qf[kb * C::kSPB + q], e4m3x2_half2(w[q]), e4m3x2_half2(w[q] >> 16));
+            for (int q = 0; q < C::kSPB; ++q) {
+              uint32_t b0, b1;
+              e4m3x4_half2(w[q], b0, b1);
+              mma16816<true>(s[nt], qf[kb * C::kSPB + q], b0, b1);
+            }
           }
         }
       }
@@ -456,7 +528,8 @@ __global__ void __launch_bounds__(kAttnThreads, AttnCfg<D, FP8>::kCtasPerSm) att
               const int d = (n / kVB) * (8 * kVB) + 2 * t4 * kVB + n % kVB;
               const uint32_t x0b = vp[attn_swz<C::kChunks, true, true>(c, d >> 4) + (d & 15)];
               const uint32_t x1b = vp[attn_swz<C::kChunks, true, true>(c, (d + kVB) >> 4) + ((d + kVB) & 15)];
-              const uint32_t h = e4m3x2_half2(x0b | (x1b << 8));
+              uint32_t h, unused;
+              e4m3x4_half2(x0b | (x1b << 8), h, unused);
               const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
               v0 = f.x, v1 = f.y;
             }
@@ -497,8 +570,11 @@ __global__ void __launch_bounds__(kAttnThreads, AttnCfg<D, FP8>::kCtasPerSm) att
 #pragma unroll
           for (int h = 0; h < kVB / 2; ++h) {  // bytes 2h, 2h + 1 of the rows, paired by key
             const uint32_t lo = __byte_perm(x[0], x[1], h ? 0x7362 : 0x5140), hi = __byte_perm(x[2], x[3], h ? 0x7362 : 0x5140);
-            mma16816<true>(o[jj * kVB + 2 * h], pa, e4m3x2_half2(lo), e4m3x2_half2(hi));
-            mma16816<true>(o[jj * kVB + 2 * h + 1], pa, e4m3x2_half2(lo >> 16), e4m3x2_half2(hi >> 16));
+            uint32_t l0h, l1h, h0h, h1h;
+            e4m3x4_half2(lo, l0h, l1h);
+            e4m3x4_half2(hi, h0h, h1h);
+            mma16816<true>(o[jj * kVB + 2 * h], pa, l0h, h0h);
+            mma16816<true>(o[jj * kVB + 2 * h + 1], pa, l1h, h1h);
           }
         }
       }
@@ -554,7 +630,7 @@ __global__ void __launch_bounds__(kAttnThreads, AttnCfg<D, FP8>::kCtasPerSm) att
         y1 = fmaf(f, x.y, y1);
       }
       if (whole) {
-        const int R = row0 + row, tok = rq.q0 + R / p.group, head = kvh * p.group + R % p.group;
+        const int dt = group_div(p, sub0 + row), tok = rq.q0 + tok0 + dt, head = kvh * p.group + sub0 + row - dt * p.group;
         const float inv = l == 0.f ? 0.f : p.v_scale / l;
         *reinterpret_cast<uint32_t*>(p.out + tok * p.o_ts + head * p.o_hs + d) = pack_bf16(y0 * inv, y1 * inv);
         if (p.lse && d == 0) p.lse[(int64_t)tok * p.n_q + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
@@ -581,42 +657,79 @@ __global__ void __launch_bounds__(kAttnThreads, AttnCfg<D, FP8>::kCtasPerSm) att
 // Joins the parts of a unit that CTA borders cut: block b looks at the border in front of CTA b's share and joins the unit there when
 // that border is the unit's first.
 constexpr int kCombineThreads = 128;
+constexpr int kJoinBatch = 8;
+// Four elements of a row, summed over parts.
+struct JoinSum {
+  float m = -INFINITY, l = 0.f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  __device__ __forceinline__ void add(const float2* ml, const float4* x, int n) {  // the first min(n, kJoinBatch) parts
+    float top = m;
+#pragma unroll
+    for (int i = 0; i < kJoinBatch; ++i)
+      if (i < n) top = fmaxf(top, ml[i].x);
+    const float f = m == -INFINITY ? 1.f : ex2(m - top);  // (sums without a maximum: zeros, or NaN that has to stay)
+    l *= f;
+    o = make_float4(o.x * f, o.y * f, o.z * f, o.w * f);
+#pragma unroll
+    for (int i = 0; i < kJoinBatch; ++i)
+      if (i < n) {
+        const float w = ml[i].x == -INFINITY ? 1.f : ex2(ml[i].x - top);
+        l = fmaf(ml[i].y, w, l);
+        o = make_float4(fmaf(x[i].x, w, o.x), fmaf(x[i].y, w, o.y), fmaf(x[i].z, w, o.z), fmaf(x[i].w, w, o.w));
+      }
+    m = top;
+  }
+  __device__ __forceinline__ void write(const AttendParams& p, int tok, int head, int d) const {
+    const float inv = l == 0.f ? 0.f : p.v_scale / l;
+    *reinterpret_cast<uint2*>(p.out + tok * p.o_ts + head * p.o_hs + d) = make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
+    if (p.lse && d == 0) p.lse[(int64_t)tok * p.n_q + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+  }
+};
 template <int D>
 __device__ __forceinline__ void rows_join(const AttendParams& p, int b, int ctas, int64_t* s_warp, int64_t* s_found) {
   const int tid = threadIdx.x;
-  const int64_t total = attn_total<kCombineThreads>(p, s_warp);
-  const int64_t share = attn_share(total, ctas, p.min_share);
+  auto cost_of = [&](int i) { return attn_cost(p, attn_request(p, i)); };
+  AttnLine<kCombineThreads> line;
+  line.init(p.nreq, cost_of, s_warp);
+  const int64_t share = attn_share(line.total, ctas, p.min_share);
   const int64_t off = b * share;
-  int64_t req_start = 0;
-  const int r = off < total ? attn_locate<kCombineThreads>(p, off, s_warp, s_found, &req_start) : -1;
-  grid_dependency_wait();
-  if (r < 0) return;
-  const AttnReq rq = attn_request(p, r);
-  const int tiles = attn_tiles(rq), n_rt = (rq.rows + kAttnRows - 1) / kAttnRows;
-  const int t0 = (int)((off - req_start) % tiles);
-  if (t0 == 0 || share < t0) return;  // no unit is cut here, or an earlier border is the unit's first
-  const int64_t u = (off - req_start) / tiles;
-  const int rt = (int)(u % n_rt), kvh = (int)(u / n_rt);
-  const int c_last = (int)((off - t0 + tiles - 1) / share);
-  const int row0 = rt * kAttnRows, rows = min(kAttnRows, rq.rows - row0);
-  for (int e = tid; e < rows * (D / 2); e += kCombineThreads) {
-    const int row = e / (D / 2), d = 2 * (e % (D / 2));
-    float m = -INFINITY, l = 0.f, y0 = 0.f, y1 = 0.f;
-    for (int c = b - 1; c <= c_last; ++c) {
-      const int64_t at = ((int64_t)c * 2 + (c == b - 1 ? 1 : 0)) * kAttnRows + row;
-      const float2 ml = p.part_ml[at];
-      const float2 x = *reinterpret_cast<const float2*>(p.part_o + at * D + d);
-      const float n = fmaxf(m, ml.x);
-      const float fa = m == -INFINITY ? 1.f : ex2(m - n), fb = ml.x == -INFINITY ? 1.f : ex2(ml.x - n);
-      l = l * fa + ml.y * fb;
-      y0 = y0 * fa + x.x * fb;
-      y1 = y1 * fa + x.y * fb;
-      m = n;
+  int64_t req_start = 0, rem;
+  const int r = line.locate(p.nreq, cost_of, off, s_warp, s_found, &req_start);
+  // (all that does not depend on the parts comes before the wait for them)
+  int rows = 0, c_last = 0, tok0 = 0, sub0 = 0, head0 = 0;
+  if (r >= 0) {
+    const AttnReq rq = attn_request(p, r);
+    const int tiles = attn_tiles(rq), n_rt = (rq.rows + kAttnRows - 1) / kAttnRows;
+    const int64_t u = attn_div(off - req_start, tiles, &rem);
+    const int t0 = (int)rem;
+    if (t0 != 0 && share >= t0) {  // else no unit is cut here, or an earlier border is the unit's first
+      const int kvh = (int)attn_div(u, n_rt, &rem), row0 = (int)rem * kAttnRows;
+      c_last = (int)attn_div(off - t0 + tiles - 1, share, &rem);
+      rows = min(kAttnRows, rq.rows - row0);
+      tok0 = row0 / p.group;
+      sub0 = row0 - tok0 * p.group;
+      tok0 += rq.q0;
+      head0 = kvh * p.group;
     }
-    const int R = row0 + row, tok = rq.q0 + R / p.group, head = kvh * p.group + R % p.group;
-    const float inv = l == 0.f ? 0.f : p.v_scale / l;
-    *reinterpret_cast<uint32_t*>(p.out + tok * p.o_ts + head * p.o_hs + d) = pack_bf16(y0 * inv, y1 * inv);
-    if (p.lse && d == 0) p.lse[(int64_t)tok * p.n_q + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+  }
+  grid_dependency_wait();
+  for (int e = tid; e < rows * (D / 4); e += kCombineThreads) {
+    const int row = e / (D / 4), d = 4 * (e % (D / 4));
+    JoinSum sum;
+    for (int c0 = b - 1; c0 <= c_last; c0 += kJoinBatch) {
+      float2 ml[kJoinBatch];
+      float4 x[kJoinBatch];
+#pragma unroll
+      for (int i = 0; i < kJoinBatch; ++i) {  // (the loads of several parts fly together)
+        const int c = min(c0 + i, c_last);
+        const int64_t at = ((int64_t)c * 2 + (c == b - 1 ? 1 : 0)) * kAttnRows + row;
+        ml[i] = p.part_ml[at];
+        x[i] = *reinterpret_cast<const float4*>(p.part_o + at * D + d);
+      }
+      sum.add(ml, x, c_last - c0 + 1);
+    }
+    const int dt = group_div(p, sub0 + row);
+    sum.write(p, tok0 + dt, head0 + sub0 + row - dt * p.group, d);
   }
 }
 

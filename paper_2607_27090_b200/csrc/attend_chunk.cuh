@@ -75,15 +75,6 @@ __device__ __forceinline__ int64_t chunk_cost(const ChunkParams& c, const AttnRe
   return chunk_head_tiles(c.a, q) * c.a.n_kv;
 }
 
-template <int THREADS>
-__device__ __forceinline__ int64_t chunk_total(const ChunkParams& c, int64_t* s_warp) {
-  int64_t sum = 0;
-  for (int r = threadIdx.x; r < c.a.nreq; r += THREADS) sum += chunk_cost(c, attn_request(c.a, r));
-  int64_t total;
-  block_scan<THREADS>(sum, s_warp, &total);
-  return total;
-}
-
 // A piece of a unit that one CTA works on: tiles t0 .. t1 - 1 of it.
 struct ChunkSeg {
   int r, kvh, rt, t0, t1, tiles;
@@ -92,37 +83,22 @@ struct ChunkSeg {
 
 // The unit that tile `off` of the line lies in, by the whole block; false when off lies behind the line.
 template <int THREADS>
-__device__ __forceinline__ bool chunk_locate(const ChunkParams& c, int64_t off, int64_t* s_warp, int64_t* s_found, ChunkSeg* seg) {
-  int64_t before = 0;
-  for (int r0 = 0; r0 < c.a.nreq; r0 += THREADS) {
-    const int r = r0 + threadIdx.x;
-    const int64_t cost = r < c.a.nreq ? chunk_cost(c, attn_request(c.a, r)) : 0;
-    int64_t total;
-    const int64_t end = before + block_scan<THREADS>(cost, s_warp, &total);
-    if (off < before + total) {  // uniform
-      if (cost > 0 && off >= end - cost && off < end) {
-        s_found[0] = r;
-        s_found[1] = off - (end - cost);
-      }
-      __syncthreads();
-      seg->r = (int)s_found[0];
-      seg->q = attn_request(c.a, seg->r);
-      const int64_t per_head = chunk_head_tiles(c.a, seg->q);
-      seg->kvh = (int)(s_found[1] / per_head);
-      int64_t rem = s_found[1] % per_head;
-      seg->rt = 0;
-      for (;;) {
-        seg->tiles = chunk_tiles(c.a, seg->q, seg->rt);
-        if (rem < seg->tiles) break;
-        rem -= seg->tiles;
-        ++seg->rt;
-      }
-      seg->t0 = (int)rem;
-      return true;
-    }
-    before += total;
+__device__ __forceinline__ bool chunk_locate(const ChunkParams& c, const AttnLine<THREADS>& line, int64_t off, int64_t* s_warp, int64_t* s_found,
+                                             ChunkSeg* seg) {
+  int64_t start, rem;
+  seg->r = line.locate(c.a.nreq, [&](int i) { return chunk_cost(c, attn_request(c.a, i)); }, off, s_warp, s_found, &start);
+  if (seg->r < 0) return false;
+  seg->q = attn_request(c.a, seg->r);
+  seg->kvh = (int)attn_div(off - start, chunk_head_tiles(c.a, seg->q), &rem);
+  seg->rt = 0;
+  for (;;) {
+    seg->tiles = chunk_tiles(c.a, seg->q, seg->rt);
+    if (rem < seg->tiles) break;
+    rem -= seg->tiles;
+    ++seg->rt;
   }
-  return false;
+  seg->t0 = (int)rem;
+  return true;
 }
 // The unit after seg (t0 = 0); false behind the last request.
 __device__ __forceinline__ bool chunk_next(const ChunkParams& c, ChunkSeg* seg) {
@@ -330,12 +306,14 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
   const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_slot, 0);
   const uint32_t limit = c.spin_limit ? c.spin_limit : kChunkSpinLimit;
 
-  const int64_t total = chunk_total<kChunkThreads>(c, s_warp);
+  AttnLine<kChunkThreads> line;
+  line.init(p.nreq, [&](int i) { return chunk_cost(c, attn_request(p, i)); }, s_warp);
+  const int64_t total = line.total;
   const int64_t share = attn_share(total, gridDim.x, c.min_share);
   int64_t off = blockIdx.x * share;
   const int64_t off_end = min(total, off + share);
   ChunkSeg seg;
-  bool more = off < off_end && chunk_locate<kChunkThreads>(c, off, s_warp, s_found, &seg);
+  bool more = off < off_end && chunk_locate<kChunkThreads>(c, line, off, s_warp, s_found, &seg);
   // every role walks the same segments
   auto set_end = [&] { seg.t1 = (int)min((int64_t)seg.tiles, seg.t0 + (off_end - off)); };
   auto next = [&] {
@@ -372,23 +350,24 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
       const AttnReq& q = seg.q;
       const int row0 = seg.rt * kChunkRows, rows = min(kChunkRows, q.rows - row0);
       const int pos0 = q.len - q.n;
-      const int key_end = min(q.keys, pos0 + (row0 + rows - 1) / p.group + 1), lim_min = pos0 + row0 / p.group;
+      const int tok0 = row0 / p.group, sub0 = row0 - tok0 * p.group;  // new token and query head of the group of row 0
+      const int lim_min = pos0 + tok0, key_end = min(q.keys, lim_min + group_div(p, sub0 + rows - 1) + 1);
       // ---- queries, once the products of the unit before have read theirs: a warp takes 64 rows, 16 bytes a lane
       auto load_queries = [&] {
         ok = chunk_wait(q_empty, q_ph, abort_flag, limit);
         q_ph ^= 1u;
         if (!ok) return;
-        constexpr int kLanes = D / 8, kPerWarp = 32 / kLanes, kBatch = 4;  // lanes of a row, rows of a load, loads in flight
+        constexpr int kLanes = D / 8, kPerWarp = 32 / kLanes, kBatch = 8;  // lanes of a row, rows of a load, loads in flight
         const int ql = lane % kLanes;
 #pragma unroll 1
         for (int i0 = 0; i0 < kChunkRows / 4 / kPerWarp; i0 += kBatch) {
           uint4 x[kBatch];
 #pragma unroll
           for (int i = 0; i < kBatch; ++i) {
-            const int row = w * (kChunkRows / 4) + (i0 + i) * kPerWarp + lane / kLanes, R = row0 + row;
+            const int row = w * (kChunkRows / 4) + (i0 + i) * kPerWarp + lane / kLanes, dt = group_div(p, sub0 + row);
             x[i] = make_uint4(0u, 0u, 0u, 0u);
             if (row < rows)
-              x[i] = *reinterpret_cast<const uint4*>(p.q + (int64_t)(q.q0 + R / p.group) * p.q_ts + (int64_t)(seg.kvh * p.group + R % p.group) * p.q_hs + ql * 8);
+              x[i] = *reinterpret_cast<const uint4*>(p.q + (int64_t)(q.q0 + tok0 + dt) * p.q_ts + (int64_t)(seg.kvh * p.group + sub0 + row - dt * p.group) * p.q_hs + ql * 8);
           }
 #pragma unroll
           for (int i = 0; i < kBatch; ++i) {
@@ -417,7 +396,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
       const int32_t* table = p.tables + (int64_t)seg.r * p.max_blocks;
       auto entry_of = [&](int t) {
         const int key = t * kChunkKeys + lt;
-        return key < key_end ? __ldg(table + key / p.block_size) : -1;
+        return key < key_end ? __ldg(table + attn_page(p, key)) : -1;
       };
       int32_t nxt = entry_of(seg.t0);
       for (int t = seg.t0; ok && t < seg.t1; ++t) {
@@ -425,7 +404,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
         if (t + 1 < seg.t1) nxt = entry_of(t + 1);
         const int key = t * kChunkKeys + lt;
         const bool live = blk >= 0 && blk < p.num_blocks;
-        const int64_t at = live ? blk * p.block_stride + (key % p.block_size) * p.token_stride + seg.kvh * p.head_stride : 0;
+        const int64_t at = live ? blk * p.block_stride + attn_in_page(p, key) * p.token_stride + seg.kvh * p.head_stride : 0;
         const uint32_t mask = __ballot_sync(0xffffffffu, live);
         const bool causal = t * kChunkKeys + kChunkKeys - 1 > lim_min;
         if (lane == 0) s_masks[mask_at * 4 + w] = mask;
@@ -467,8 +446,10 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
                 }
               }
               uint4 lo, hi;
-              lo = make_uint4(e4m3x2_half2(y[0]), e4m3x2_half2(y[0] >> 16), e4m3x2_half2(y[1]), e4m3x2_half2(y[1] >> 16));
-              hi = make_uint4(e4m3x2_half2(y[2]), e4m3x2_half2(y[2] >> 16), e4m3x2_half2(y[3]), e4m3x2_half2(y[3] >> 16));
+              e4m3x4_half2(y[0], lo.x, lo.y);
+              e4m3x4_half2(y[1], lo.z, lo.w);
+              e4m3x4_half2(y[2], hi.x, hi.y);
+              e4m3x4_half2(y[3], hi.z, hi.w);
               uint8_t* d = dst + (ch >> 2) * 16384;
               *reinterpret_cast<uint4*>(d + chunk_swz(row, 2 * (ch & 3))) = lo;
               *reinterpret_cast<uint4*>(d + chunk_swz(row, 2 * (ch & 3) + 1)) = hi;
@@ -629,8 +610,9 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
         mask_at = (mask_at + nt) % kChunkMaskRing;
         continue;
       }
-      const int pos0 = q.len - q.n;
-      const int lim = pos0 + (row0 + min(row, rows - 1)) / p.group, lim_min = pos0 + row0 / p.group;
+      const int tok0 = row0 / p.group, sub0 = row0 - tok0 * p.group;
+      const int dt = group_div(p, sub0 + min(row, rows - 1));
+      const int lim_min = q.len - q.n + tok0, lim = lim_min + dt;
       float m = -INFINITY, l = 0.f, sc = p.scale_log2;
       bool any_bad = false;
       int v_at = 0;
@@ -684,10 +666,9 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
           else
             form(mm, ChunkNo{});
         };
-        if (ok) form_any(m);
-        // (always in a segment's first tile, rarely later; also the point from which both warps have read their scores, over which
-        // the weights are stored)
-        const bool renew = sum > kChunkMaxSum || m == -INFINITY;
+        if (ok && j > 0) form_any(m);
+        // (also the point from which both warps have read their scores, over which the weights are stored)
+        const bool renew = sum > kChunkMaxSum || m == -INFINITY;  // (always in a segment's first tile, rarely later)
         if (pair_any(pair, !ok || renew)) {
           if (pair_any(pair, !ok)) {  // a wait ran out: both warps leave together, neither is left at a barrier
             ok = false;
@@ -745,7 +726,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
       if (nt > 0) l = pair_join(l, [](float a, float b) { return a + b; });
       const bool whole = seg.t0 == 0 && seg.t1 == seg.tiles;
       const bool mine = row < rows;
-      const int R = row0 + min(row, rows - 1), tok = q.q0 + R / p.group, head = seg.kvh * p.group + R % p.group;
+      const int tok = q.q0 + tok0 + dt, head = seg.kvh * p.group + sub0 + min(row, rows - 1) - dt * p.group;
       const float inv = l == 0.f ? 0.f : p.v_scale / l;
       const int64_t slot = (int64_t)blockIdx.x * 2 + (seg.t0 == 0 ? 1 : 0);
       if (mine && part == 0) {
@@ -823,34 +804,34 @@ constexpr int kChunkJoinRows = 16;
 template <int D>
 __device__ __forceinline__ void chunk_join(const ChunkParams& c, int b, int y, int ctas, int64_t* s_warp, int64_t* s_found) {
   const AttendParams& p = c.a;
-  const int64_t total = chunk_total<kCombineThreads>(c, s_warp);
-  const int64_t share = attn_share(total, ctas, c.min_share);
+  AttnLine<kCombineThreads> line;
+  line.init(p.nreq, [&](int i) { return chunk_cost(c, attn_request(p, i)); }, s_warp);
+  const int64_t share = attn_share(line.total, ctas, c.min_share);
   const int64_t off = b * share;
   ChunkSeg seg;
-  const bool found = off < total && chunk_locate<kCombineThreads>(c, off, s_warp, s_found, &seg);
-  grid_dependency_wait();
-  if (!found || seg.t0 == 0 || share < seg.t0) return;  // no unit is cut here, or an earlier border is the unit's first
-  const int c_last = (int)((off - seg.t0 + seg.tiles - 1) / share);
-  const int row0 = seg.rt * kChunkRows, rows = min(kChunkRows, seg.q.rows - row0);
+  const bool found = chunk_locate<kCombineThreads>(c, line, off, s_warp, s_found, &seg) && seg.t0 != 0 && share >= seg.t0;
+  // (else no unit is cut here, or an earlier border is the unit's first)
+  int64_t rem;
+  const int c_last = found ? (int)attn_div(off - seg.t0 + seg.tiles - 1, share, &rem) : 0;
   const int row = y * kChunkJoinRows + threadIdx.x % kChunkJoinRows;
-  if (row >= rows) return;
-  const int R = row0 + row, tok = seg.q.q0 + R / p.group, head = seg.kvh * p.group + R % p.group;
+  grid_dependency_wait();
+  if (!found || row >= min(kChunkRows, seg.q.rows - seg.rt * kChunkRows)) return;
+  const int R = seg.rt * kChunkRows + row, tok = seg.q.q0 + R / p.group, head = seg.kvh * p.group + R % p.group;
   for (int d4 = threadIdx.x / kChunkJoinRows; d4 < D / 4; d4 += kCombineThreads / kChunkJoinRows) {
-    float m = -INFINITY, l = 0.f;
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int i = b - 1; i <= c_last; ++i) {
-      const int64_t slot = (int64_t)i * 2 + (i == b - 1 ? 1 : 0);
-      const float2 ml = c.part_ml[slot * kChunkRows + row];
-      const float4 x = *reinterpret_cast<const float4*>(c.part_o + ((slot * (D / 4) + d4) * kChunkRows + row) * 4);
-      const float n = fmaxf(m, ml.x);
-      const float fa = m == -INFINITY ? 1.f : ex2(m - n), fb = ml.x == -INFINITY ? 1.f : ex2(ml.x - n);
-      l = l * fa + ml.y * fb;
-      o = make_float4(o.x * fa + x.x * fb, o.y * fa + x.y * fb, o.z * fa + x.z * fb, o.w * fa + x.w * fb);
-      m = n;
+    JoinSum sum;
+    for (int i0 = b - 1; i0 <= c_last; i0 += kJoinBatch) {
+      float2 ml[kJoinBatch];
+      float4 x[kJoinBatch];
+#pragma unroll
+      for (int k = 0; k < kJoinBatch; ++k) {
+        const int i = min(i0 + k, c_last);
+        const int64_t slot = (int64_t)i * 2 + (i == b - 1 ? 1 : 0);
+        ml[k] = c.part_ml[slot * kChunkRows + row];
+        x[k] = *reinterpret_cast<const float4*>(c.part_o + ((slot * (D / 4) + d4) * kChunkRows + row) * 4);
+      }
+      sum.add(ml, x, c_last - i0 + 1);
     }
-    const float inv = l == 0.f ? 0.f : p.v_scale / l;
-    *reinterpret_cast<uint2*>(p.out + tok * p.o_ts + head * p.o_hs + d4 * 4) = make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
-    if (p.lse && d4 == 0) p.lse[(int64_t)tok * p.n_q + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+    sum.write(p, tok, head, d4 * 4);
   }
 }
 

@@ -186,7 +186,7 @@ ms_status memstore_append(memstore_t* s, int32_t layer, const ms_heads* q, int32
 // Requests with more rows (new tokens x query heads per K/V head) than this go to the tensor-core kernel, when head_dim allows it.
 constexpr int kChunkMinRows = kAttnRows;
 
-// The workspace: unfinished rows of the rows kernel (two CTAs per SM at most) and their statistics, then those of the chunk kernel
+// The workspace: unfinished rows of the rows kernel (kAttnMaxCtasPerSm CTAs per SM at most) and their statistics, then those of the chunk kernel
 // (one CTA per SM) and its error words.  It depends on the GPU and head_dim alone.
 struct AttendLayout {
   size_t rows_o, rows_ml, chunk_o, chunk_ml, errors, bytes;
@@ -201,8 +201,8 @@ static AttendLayout attend_layout(const memstore* s) {
     at += (bytes + 255) & ~(size_t)255;
     return here;
   };
-  w.rows_o = take(sms * 2 * 2 * kAttnRows * d * 4);
-  w.rows_ml = take(sms * 2 * 2 * kAttnRows * 8);
+  w.rows_o = take(sms * kAttnMaxCtasPerSm * 2 * kAttnRows * d * 4);
+  w.rows_ml = take(sms * kAttnMaxCtasPerSm * 2 * kAttnRows * 8);
   if (attend_has_chunks(s->cfg.head_dim)) {
     w.chunk_o = take(sms * 2 * kChunkRows * d * 4);
     w.chunk_ml = take(sms * 2 * kChunkRows * 8);
@@ -276,6 +276,7 @@ ms_status memstore_attend(memstore_t* s, int32_t layer, const ms_heads* q, int32
   if (n_q_heads <= 0 || n_q_heads % c.n_kv_heads)
     return fail(s, MS_ERR_INVALID_ARG, "%d query heads for %d K/V heads", n_q_heads, c.n_kv_heads);
   const int32_t group = n_q_heads / c.n_kv_heads;
+  if (group > kAttnMaxGroup) return fail(s, MS_ERR_UNSUPPORTED, "%d query heads per K/V head (at most %d)", group, kAttnMaxGroup);
   if ((int64_t)n_tokens * group > 0x7fffffff - 256) return fail(s, MS_ERR_UNSUPPORTED, "%d tokens of %d heads", n_tokens, n_q_heads);
   if (!(scale >= 0.f) || !std::isfinite(scale)) return fail(s, MS_ERR_INVALID_ARG, "scale must be positive and finite, or 0 for the default");
   ms_status rc = check_cache(s, cache, layer, true);
@@ -300,6 +301,7 @@ ms_status memstore_attend(memstore_t* s, int32_t layer, const ms_heads* q, int32
   p.n_q = n_q_heads;
   p.n_kv = c.n_kv_heads;
   p.group = group;
+  p.group_magic = group == 1 ? 0u : (uint32_t)((1ull << 32) / (uint32_t)group + 1);
   p.n_tokens = n_tokens;
   p.q_start = q_start;
   p.seq_lens = seq_lens;
@@ -313,6 +315,7 @@ ms_status memstore_attend(memstore_t* s, int32_t layer, const ms_heads* q, int32
   p.head_stride = cache->head_stride * esz;
   p.num_blocks = cache->num_blocks;
   p.block_size = cache->block_size;
+  p.block_shift = (p.block_size & (p.block_size - 1)) ? -1 : __builtin_ctz((unsigned)p.block_size);
   const double sc = scale > 0.f ? (double)scale : 1.0 / std::sqrt((double)c.head_dim);
   p.scale_log2 = (float)(sc * 1.4426950408889634 * (fp8 ? (double)cache->k_scale : 1.0));
   p.v_scale = fp8 ? cache->v_scale : 1.f;
@@ -323,7 +326,7 @@ ms_status memstore_attend(memstore_t* s, int32_t layer, const ms_heads* q, int32
   char* base = (char*)workspace;
   p.part_o = (float*)(base + w.rows_o);
   p.part_ml = (float2*)(base + w.rows_ml);
-  cp.min_share = 2;
+  cp.min_share = 1;
   cp.part_o = (float*)(base + w.chunk_o);
   cp.part_ml = (float2*)(base + w.chunk_ml);
   cp.errors = (int32_t*)(base + w.errors);

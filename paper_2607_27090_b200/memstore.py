@@ -313,7 +313,7 @@ class MemStore:
                       kv_arena.numel() * kv_arena.element_size() if kv_arena is not None else 0, max_host_kv_tokens,
                       rotary_dim, 0)  # fmt: skip
         self.n_layers, self.n_kv_heads, self.head_dim, self.emb_dim = n_layers, n_kv_heads, head_dim, emb_dim
-        self._index, self._workspace_bytes = self.device.index, None
+        self._index, self._workspace_bytes, self._workspaces = self.device.index, None, {}
         rc = self._lib.memstore_create(C.byref(cfg), C.byref(self._h))
         if rc != MS_OK:
             self._h = C.c_void_p()
@@ -659,28 +659,47 @@ class MemStore:
             self._workspace_bytes = int(self._lib.memstore_attend_workspace(self._h))
         return self._workspace_bytes
 
+    def _workspace(self, raw: int, stream) -> torch.Tensor:
+        """Workspace of an attend call: calls on one stream follow one another and share one; a capture gets its own from the
+        graph's pool (its replays may run beside anything), and so does a stream given by the caller."""
+        if stream is not None or torch._C._cuda_isCurrentStreamCapturing():
+            return self._empty(stream, (self.attend_workspace_bytes(), torch.uint8))[0]
+        w = self._workspaces.get(raw)
+        if w is None:
+            w = self._workspaces[raw] = self._empty(None, (self.attend_workspace_bytes(), torch.uint8))[0]
+        return w
+
     def attend(self, layer: int, q, cache: PagedCache, q_start, seq_lens, block_tables, scale: float = 0.0, max_q_len: int = 0, out=None,
                want_lse: bool = False, out_lse=None, out_status=None, workspace=None, stream=None):  # fmt: skip
         """Attention of the new tokens ``q`` [T, n_q_heads, d] (rows ``q_start[r] .. q_start[r+1] - 1`` are the last tokens
         of request r's ``seq_lens[r]`` cached ones) over ``layer`` of the cache.  Returns (out, lse or None, out_status).
-        ``workspace``: a uint8 tensor of ``attend_workspace_bytes()``; by default one comes from torch's allocator for
-        every call, so calls on different streams or in different CUDA graphs have their own."""
+        ``workspace``: a uint8 tensor of ``attend_workspace_bytes()``; by default the store keeps one per current stream, and
+        captures and calls with ``stream`` get one of their own."""
         (T, n_q, _), nreq, i32, ptr = q.shape, seq_lens.shape[0], torch.int32, self._ptr
         if block_tables.dim() != 2 or block_tables.shape[0] != nreq:
             raise ValueError(f"block_tables must have shape ({nreq}, max_blocks), got {tuple(block_tables.shape)}")
         hq = self._heads(q, T, n_q, "q")
-        if out is None:
-            (out,) = self._empty(stream, ((T, n_q, self.head_dim), torch.bfloat16))
+        if out is q:
+            ho = hq
+        elif out is not None:
+            ho = self._heads(out, T, n_q, "out")
+        else:
+            if stream is None:
+                out = torch.empty_like(q, memory_format=torch.contiguous_format)
+            else:
+                (out,) = self._empty(stream, ((T, n_q, self.head_dim), torch.bfloat16))
+            ho = _Heads(out.data_ptr(), n_q * self.head_dim, self.head_dim)
         if out_lse is None and want_lse:
             (out_lse,) = self._empty(stream, ((T, n_q), torch.float32))
+        raw = self._raw_stream(stream)
         if workspace is None:
-            (workspace,) = self._empty(stream, (self.attend_workspace_bytes(), torch.uint8))
+            workspace = self._workspace(raw, stream)
         self._check(self._lib.memstore_attend(
             self._h, layer, hq, n_q, T, ptr(q_start, i32, "q_start", (nreq + 1,)), ptr(seq_lens, i32, "seq_lens", (nreq,)), nreq,
             ptr(block_tables, i32, "block_tables"), block_tables.shape[1], self._paged(cache), scale, max_q_len,
-            hq if out is q else self._heads(out, T, n_q, "out"), None if out_lse is None else ptr(out_lse, torch.float32, "out_lse", (T, n_q)),
+            ho, None if out_lse is None else ptr(out_lse, torch.float32, "out_lse", (T, n_q)),
             None if out_status is None else ptr(out_status, i32, "out_status", (nreq,)), ptr(workspace, torch.uint8, "workspace"),
-            workspace.numel(), self._raw_stream(stream)))  # fmt: skip
+            workspace.numel(), raw))  # fmt: skip
         return out, out_lse, out_status
 
     def stats(self) -> dict:
