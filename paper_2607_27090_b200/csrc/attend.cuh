@@ -30,6 +30,15 @@ constexpr int kAttnMaxGroup = 1024;
 constexpr int kAttnMaxCtasPerSm = 3;
 constexpr int32_t kAttnMaxLen = 1 << 30;  // (key numbers stay inside 32 bits)
 
+// What the border in front of a CTA's share cuts, written by that CTA: the unit to join when the border is the unit's first one.
+struct __align__(16) AttnCut {
+  int32_t c_last;          // last CTA with a part of the unit, -1: nothing to join
+  int32_t rows;            // rows of the unit
+  int32_t tok0, sub0;      // token and query head of the group of row 0
+  int32_t head0;           // first query head of the K/V head
+  int32_t pad[3];
+};
+
 struct AttendParams {
   const __nv_bfloat16* q;
   int64_t q_ts, q_hs;
@@ -55,6 +64,7 @@ struct AttendParams {
   int32_t min_share; // fewest tiles a CTA takes
   float* part_o;     // [CTAs][2][kAttnRows][head_dim]
   float2* part_ml;   // [CTAs][2][kAttnRows]
+  AttnCut* cuts;     // [CTAs]
 };
 
 // One request as the kernels see it.
@@ -268,11 +278,13 @@ __global__ void __launch_bounds__(kAttnThreads, AttnCfg<D, FP8>::kCtasPerSm) att
   const int64_t share = attn_share(total, gridDim.x, p.min_share);
   int64_t off = blockIdx.x * share;
   const int64_t off_end = min(total, off + share);
+  if (tid == 0) p.cuts[blockIdx.x].c_last = -1;  // (until the first unit says otherwise)
   if (off >= off_end) return;
   int64_t req_start;
   int r = line.locate(p.nreq, cost_of, off, s_warp, s_found, &req_start);
   if (r < 0) return;
   AttnReq rq = attn_request(p, r);
+  bool first = true;
 
   uint8_t* ring = smem + warp * (C::kStages * C::kStageBytes);
   const uint32_t ring_u = attn_smem(ring);
@@ -289,6 +301,16 @@ __global__ void __launch_bounds__(kAttnThreads, AttnCfg<D, FP8>::kCtasPerSm) att
     const int row0 = rt * kAttnRows;
     const int rows = min(kAttnRows, rq.rows - row0);
     const int tok0 = row0 / p.group, sub0 = row0 - tok0 * p.group;  // new token and query head of the group of row 0
+    if (first && tid == 0 && t0 != 0 && share >= t0) {
+      AttnCut cut{};
+      cut.c_last = (int)attn_div(off - t0 + tiles - 1, share, &rem);
+      cut.rows = rows;
+      cut.tok0 = rq.q0 + tok0;
+      cut.sub0 = sub0;
+      cut.head0 = kvh * p.group;
+      p.cuts[blockIdx.x] = cut;
+    }
+    first = false;
     const int pos0 = rq.len - rq.n;  // position of the request's first new token
     const int last_pos = pos0 + tok0 + group_div(p, sub0 + rows - 1);
     const int key_end = min(rq.keys, last_pos + 1);  // keys that any row of the unit may see
@@ -654,8 +676,7 @@ __global__ void __launch_bounds__(kAttnThreads, AttnCfg<D, FP8>::kCtasPerSm) att
   }
 }
 
-// Joins the parts of a unit that CTA borders cut: block b looks at the border in front of CTA b's share and joins the unit there when
-// that border is the unit's first.
+// Joins the parts of the unit that the border in front of CTA b's share cuts, if it is the unit's first border.
 constexpr int kCombineThreads = 128;
 constexpr int kJoinBatch = 8;
 // Four elements of a row, summed over parts.
@@ -686,34 +707,11 @@ struct JoinSum {
   }
 };
 template <int D>
-__device__ __forceinline__ void rows_join(const AttendParams& p, int b, int ctas, int64_t* s_warp, int64_t* s_found) {
-  const int tid = threadIdx.x;
-  auto cost_of = [&](int i) { return attn_cost(p, attn_request(p, i)); };
-  AttnLine<kCombineThreads> line;
-  line.init(p.nreq, cost_of, s_warp);
-  const int64_t share = attn_share(line.total, ctas, p.min_share);
-  const int64_t off = b * share;
-  int64_t req_start = 0, rem;
-  const int r = line.locate(p.nreq, cost_of, off, s_warp, s_found, &req_start);
-  // (all that does not depend on the parts comes before the wait for them)
-  int rows = 0, c_last = 0, tok0 = 0, sub0 = 0, head0 = 0;
-  if (r >= 0) {
-    const AttnReq rq = attn_request(p, r);
-    const int tiles = attn_tiles(rq), n_rt = (rq.rows + kAttnRows - 1) / kAttnRows;
-    const int64_t u = attn_div(off - req_start, tiles, &rem);
-    const int t0 = (int)rem;
-    if (t0 != 0 && share >= t0) {  // else no unit is cut here, or an earlier border is the unit's first
-      const int kvh = (int)attn_div(u, n_rt, &rem), row0 = (int)rem * kAttnRows;
-      c_last = (int)attn_div(off - t0 + tiles - 1, share, &rem);
-      rows = min(kAttnRows, rq.rows - row0);
-      tok0 = row0 / p.group;
-      sub0 = row0 - tok0 * p.group;
-      tok0 += rq.q0;
-      head0 = kvh * p.group;
-    }
-  }
-  grid_dependency_wait();
-  for (int e = tid; e < rows * (D / 4); e += kCombineThreads) {
+__device__ __forceinline__ void rows_join(const AttendParams& p, int b) {
+  const AttnCut cut = p.cuts[b];
+  if (cut.c_last < 0) return;
+  const int c_last = cut.c_last;
+  for (int e = threadIdx.x; e < cut.rows * (D / 4); e += kCombineThreads) {
     const int row = e / (D / 4), d = 4 * (e % (D / 4));
     JoinSum sum;
     for (int c0 = b - 1; c0 <= c_last; c0 += kJoinBatch) {
@@ -728,8 +726,8 @@ __device__ __forceinline__ void rows_join(const AttendParams& p, int b, int ctas
       }
       sum.add(ml, x, c_last - c0 + 1);
     }
-    const int dt = group_div(p, sub0 + row);
-    sum.write(p, tok0 + dt, head0 + sub0 + row - dt * p.group, d);
+    const int dt = group_div(p, cut.sub0 + row);
+    sum.write(p, cut.tok0 + dt, cut.head0 + cut.sub0 + row - dt * p.group, d);
   }
 }
 

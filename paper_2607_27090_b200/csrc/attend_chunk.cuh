@@ -53,6 +53,7 @@ struct ChunkParams {
   int32_t min_share;
   float* part_o;      // [CTAs][2][D / 4][kChunkRows][4]
   float2* part_ml;    // [CTAs][2][kChunkRows]
+  AttnCut* cuts;      // [CTAs]
   int32_t* errors;    // [CTAs]: 1 when a wait ran out
   uint32_t spin_limit;
   int mute_producer;
@@ -306,14 +307,59 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
   const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_slot, 0);
   const uint32_t limit = c.spin_limit ? c.spin_limit : kChunkSpinLimit;
 
-  AttnLine<kChunkThreads> line;
-  line.init(p.nreq, [&](int i) { return chunk_cost(c, attn_request(p, i)); }, s_warp);
-  const int64_t total = line.total;
-  const int64_t share = attn_share(total, gridDim.x, c.min_share);
-  int64_t off = blockIdx.x * share;
-  const int64_t off_end = min(total, off + share);
+  auto cost_of = [&](int i) { return chunk_cost(c, attn_request(p, i)); };
+  int64_t off, off_end, share;
   ChunkSeg seg;
-  bool more = off < off_end && chunk_locate<kChunkThreads>(c, line, off, s_warp, s_found, &seg);
+  bool more;
+  auto find = [&] {
+    AttnLine<kChunkThreads> line;
+    line.init(p.nreq, cost_of, s_warp);
+    share = attn_share(line.total, gridDim.x, c.min_share);
+    off = blockIdx.x * share;
+    off_end = min(line.total, off + share);
+    more = off < off_end && chunk_locate<kChunkThreads>(c, line, off, s_warp, s_found, &seg);
+  };
+  if (p.nreq <= 32 * kLinePerLane) {
+    // one warp looks for the CTA's first unit (twenty-four doing the same would wait for one another's issue slots)
+    int32_t* s_seg = reinterpret_cast<int32_t*>(s_warp);
+    if (warp == 0) {
+      find();
+      if (lane == 0) {
+        s_warp[8] = off;
+        s_warp[9] = off_end;
+        s_warp[10] = share;
+        s_seg[0] = more;
+        if (more) {
+          const int32_t v[10] = {seg.r, seg.kvh, seg.rt, seg.t0, seg.tiles, seg.q.q0, seg.q.n, seg.q.len, seg.q.keys, seg.q.rows};
+#pragma unroll
+          for (int i = 0; i < 10; ++i) s_seg[1 + i] = v[i];
+        }
+      }
+    }
+    __syncthreads();
+    off = s_warp[8];
+    off_end = s_warp[9];
+    share = s_warp[10];
+    more = s_seg[0] != 0;
+    seg.r = s_seg[1], seg.kvh = s_seg[2], seg.rt = s_seg[3], seg.t0 = s_seg[4], seg.tiles = s_seg[5];
+    seg.q.q0 = s_seg[6], seg.q.n = s_seg[7], seg.q.len = s_seg[8], seg.q.keys = s_seg[9], seg.q.rows = s_seg[10];
+  } else {
+    find();
+  }
+  if (tid == 0) {
+    AttnCut cut{};
+    cut.c_last = -1;
+    if (more && seg.t0 != 0 && share >= seg.t0) {
+      int64_t rem;
+      const int row0 = seg.rt * kChunkRows, tok0 = row0 / p.group;
+      cut.c_last = (int)attn_div(off - seg.t0 + seg.tiles - 1, share, &rem);
+      cut.rows = min(kChunkRows, seg.q.rows - row0);
+      cut.tok0 = seg.q.q0 + tok0;
+      cut.sub0 = row0 - tok0 * p.group;
+      cut.head0 = seg.kvh * p.group;
+    }
+    c.cuts[blockIdx.x] = cut;
+  }
   // every role walks the same segments
   auto set_end = [&] { seg.t1 = (int)min((int64_t)seg.tiles, seg.t0 + (off_end - off)); };
   auto next = [&] {
@@ -359,21 +405,34 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
         if (!ok) return;
         constexpr int kLanes = D / 8, kPerWarp = 32 / kLanes, kBatch = 8;  // lanes of a row, rows of a load, loads in flight
         const int ql = lane % kLanes;
-#pragma unroll 1
-        for (int i0 = 0; i0 < kChunkRows / 4 / kPerWarp; i0 += kBatch) {
-          uint4 x[kBatch];
-#pragma unroll
-          for (int i = 0; i < kBatch; ++i) {
-            const int row = w * (kChunkRows / 4) + (i0 + i) * kPerWarp + lane / kLanes, dt = group_div(p, sub0 + row);
-            x[i] = make_uint4(0u, 0u, 0u, 0u);
-            if (row < rows)
-              x[i] = *reinterpret_cast<const uint4*>(p.q + (int64_t)(q.q0 + tok0 + dt) * p.q_ts + (int64_t)(seg.kvh * p.group + sub0 + row - dt * p.group) * p.q_hs + ql * 8);
+        auto place = [&](int row) { return q_smem + (row >> 7) * (C::kQBytes / 2) + (ql >> 3) * 16384 + chunk_swz(row & 127, ql & 7); };
+        auto source = [&](int row) {
+          const int dt = group_div(p, sub0 + row);
+          return p.q + (int64_t)(q.q0 + tok0 + dt) * p.q_ts + (int64_t)(seg.kvh * p.group + sub0 + row - dt * p.group) * p.q_hs + ql * 8;
+        };
+        if constexpr (!FP8) {
+#pragma unroll 4
+          for (int i = 0; i < kChunkRows / 4 / kPerWarp; ++i) {
+            const int row = w * (kChunkRows / 4) + i * kPerWarp + lane / kLanes;
+            cp_async16(smem_u32(place(row)), row < rows ? source(row) : p.q, row < rows);
           }
+          cp_async_commit();
+          cp_async_wait<0>();
+        } else {
+#pragma unroll 1
+          for (int i0 = 0; i0 < kChunkRows / 4 / kPerWarp; i0 += kBatch) {
+            uint4 x[kBatch];
 #pragma unroll
-          for (int i = 0; i < kBatch; ++i) {
-            const int row = w * (kChunkRows / 4) + (i0 + i) * kPerWarp + lane / kLanes;
-            uint32_t y[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
-            if constexpr (FP8) {  // to fp16 by a power of two per row (see attend.cuh)
+            for (int i = 0; i < kBatch; ++i) {
+              const int row = w * (kChunkRows / 4) + (i0 + i) * kPerWarp + lane / kLanes;
+              x[i] = make_uint4(0u, 0u, 0u, 0u);
+              if (row < rows) x[i] = *reinterpret_cast<const uint4*>(source(row));
+            }
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i) {
+              // to fp16 by a power of two per row (see attend.cuh)
+              const int row = w * (kChunkRows / 4) + (i0 + i) * kPerWarp + lane / kLanes;
+              uint32_t y[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
               float m = 0.f;
 #pragma unroll
               for (int e = 0; e < 4; ++e) m = fmaxf(m, fmaxf(fabsf(bf16lo(y[e])), fabsf(bf16hi(y[e]))));
@@ -384,8 +443,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
               if (ql == 0) s_qexp[row] = (uint8_t)(254 - ex);
 #pragma unroll
               for (int e = 0; e < 4; ++e) y[e] = pack_half(bf16lo(y[e]) * f, bf16hi(y[e]) * f);
+              *reinterpret_cast<uint4*>(place(row)) = make_uint4(y[0], y[1], y[2], y[3]);
             }
-            *reinterpret_cast<uint4*>(q_smem + (row >> 7) * (C::kQBytes / 2) + (ql >> 3) * 16384 + chunk_swz(row & 127, ql & 7)) = make_uint4(y[0], y[1], y[2], y[3]);
           }
         }
         fence_async_smem();
@@ -676,17 +735,21 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
           }
           float mx = -INFINITY;
 #pragma unroll 1
-          for (int b = 0; b < 4; ++b) {
-            float s[16];
-            tmem_ld16(ts + part * 64 + b * 16, s);
+          for (int b = 0; b < 2; ++b) {
+            float s[32];
+            tmem_ld32(ts + part * 64 + b * 32, s);
             tmem_ld_wait();
-            if (masked) chunk_mask(s, chunk_see(b >= 2 ? there.y : there.x, k0 + (b >> 1) * 32, lim) >> ((b & 1) * 16));
+            if (masked) {
+              const uint32_t see = chunk_see(b ? there.y : there.x, k0 + b * 32, lim);
+              chunk_mask(s, see);
+              chunk_mask(s + 16, see >> 16);
+            }
 #pragma unroll
-            for (int e = 0; e < 16; e += 2) mx = max3(mx, s[e], s[e + 1]);
+            for (int e = 0; e < 32; e += 2) mx = max3(mx, s[e], s[e + 1]);
           }
           // (a row's maximum changes by its own scores alone, so that a row does not depend on its neighbours)
           mx = pair_join(mx, [](float a, float b) { return fmaxf(a, b); });
-          const bool own = pair_join(renew ? 1.f : 0.f, [](float a, float b) { return fmaxf(a, b); }) != 0.f;
+          const bool own = j == 0 || pair_join(renew ? 1.f : 0.f, [](float a, float b) { return fmaxf(a, b); }) != 0.f;
           const float n = own ? fmaxf(m, mx * sc) : m;
           const float f = n == -INFINITY || m == n ? 1.f : ex2(m - n);
           if (j > 0) {
@@ -798,25 +861,15 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
   }
 }
 
-// Joins the parts of a chunk unit that CTA borders cut: block (b - 1, y) looks at the border in front of CTA b's share and serves 16 rows
-// of the unit there when that border is the unit's first.
+// Joins 16 rows of the chunk unit that the border in front of CTA b's share cuts, if it is the unit's first border.
 constexpr int kChunkJoinRows = 16;
 template <int D>
-__device__ __forceinline__ void chunk_join(const ChunkParams& c, int b, int y, int ctas, int64_t* s_warp, int64_t* s_found) {
+__device__ __forceinline__ void chunk_join(const ChunkParams& c, int b, int y) {
   const AttendParams& p = c.a;
-  AttnLine<kCombineThreads> line;
-  line.init(p.nreq, [&](int i) { return chunk_cost(c, attn_request(p, i)); }, s_warp);
-  const int64_t share = attn_share(line.total, ctas, c.min_share);
-  const int64_t off = b * share;
-  ChunkSeg seg;
-  const bool found = chunk_locate<kCombineThreads>(c, line, off, s_warp, s_found, &seg) && seg.t0 != 0 && share >= seg.t0;
-  // (else no unit is cut here, or an earlier border is the unit's first)
-  int64_t rem;
-  const int c_last = found ? (int)attn_div(off - seg.t0 + seg.tiles - 1, share, &rem) : 0;
+  const AttnCut cut = c.cuts[b];
   const int row = y * kChunkJoinRows + threadIdx.x % kChunkJoinRows;
-  grid_dependency_wait();
-  if (!found || row >= min(kChunkRows, seg.q.rows - seg.rt * kChunkRows)) return;
-  const int R = seg.rt * kChunkRows + row, tok = seg.q.q0 + R / p.group, head = seg.kvh * p.group + R % p.group;
+  if (cut.c_last < 0 || row >= cut.rows) return;
+  const int c_last = cut.c_last, dt = group_div(p, cut.sub0 + row), tok = cut.tok0 + dt, head = cut.head0 + cut.sub0 + row - dt * p.group;
   for (int d4 = threadIdx.x / kChunkJoinRows; d4 < D / 4; d4 += kCombineThreads / kChunkJoinRows) {
     JoinSum sum;
     for (int i0 = b - 1; i0 <= c_last; i0 += kJoinBatch) {
@@ -839,18 +892,16 @@ __device__ __forceinline__ void chunk_join(const ChunkParams& c, int b, int y, i
 // each, borders of the rows kernel, then four requests each.
 template <int D>
 __global__ void __launch_bounds__(kCombineThreads) attend_join_kernel(const ChunkParams c, const int chunk_ctas, const int rows_ctas) {
-  __shared__ int64_t s_warp[32], s_found[2];
   grid_launch_dependents();
-  // (every path waits for the kernels before this one, so that whatever waits for this kernel has waited for them)
+  grid_dependency_wait();
   constexpr int kPieces = kChunkRows / kChunkJoinRows;
   int b = blockIdx.x;
   const int chunk_blocks = chunk_ctas > 1 ? (chunk_ctas - 1) * kPieces : 0, row_blocks = rows_ctas > 1 ? rows_ctas - 1 : 0;
   if (b < chunk_blocks) {
-    chunk_join<D>(c, b / kPieces + 1, b % kPieces, chunk_ctas, s_warp, s_found);
+    chunk_join<D>(c, b / kPieces + 1, b % kPieces);
   } else if (b < chunk_blocks + row_blocks) {
-    rows_join<D>(c.a, b - chunk_blocks + 1, rows_ctas, s_warp, s_found);
+    rows_join<D>(c.a, b - chunk_blocks + 1);
   } else {
-    grid_dependency_wait();
     attend_report(c.a, b - chunk_blocks - row_blocks, chunk_ctas > 0 ? c.errors : nullptr, chunk_ctas, c.min_rows);
   }
 }

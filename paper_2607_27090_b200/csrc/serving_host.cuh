@@ -189,7 +189,7 @@ constexpr int kChunkMinRows = kAttnRows;
 // The workspace: unfinished rows of the rows kernel (kAttnMaxCtasPerSm CTAs per SM at most) and their statistics, then those of the chunk kernel
 // (one CTA per SM) and its error words.  It depends on the GPU and head_dim alone.
 struct AttendLayout {
-  size_t rows_o, rows_ml, chunk_o, chunk_ml, errors, bytes;
+  size_t rows_o, rows_ml, rows_cuts, chunk_o, chunk_ml, chunk_cuts, errors, bytes;
 };
 static bool attend_has_chunks(int head_dim) { return head_dim == 64 || head_dim == 128; }
 static AttendLayout attend_layout(const memstore* s) {
@@ -203,9 +203,11 @@ static AttendLayout attend_layout(const memstore* s) {
   };
   w.rows_o = take(sms * kAttnMaxCtasPerSm * 2 * kAttnRows * d * 4);
   w.rows_ml = take(sms * kAttnMaxCtasPerSm * 2 * kAttnRows * 8);
+  w.rows_cuts = take(sms * kAttnMaxCtasPerSm * sizeof(AttnCut));
   if (attend_has_chunks(s->cfg.head_dim)) {
     w.chunk_o = take(sms * 2 * kChunkRows * d * 4);
     w.chunk_ml = take(sms * 2 * kChunkRows * 8);
+    w.chunk_cuts = take(sms * sizeof(AttnCut));
     w.errors = take(sms * 4);
   }
   w.bytes = at;
@@ -326,9 +328,11 @@ ms_status memstore_attend(memstore_t* s, int32_t layer, const ms_heads* q, int32
   char* base = (char*)workspace;
   p.part_o = (float*)(base + w.rows_o);
   p.part_ml = (float2*)(base + w.rows_ml);
+  p.cuts = (AttnCut*)(base + w.rows_cuts);
   cp.min_share = 1;
   cp.part_o = (float*)(base + w.chunk_o);
   cp.part_ml = (float2*)(base + w.chunk_ml);
+  cp.cuts = (AttnCut*)(base + w.chunk_cuts);
   cp.errors = (int32_t*)(base + w.errors);
   cp.spin_limit = s->test_spin_limit;
   cp.mute_producer = s->test_mute_producers;
