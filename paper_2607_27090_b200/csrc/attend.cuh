@@ -111,8 +111,8 @@ __device__ __forceinline__ int group_div(const AttendParams& p, int x) { return 
 constexpr int kLinePerLane = 4;
 template <int THREADS>
 struct AttnLine {
-  int64_t cost[kLinePerLane], before;  // of this lane's requests, and of all requests before them
-  int64_t total;
+  int64_t cost[kLinePerLane] = {}, before = 0;  // of this lane's requests, and of all requests before them
+  int64_t total = 0;
 
   template <typename F>
   __device__ __forceinline__ void init(int nreq, F cost_of, int64_t* s_warp) {
@@ -677,8 +677,32 @@ __global__ void __launch_bounds__(kAttnThreads, AttnCfg<D, FP8>::kCtasPerSm) att
 }
 
 // Joins the parts of the unit that the border in front of CTA b's share cuts, if it is the unit's first border.
-constexpr int kCombineThreads = 128;
+constexpr int kCombineThreads = 512;
 constexpr int kJoinBatch = 8;
+// CTA whose border makes the n-th cut, or -1; by the whole block.
+__device__ __forceinline__ int nth_cut(const AttnCut* cuts, int ctas, int n) {
+  __shared__ int s_count[kCombineThreads / 32], s_cta;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  if (threadIdx.x == 0) s_cta = -1;
+  int before = 0;
+  for (int c0 = 0; c0 < ctas; c0 += kCombineThreads) {
+    const int cta = c0 + threadIdx.x;
+    const bool cut = cta < ctas && cuts[cta].c_last >= 0;
+    const unsigned m = __ballot_sync(0xffffffffu, cut);
+    if (lane == 0) s_count[warp] = __popc(m);
+    __syncthreads();
+    int at = before;
+#pragma unroll
+    for (int w = 0; w < kCombineThreads / 32; ++w) {
+      if (w < warp) at += s_count[w];
+      before += s_count[w];
+    }
+    if (cut && at + __popc(m & ((1u << lane) - 1u)) == n) s_cta = cta;
+    __syncthreads();
+  }
+  return s_cta;
+}
+
 // Four elements of a row, summed over parts.
 struct JoinSum {
   float m = -INFINITY, l = 0.f;
@@ -731,7 +755,7 @@ __device__ __forceinline__ void rows_join(const AttendParams& p, int b) {
   }
 }
 
-// The status words of four requests, a warp each; errors: time-outs of the chunk kernel's CTAs (it serves requests of more than
+// The status words of sixteen requests, a warp each; errors: time-outs of the chunk kernel's CTAs (it serves requests of more than
 // min_rows rows), or nullptr.
 __device__ __forceinline__ void attend_report(const AttendParams& p, int block, const int32_t* errors, int n_errors, int min_rows) {
   const int r = block * (kCombineThreads / 32) + (threadIdx.x >> 5), lane = threadIdx.x & 31;

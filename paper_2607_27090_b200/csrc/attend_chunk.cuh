@@ -8,11 +8,12 @@
 // of a group.  Two halves of 128 rows work in turn: while the tensor cores multiply for one half, the other half's warps form its
 // weights.  Scores go to TMEM, a thread owns one row (no shuffles), the weights return to TMEM in the type of V over the scores'
 // columns and are the A operand of the second product, whose accumulator stays in TMEM for the whole unit.
-//   warps 0-7, 8-15  weights of rows 0-127, 128-255, and the epilogue: two threads share a row, 64 of the tile's keys each (16 warps: a
-//                    single warp per scheduler cannot keep the exponentials' unit busy)
-//   warps 16-19      loads: queries (scaled to fp16 for an 8-bit cache), then K and V tiles of 128 keys through a ring of 5 buffers,
-//                    gathered through the block table with cp.async (8-bit: loaded, converted to fp16 exactly, stored)
-//   warp 20          TMEM allocation, tcgen05.mma issue by one elected lane (warps 21-23 complete its warpgroup)
+//   warps 0-7, 8-15  queries (scaled to fp16 for an 8-bit cache), weights and epilogue of rows 0-127, 128-255: two threads share a row,
+//                    64 of the tile's keys each (16 warps: a single warp per scheduler cannot keep the exponentials' unit busy)
+//   warps 16-19      loads: K and V tiles of 128 keys through a ring of 5 buffers, gathered through the block table with cp.async
+//                    (8-bit: loaded, converted to fp16 exactly, stored)
+//   warp 20          TMEM allocation, tcgen05.mma issue by one elected lane
+//   warp 21          walks the CTA's share of the line and describes its units to the other roles (warps 22, 23 complete the warpgroup)
 // Work split: as in attend.cuh, the tiles of all units (causal: only as many as a unit's last row sees) form one line of which every
 // CTA takes an equal share, so 64 units on 148 SMs balance as well as 6400.
 // Running maximum: the weights are formed with the maximum of the tiles before; no maximum is looked for unless the sum of a thread's 64
@@ -41,7 +42,7 @@ struct ChunkCfg {
   static constexpr int kTileBytes = kChunkKeys * D * 2;              // K or V tile, 16 bits per element
   static constexpr int kQBytes = kChunkRows * D * 2;
   static constexpr int kRingBytes = kChunkStages * kTileBytes;
-  static constexpr int kSmemBytes = 1024 + kQBytes + kRingBytes + 1984;  // alignment, tiles, barriers and small arrays
+  static constexpr int kSmemBytes = 1024 + kQBytes + kRingBytes + 2048;  // alignment, tiles, barriers and small arrays
   static_assert(kSmemBytes <= 232448, "shared memory of a CTA");
   static constexpr int kColO = 2 * kChunkKeys;                       // TMEM: S0, S1 (128 columns each), O0, O1 (D columns each)
   static constexpr int kTmemCols = 512;
@@ -75,6 +76,20 @@ __device__ __forceinline__ int64_t chunk_cost(const ChunkParams& c, const AttnRe
   if (q.n == 0 || q.rows <= c.min_rows) return 0;
   return chunk_head_tiles(c.a, q) * c.a.n_kv;
 }
+
+// What the roles need to know of a unit, in a small ring of shared memory: worked out once, ahead of its use.
+constexpr int kChunkUnits = 4;
+struct __align__(16) ChunkUnit {
+  int32_t nt;               // tiles with keys in this CTA's part, -1: no more units
+  int32_t t0, t1;           // first tile, and one behind the last on the line (t1 - t0 = nt unless the unit has no keys)
+  int32_t rows;             // rows of the unit
+  int32_t req, kvh;         // request and K/V head
+  int32_t tok0, sub0;       // token (row of q) and query head of the group of the unit's row 0
+  int32_t lim_min;          // position of that token: last key that every row sees
+  int32_t key_end;          // one behind the last key that any row sees
+  int32_t keys;             // keys of the request that the table can name
+  int32_t whole;            // all tiles of the unit are here
+};
 
 // A piece of a unit that one CTA works on: tiles t0 .. t1 - 1 of it.
 struct ChunkSeg {
@@ -261,14 +276,15 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
   uint8_t* q_smem = smem;                    // [2 halves of rows][D / 64 column blocks][128 rows][128 B]
   uint8_t* ring = smem + C::kQBytes;         // kChunkStages tiles of [D / 64][128 keys][128 B]
   uint64_t* bars = reinterpret_cast<uint64_t*>(ring + C::kRingBytes);
-  uint64_t* q_full = bars;
-  uint64_t* q_empty = bars + 1;
+  uint64_t* q_full = bars;  // [2 halves]
   uint64_t* kv_full = bars + 2;
   uint64_t* kv_empty = kv_full + kChunkStages;
   uint64_t* s_full = kv_empty + kChunkStages;  // [2]
   uint64_t* p_full = s_full + 2;               // [2]
   uint64_t* o_full = p_full + 2;               // [2]
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(o_full + 2);
+  uint64_t* u_full = o_full + 2;               // [kChunkUnits]
+  uint64_t* u_empty = u_full + kChunkUnits;    // [kChunkUnits]
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(u_empty + kChunkUnits);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   uint32_t* s_masks = tmem_slot + 4;           // [kChunkMaskRing][4]: keys of the tile that the table names
   uint32_t* s_bad = s_masks + 4 * kChunkMaskRing;  // [kChunkMaskRing][4]: a loading warp's part of the V tile holds values that are not
@@ -277,19 +293,24 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
   uint8_t* s_qexp = reinterpret_cast<uint8_t*>(s_pair + kChunkRows);  // [256], 8-bit cache: exponent fields of the rows' inverse powers of two
   int64_t* s_warp = reinterpret_cast<int64_t*>(s_qexp + kChunkRows);  // [32]
   int64_t* s_found = s_warp + 32;                                      // [2]
+  ChunkUnit* units = reinterpret_cast<ChunkUnit*>(s_warp);             // [kChunkUnits], once the first unit has been found
+  static_assert(sizeof(ChunkUnit) * kChunkUnits <= 32 * sizeof(int64_t), "the units' ring takes the place of the scan's");
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
-    mbar_init(q_full, 4);
-    mbar_init(q_empty, 1);
     for (int s = 0; s < kChunkStages; ++s) {
       mbar_init(&kv_full[s], 4);
       mbar_init(&kv_empty[s], 1);
     }
     for (int h = 0; h < 2; ++h) {
+      mbar_init(&q_full[h], 8);
       mbar_init(&s_full[h], 1);
       mbar_init(&p_full[h], 8);
       mbar_init(&o_full[h], 1);
+    }
+    for (int i = 0; i < kChunkUnits; ++i) {
+      mbar_init(&u_full[i], 1);
+      mbar_init(&u_empty[i], 21);  // every warp of the other roles
     }
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -308,9 +329,9 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
   const uint32_t limit = c.spin_limit ? c.spin_limit : kChunkSpinLimit;
 
   auto cost_of = [&](int i) { return chunk_cost(c, attn_request(p, i)); };
-  int64_t off, off_end, share;
+  int64_t off = 0, off_end = 0, share = 1;
   ChunkSeg seg;
-  bool more;
+  bool more = false;
   auto find = [&] {
     AttnLine<kChunkThreads> line;
     line.init(p.nreq, cost_of, s_warp);
@@ -319,58 +340,14 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
     off_end = min(line.total, off + share);
     more = off < off_end && chunk_locate<kChunkThreads>(c, line, off, s_warp, s_found, &seg);
   };
-  if (p.nreq <= 32 * kLinePerLane) {
-    // one warp looks for the CTA's first unit (twenty-four doing the same would wait for one another's issue slots)
-    int32_t* s_seg = reinterpret_cast<int32_t*>(s_warp);
-    if (warp == 0) {
-      find();
-      if (lane == 0) {
-        s_warp[8] = off;
-        s_warp[9] = off_end;
-        s_warp[10] = share;
-        s_seg[0] = more;
-        if (more) {
-          const int32_t v[10] = {seg.r, seg.kvh, seg.rt, seg.t0, seg.tiles, seg.q.q0, seg.q.n, seg.q.len, seg.q.keys, seg.q.rows};
-#pragma unroll
-          for (int i = 0; i < 10; ++i) s_seg[1 + i] = v[i];
-        }
-      }
-    }
-    __syncthreads();
-    off = s_warp[8];
-    off_end = s_warp[9];
-    share = s_warp[10];
-    more = s_seg[0] != 0;
-    seg.r = s_seg[1], seg.kvh = s_seg[2], seg.rt = s_seg[3], seg.t0 = s_seg[4], seg.tiles = s_seg[5];
-    seg.q.q0 = s_seg[6], seg.q.n = s_seg[7], seg.q.len = s_seg[8], seg.q.keys = s_seg[9], seg.q.rows = s_seg[10];
-  } else {
-    find();
+  if (p.nreq > 32 * kLinePerLane) {
+    find();           // (by the whole block; few requests are looked through by the describing warp alone)
+    __syncthreads();  // the scan's memory becomes the units' ring
   }
-  if (tid == 0) {
-    AttnCut cut{};
-    cut.c_last = -1;
-    if (more && seg.t0 != 0 && share >= seg.t0) {
-      int64_t rem;
-      const int row0 = seg.rt * kChunkRows, tok0 = row0 / p.group;
-      cut.c_last = (int)attn_div(off - seg.t0 + seg.tiles - 1, share, &rem);
-      cut.rows = min(kChunkRows, seg.q.rows - row0);
-      cut.tok0 = seg.q.q0 + tok0;
-      cut.sub0 = row0 - tok0 * p.group;
-      cut.head0 = seg.kvh * p.group;
-    }
-    c.cuts[blockIdx.x] = cut;
-  }
-  // every role walks the same segments
-  auto set_end = [&] { seg.t1 = (int)min((int64_t)seg.tiles, seg.t0 + (off_end - off)); };
-  auto next = [&] {
-    off += seg.t1 - seg.t0;
-    more = off < off_end && chunk_next(c, &seg);
-  };
-  // tiles of a segment that hold keys (a unit without keys counts one tile on the line)
-  auto n_tiles = [&] {
-    const int last_row = min((seg.rt + 1) * kChunkRows, seg.q.rows) - 1;
-    const int end = min(seg.q.keys, seg.q.len - seg.q.n + last_row / p.group + 1);
-    return end <= 0 ? 0 : seg.t1 - seg.t0;
+  // unit n of this CTA, once it has been described
+  auto unit_ready = [&](int n) { return chunk_wait(&u_full[n % kChunkUnits], (uint32_t)(n / kChunkUnits) & 1u, abort_flag, limit); };
+  auto unit_done = [&](int n) {
+    if (lane == 0) mbar_arrive(&u_empty[n % kChunkUnits]);
   };
 
   if (warp >= 16 && warp < 20) {
@@ -378,7 +355,6 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
     regs_down<kChunkRegsLoads>();
     const int w = warp - 16, lt = tid - 16 * 32;
     bool ok = !c.mute_producer;
-    uint32_t q_ph = 1;
     int stage = 0, pub = 0, unpublished = 0, mask_at = 0;
     uint32_t ph = 1;
     // the oldest tile's copies have landed: make them visible to the tensor cores, then count the warp in
@@ -389,83 +365,29 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
       if (++pub == kChunkStages) pub = 0;
       --unpublished;
     };
-    for (; more && ok; next()) {
-      set_end();
-      const int nt = n_tiles();
-      if (nt == 0) continue;
-      const AttnReq& q = seg.q;
-      const int row0 = seg.rt * kChunkRows, rows = min(kChunkRows, q.rows - row0);
-      const int pos0 = q.len - q.n;
-      const int tok0 = row0 / p.group, sub0 = row0 - tok0 * p.group;  // new token and query head of the group of row 0
-      const int lim_min = pos0 + tok0, key_end = min(q.keys, lim_min + group_div(p, sub0 + rows - 1) + 1);
-      // ---- queries, once the products of the unit before have read theirs: a warp takes 64 rows, 16 bytes a lane
-      auto load_queries = [&] {
-        ok = chunk_wait(q_empty, q_ph, abort_flag, limit);
-        q_ph ^= 1u;
-        if (!ok) return;
-        constexpr int kLanes = D / 8, kPerWarp = 32 / kLanes, kBatch = 8;  // lanes of a row, rows of a load, loads in flight
-        const int ql = lane % kLanes;
-        auto place = [&](int row) { return q_smem + (row >> 7) * (C::kQBytes / 2) + (ql >> 3) * 16384 + chunk_swz(row & 127, ql & 7); };
-        auto source = [&](int row) {
-          const int dt = group_div(p, sub0 + row);
-          return p.q + (int64_t)(q.q0 + tok0 + dt) * p.q_ts + (int64_t)(seg.kvh * p.group + sub0 + row - dt * p.group) * p.q_hs + ql * 8;
-        };
-        if constexpr (!FP8) {
-#pragma unroll 4
-          for (int i = 0; i < kChunkRows / 4 / kPerWarp; ++i) {
-            const int row = w * (kChunkRows / 4) + i * kPerWarp + lane / kLanes;
-            cp_async16(smem_u32(place(row)), row < rows ? source(row) : p.q, row < rows);
-          }
-          cp_async_commit();
-          cp_async_wait<0>();
-        } else {
-#pragma unroll 1
-          for (int i0 = 0; i0 < kChunkRows / 4 / kPerWarp; i0 += kBatch) {
-            uint4 x[kBatch];
-#pragma unroll
-            for (int i = 0; i < kBatch; ++i) {
-              const int row = w * (kChunkRows / 4) + (i0 + i) * kPerWarp + lane / kLanes;
-              x[i] = make_uint4(0u, 0u, 0u, 0u);
-              if (row < rows) x[i] = *reinterpret_cast<const uint4*>(source(row));
-            }
-#pragma unroll
-            for (int i = 0; i < kBatch; ++i) {
-              // to fp16 by a power of two per row (see attend.cuh)
-              const int row = w * (kChunkRows / 4) + (i0 + i) * kPerWarp + lane / kLanes;
-              uint32_t y[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
-              float m = 0.f;
-#pragma unroll
-              for (int e = 0; e < 4; ++e) m = fmaxf(m, fmaxf(fabsf(bf16lo(y[e])), fabsf(bf16hi(y[e]))));
-#pragma unroll
-              for (int o = kLanes / 2; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-              const int ex = min(max(268 - (int)(__float_as_uint(m) >> 23), 13), 227);
-              const float f = __uint_as_float((uint32_t)ex << 23);
-              if (ql == 0) s_qexp[row] = (uint8_t)(254 - ex);
-#pragma unroll
-              for (int e = 0; e < 4; ++e) y[e] = pack_half(bf16lo(y[e]) * f, bf16hi(y[e]) * f);
-              *reinterpret_cast<uint4*>(place(row)) = make_uint4(y[0], y[1], y[2], y[3]);
-            }
-          }
-        }
-        fence_async_smem();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(q_full);
-      };
+    for (int n = 0; ok; ++n) {
+      ok = unit_ready(n);
+      if (!ok) break;
+      const ChunkUnit u = units[n % kChunkUnits];
+      __syncwarp();
+      if (u.nt < 0) break;
+      unit_done(n);
+      const int t_end = u.t0 + u.nt;
       // ---- tiles: K, V, K, V ...; a thread looks up key lt of the tile, a warp copies its own 32 keys
-      const int32_t* table = p.tables + (int64_t)seg.r * p.max_blocks;
+      const int32_t* table = p.tables + (int64_t)u.req * p.max_blocks;
       auto entry_of = [&](int t) {
         const int key = t * kChunkKeys + lt;
-        return key < key_end ? __ldg(table + attn_page(p, key)) : -1;
+        return key < u.key_end ? __ldg(table + attn_page(p, key)) : -1;
       };
-      int32_t nxt = entry_of(seg.t0);
-      for (int t = seg.t0; ok && t < seg.t1; ++t) {
+      int32_t nxt = entry_of(u.t0);
+      for (int t = u.t0; ok && t < t_end; ++t) {
         const int32_t blk = nxt;
-        if (t + 1 < seg.t1) nxt = entry_of(t + 1);
+        if (t + 1 < t_end) nxt = entry_of(t + 1);
         const int key = t * kChunkKeys + lt;
         const bool live = blk >= 0 && blk < p.num_blocks;
-        const int64_t at = live ? blk * p.block_stride + attn_in_page(p, key) * p.token_stride + seg.kvh * p.head_stride : 0;
+        const int64_t at = live ? blk * p.block_stride + attn_in_page(p, key) * p.token_stride + u.kvh * p.head_stride : 0;
         const uint32_t mask = __ballot_sync(0xffffffffu, live);
-        const bool causal = t * kChunkKeys + kChunkKeys - 1 > lim_min;
+        const bool causal = t * kChunkKeys + kChunkKeys - 1 > u.lim_min;
         if (lane == 0) s_masks[mask_at * 4 + w] = mask;
         bool bad = false;
         for (int kv = 0; kv < 2; ++kv) {
@@ -556,11 +478,6 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
             stage = 0;
             ph ^= 1u;
           }
-          if (kv == 0 && t == seg.t0) {  // the first K tile is on its way
-            // (and everything before it is published: the unit before can end)
-            load_queries();
-            if (!ok) break;
-          }
         }
         if (++mask_at == kChunkMaskRing) mask_at = 0;
       }
@@ -570,7 +487,56 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
   } else if (warp >= 20) {
     // ------------------------------------------------------------------ tensor-core issue
     regs_down<kChunkRegsIssue>();
-    if (warp == 20) {
+    if (warp == 21) {
+      // ---------------------------------------------------------------- units
+      if (p.nreq <= 32 * kLinePerLane) find();
+      auto next = [&] {
+        off += seg.t1 - seg.t0;
+        more = off < off_end && chunk_next(c, &seg);
+      };
+      bool ok = true;
+      for (int n = 0; ok; ++n) {
+        ChunkUnit u{};
+        u.nt = -1;
+        if (more) {
+          const int row0 = seg.rt * kChunkRows, tok0 = row0 / p.group;
+          seg.t1 = (int)min((int64_t)seg.tiles, seg.t0 + (off_end - off));
+          u.t0 = seg.t0;
+          u.t1 = seg.t1;
+          u.rows = min(kChunkRows, seg.q.rows - row0);
+          u.req = seg.r;
+          u.kvh = seg.kvh;
+          u.tok0 = seg.q.q0 + tok0;
+          u.sub0 = row0 - tok0 * p.group;
+          u.lim_min = seg.q.len - seg.q.n + tok0;
+          u.key_end = min(seg.q.keys, u.lim_min + group_div(p, u.sub0 + u.rows - 1) + 1);
+          u.keys = seg.q.keys;
+          u.nt = u.key_end <= 0 ? 0 : seg.t1 - seg.t0;
+          u.whole = seg.t0 == 0 && seg.t1 == seg.tiles;
+        }
+        if (n == 0 && lane == 0) {
+          AttnCut cut{};
+          cut.c_last = -1;
+          if (more && seg.t0 != 0 && share >= seg.t0) {
+            int64_t rem;
+            cut.c_last = (int)attn_div(off - seg.t0 + seg.tiles - 1, share, &rem);
+            cut.rows = u.rows;
+            cut.tok0 = u.tok0;
+            cut.sub0 = u.sub0;
+            cut.head0 = u.kvh * p.group;
+          }
+          c.cuts[blockIdx.x] = cut;
+        }
+        ok = chunk_wait(&u_empty[n % kChunkUnits], ((uint32_t)(n / kChunkUnits) & 1u) ^ 1u, abort_flag, limit);
+        if (!ok) break;
+        if (lane == 0) {
+          units[n % kChunkUnits] = u;
+          mbar_arrive(&u_full[n % kChunkUnits]);
+        }
+        if (u.nt < 0) break;
+        next();
+      }
+    } else if (warp == 20) {
       const bool lead = elect_one();
       constexpr uint32_t kTypes = FP8 ? 0u : (1u << 7) | (1u << 10);  // fp16 or bf16 operands
       constexpr uint32_t kIdescS = (1u << 4) | kTypes | ((uint32_t)(kChunkKeys >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
@@ -580,13 +546,14 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
       int stage = 0;
       uint32_t ph = 0;
       const uint32_t q_u = smem_u32(q_smem), ring_u = smem_u32(ring);
-      for (; more && ok; next()) {
-        set_end();
-        const int nt = n_tiles();
+      for (int n = 0; ok; ++n) {
+        ok = unit_ready(n);
+        if (!ok) break;
+        const int nt = units[n % kChunkUnits].nt, halves = units[n % kChunkUnits].rows > 128 ? 2 : 1;
+        __syncwarp();
+        if (nt < 0) break;
+        unit_done(n);
         if (nt == 0) continue;
-        const int halves = min(kChunkRows, seg.q.rows - seg.rt * kChunkRows) > 128 ? 2 : 1;
-        ok = chunk_wait(q_full, q_ph, abort_flag, limit);
-        q_ph ^= 1u;
         int v_stage = 0;
         uint32_t v_ph = 0;
         for (int j = 0; ok && j <= nt; ++j) {
@@ -610,6 +577,11 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
               if (j == nt) umma_commit_if(lead, &o_full[h]);
             }
             if (j < nt) {  // S = Q K^T
+              if (j == 0) {
+                ok = chunk_wait(&q_full[h], (q_ph >> h) & 1u, abort_flag, limit);
+                if (!ok) break;
+                q_ph ^= 1u << h;
+              }
               tc_fence_after();
               const uint32_t qd = desc_lo_k(q_u + h * (C::kQBytes / 2)), kd = desc_lo_k(ring_u + k_stage * C::kTileBytes);
 #pragma unroll
@@ -621,7 +593,6 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
           if (!ok) break;
           if (j < nt) {
             umma_commit_if(lead, &kv_empty[k_stage]);
-            if (j == nt - 1) umma_commit_if(lead, q_empty);
             if (++stage == kChunkStages) {
               stage = 0;
               ph ^= 1u;
@@ -660,18 +631,74 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
     bool ok = true;
     uint32_t s_ph = 0, o_ph = 0;
     int mask_at = 0;
-    for (; more && ok; next()) {
-      set_end();
-      const int nt = n_tiles();
-      const AttnReq& q = seg.q;
-      const int row0 = seg.rt * kChunkRows, rows = min(kChunkRows, q.rows - row0);
+    // queries of this warp's 16 rows of a unit, 16 bytes a lane; the products of the unit before have read theirs
+    auto load_queries = [&](const ChunkUnit& g) {
+      constexpr int kLanes = D / 8, kPerWarp = 32 / kLanes, kLoads = 16 / kPerWarp;  // lanes of a row, rows of a load
+      const int ql = lane % kLanes, first = h * 128 + (warp & 3) * 32 + part * 16 + lane / kLanes;
+      const int rows = g.rows, sub0 = g.sub0, head0 = g.kvh * p.group;
+      const __nv_bfloat16* q0 = p.q + g.tok0 * p.q_ts + ql * 8;
+      auto place = [&](int r) { return q_smem + h * (C::kQBytes / 2) + (ql >> 3) * 16384 + chunk_swz(r & 127, ql & 7); };
+      auto source = [&](int r) {
+        const int dt = group_div(p, sub0 + r);
+        return q0 + dt * p.q_ts + (int64_t)(head0 + sub0 + r - dt * p.group) * p.q_hs;
+      };
+      if constexpr (!FP8) {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+          const int r = first + i * kPerWarp;
+          cp_async16(smem_u32(place(r)), r < rows ? source(r) : p.q, r < rows);
+        }
+        cp_async_commit();
+        cp_async_wait<0>();
+      } else {
+        uint4 x[kLoads];
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+          const int r = first + i * kPerWarp;
+          x[i] = make_uint4(0u, 0u, 0u, 0u);
+          if (r < rows) x[i] = *reinterpret_cast<const uint4*>(source(r));
+        }
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+          // to fp16 by a power of two per row (see attend.cuh)
+          const int r = first + i * kPerWarp;
+          uint32_t y[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+          float top = 0.f;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) top = fmaxf(top, fmaxf(fabsf(bf16lo(y[e])), fabsf(bf16hi(y[e]))));
+#pragma unroll
+          for (int o = kLanes / 2; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+          const int ex = min(max(268 - (int)(__float_as_uint(top) >> 23), 13), 227);
+          const float f = __uint_as_float((uint32_t)ex << 23);
+          if (ql == 0) s_qexp[r] = (uint8_t)(254 - ex);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) y[e] = pack_half(bf16lo(y[e]) * f, bf16hi(y[e]) * f);
+          *reinterpret_cast<uint4*>(place(r)) = make_uint4(y[0], y[1], y[2], y[3]);
+        }
+      }
+      fence_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&q_full[h]);
+    };
+    // (the two warps of a pair always learn the same of a wait: neither is left at a barrier)
+    bool ready = false, loaded = false;  // the unit has been waited for already, and its queries loaded
+    for (int n = 0; ok; ++n) {
+      if (!ready) ok = !pair_any(pair, !unit_ready(n));
+      if (!ok) break;
+      ready = false;
+      const ChunkUnit& un = units[n % kChunkUnits];
+      const int nt = un.nt;
+      if (nt < 0) break;
+      const int rows = un.rows;
       if (h == 1 && rows <= 128) {
         mask_at = (mask_at + nt) % kChunkMaskRing;
+        __syncwarp();
+        unit_done(n);
         continue;
       }
-      const int tok0 = row0 / p.group, sub0 = row0 - tok0 * p.group;
-      const int dt = group_div(p, sub0 + min(row, rows - 1));
-      const int lim_min = q.len - q.n + tok0, lim = lim_min + dt;
+      if (!loaded && nt > 0) load_queries(un);
+      loaded = false;
+      const int lim_min = un.lim_min, lim = lim_min + group_div(p, un.sub0 + min(row, rows - 1)), t0 = un.t0;
       float m = -INFINITY, l = 0.f, sc = p.scale_log2;
       bool any_bad = false;
       int v_at = 0;
@@ -685,11 +712,11 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
         s_ph ^= 1u;
         tc_fence_after();
         if (FP8 && j == 0) sc = p.scale_log2 * __uint_as_float((uint32_t)s_qexp[row] << 23);
-        const int k0 = (seg.t0 + j) * kChunkKeys + part * 64;
+        const int k0 = (t0 + j) * kChunkKeys + part * 64;
         const uint2 there = *reinterpret_cast<const uint2*>(s_masks + mask_at * 4 + part * 2);
         if (v_causal) look_at_v();  // (of the tile before: its product with V was issued before these scores)
         v_at = mask_at;
-        v_causal = (seg.t0 + j) * kChunkKeys + kChunkKeys - 1 > lim_min;
+        v_causal = (t0 + j) * kChunkKeys + kChunkKeys - 1 > lim_min;
         if (++mask_at == kChunkMaskRing) mask_at = 0;
         const bool masked = k0 + 63 > lim_min || (there.x & there.y) != 0xffffffffu;
         uint32_t pk[32];
@@ -777,6 +804,16 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
         __syncwarp();
         if (lane == 0) mbar_arrive(&p_full[h]);
       }
+      // all scores of this half have been taken, so its queries' place is free: the next unit's come while the last product runs
+      if (ok) {
+        ok = !pair_any(pair, !unit_ready(n + 1));
+        const ChunkUnit& next = units[(n + 1) % kChunkUnits];
+        ready = ok;
+        if (ok && next.nt > 0 && (h == 0 || next.rows > 128)) {
+          load_queries(next);
+          loaded = true;
+        }
+      }
       if (ok && nt > 0) {
         ok = chunk_wait(&o_full[h], o_ph, abort_flag, limit);
         o_ph ^= 1u;
@@ -787,11 +824,11 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
       if (!ok) break;
       // ---- epilogue: this thread's half of its row
       if (nt > 0) l = pair_join(l, [](float a, float b) { return a + b; });
-      const bool whole = seg.t0 == 0 && seg.t1 == seg.tiles;
+      const bool whole = un.whole != 0;
       const bool mine = row < rows;
-      const int tok = q.q0 + tok0 + dt, head = seg.kvh * p.group + sub0 + min(row, rows - 1) - dt * p.group;
+      const int sr = un.sub0 + min(row, rows - 1), dt = group_div(p, sr), tok = un.tok0 + dt, head = un.kvh * p.group + sr - dt * p.group;
       const float inv = l == 0.f ? 0.f : p.v_scale / l;
-      const int64_t slot = (int64_t)blockIdx.x * 2 + (seg.t0 == 0 ? 1 : 0);
+      const int64_t slot = (int64_t)blockIdx.x * 2 + (t0 == 0 ? 1 : 0);
       if (mine && part == 0) {
         if (whole) {
           if (p.lse) p.lse[(int64_t)tok * p.n_q + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
@@ -800,28 +837,28 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
         }
       }
 #pragma unroll 1
-      for (int b = 0; b < D / 2; b += 16) {
+      for (int b = 0; b < D / 2; b += 32) {
         const int col = part * (D / 2) + b;
-        float o[16];
+        float o[32];
         if (nt > 0) {
-          tmem_ld16(to + b, o);
+          tmem_ld32(to + b, o);
           tmem_ld_wait();
         } else {
 #pragma unroll
-          for (int e = 0; e < 16; ++e) o[e] = 0.f;
+          for (int e = 0; e < 32; ++e) o[e] = 0.f;
         }
         if (any_bad) {
           // values that are not finite, at the keys of this segment's causal tiles that the row sees: their weight is positive, so
           // they decide the sum
-          const int32_t* table = p.tables + (int64_t)seg.r * p.max_blocks;
-          const int from = max(seg.t0, (lim_min + 1) / kChunkKeys) * kChunkKeys;
-          const int to_key = min(min(lim, q.keys - 1), seg.t1 * kChunkKeys - 1);
+          const int32_t* table = p.tables + (int64_t)un.req * p.max_blocks;
+          const int from = max(t0, (lim_min + 1) / kChunkKeys) * kChunkKeys;
+          const int to_key = min(min(lim, un.keys - 1), un.t1 * kChunkKeys - 1);
           for (int key = from; key <= to_key; ++key) {
             const int32_t blk = __ldg(table + key / p.block_size);
             if (blk < 0 || blk >= p.num_blocks) continue;
-            const uint8_t* v = p.v_cache + blk * p.block_stride + (key % p.block_size) * p.token_stride + seg.kvh * p.head_stride;
+            const uint8_t* v = p.v_cache + blk * p.block_stride + (key % p.block_size) * p.token_stride + un.kvh * p.head_stride;
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
+            for (int e = 0; e < 32; ++e) {
               if (FP8) {
                 if ((v[col + e] & 0x7f) == 0x7f) o[e] = NAN;
               } else {
@@ -835,16 +872,18 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
           if (whole) {
             __nv_bfloat16* dst = p.out + tok * p.o_ts + head * p.o_hs + col;
 #pragma unroll
-            for (int e = 0; e < 16; e += 8)
+            for (int e = 0; e < 32; e += 8)
               *reinterpret_cast<uint4*>(dst + e) = make_uint4(pack_bf16(o[e] * inv, o[e + 1] * inv), pack_bf16(o[e + 2] * inv, o[e + 3] * inv),
                                                               pack_bf16(o[e + 4] * inv, o[e + 5] * inv), pack_bf16(o[e + 6] * inv, o[e + 7] * inv));
           } else {
 #pragma unroll
-            for (int e = 0; e < 16; e += 4)
+            for (int e = 0; e < 32; e += 4)
               *reinterpret_cast<float4*>(c.part_o + ((slot * (D / 4) + (col + e) / 4) * kChunkRows + row) * 4) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
           }
         }
       }
+      __syncwarp();
+      unit_done(n);
       tc_fence_before();  // (the accumulator is read; the next unit's first product follows this warp's next arrival)
     }
   }
@@ -888,21 +927,24 @@ __device__ __forceinline__ void chunk_join(const ChunkParams& c, int b, int y) {
   }
 }
 
-// Joins what CTA borders cut and reports on the requests; the last kernel of a call.  Blocks: 16 rows of a border of the chunk kernel
-// each, borders of the rows kernel, then four requests each.
+// Joins what CTA borders cut and reports on the requests; the last kernel of a call.  Blocks: 16 rows of a cut unit of the chunk kernel
+// each, cut units of the rows kernel, then sixteen requests each.  There are as many blocks as units could be cut - no more than there
+// are units or borders - and block n looks for the n-th cut among those that the CTAs recorded.
 template <int D>
-__global__ void __launch_bounds__(kCombineThreads) attend_join_kernel(const ChunkParams c, const int chunk_ctas, const int rows_ctas) {
+__global__ void __launch_bounds__(kCombineThreads) attend_join_kernel(const ChunkParams c, const int chunk_ctas, const int chunk_joins, const int rows_ctas,
+                                                                      const int rows_joins) {
   grid_launch_dependents();
   grid_dependency_wait();
   constexpr int kPieces = kChunkRows / kChunkJoinRows;
   int b = blockIdx.x;
-  const int chunk_blocks = chunk_ctas > 1 ? (chunk_ctas - 1) * kPieces : 0, row_blocks = rows_ctas > 1 ? rows_ctas - 1 : 0;
-  if (b < chunk_blocks) {
-    chunk_join<D>(c, b / kPieces + 1, b % kPieces);
-  } else if (b < chunk_blocks + row_blocks) {
-    rows_join<D>(c.a, b - chunk_blocks + 1);
+  if (b < chunk_joins * kPieces) {
+    const int cta = nth_cut(c.cuts, chunk_ctas, b / kPieces);
+    if (cta >= 0) chunk_join<D>(c, cta, b % kPieces);
+  } else if ((b -= chunk_joins * kPieces) < rows_joins) {
+    const int cta = nth_cut(c.a.cuts, rows_ctas, b);
+    if (cta >= 0) rows_join<D>(c.a, cta);
   } else {
-    attend_report(c.a, b - chunk_blocks - row_blocks, chunk_ctas > 0 ? c.errors : nullptr, chunk_ctas, c.min_rows);
+    attend_report(c.a, b - rows_joins, chunk_ctas > 0 ? c.errors : nullptr, chunk_ctas, c.min_rows);
   }
 }
 

@@ -254,9 +254,13 @@ static ms_status attend_launch(memstore* s, ChunkParams& c, int64_t max_rows, cu
     s->kernels_launched++;
   }
   const int checks = p.status ? (p.nreq + kCombineThreads / 32 - 1) / (kCombineThreads / 32) : 0;
-  const int joins = (chunk_ctas > 1 ? (chunk_ctas - 1) * (kChunkRows / kChunkJoinRows) : 0) + (rows_ctas > 1 ? rows_ctas - 1 : 0);
-  if (joins + checks > 0) {
-    MS_CUDA(s, launch_dependent(attend_join_kernel<D>, dim3((unsigned)(joins + checks)), dim3(kCombineThreads), 0, st, c, chunk_ctas, rows_ctas));
+  // units that the call can have, and so cuts to join (each unit has one first border)
+  const int64_t all_rows = (int64_t)p.n_tokens * p.group;
+  const int chunk_joins = (int)std::max<int64_t>(0, std::min<int64_t>(chunk_ctas - 1, p.n_kv * (all_rows / kChunkRows + p.nreq)));
+  const int rows_joins = (int)std::max<int64_t>(0, std::min<int64_t>(rows_ctas - 1, p.n_kv * (all_rows / kAttnRows + p.nreq)));
+  const int blocks = chunk_joins * (kChunkRows / kChunkJoinRows) + rows_joins + checks;
+  if (blocks > 0) {
+    MS_CUDA(s, launch_dependent(attend_join_kernel<D>, dim3((unsigned)blocks), dim3(kCombineThreads), 0, st, c, chunk_ctas, chunk_joins, rows_ctas, rows_joins));
     s->kernels_launched++;
   }
   return MS_OK;
