@@ -62,6 +62,7 @@ struct AttendParams {
   int32_t* status;
   int32_t max_rows;  // requests with more rows per K/V head are served by the kernel for chunks
   int32_t min_share; // fewest tiles a CTA takes
+  int32_t beside;    // the kernel before this one is the same call's chunk kernel
   float* part_o;     // [CTAs][2][kAttnRows][head_dim]
   float2* part_ml;   // [CTAs][2][kAttnRows]
   AttnCut* cuts;     // [CTAs]
@@ -106,33 +107,32 @@ __device__ __forceinline__ int64_t attn_div(int64_t a, int64_t b, int64_t* rem) 
 // x / group for x < 2^20 (exact: the product's error x * group / 2^32 stays below 1 / group)
 __device__ __forceinline__ int group_div(const AttendParams& p, int x) { return p.group_magic ? (int)__umulhi((uint32_t)x, p.group_magic) : x; }
 
-// The line of all tiles of a call.  Up to 128 requests every warp holds the line by itself, four requests a lane (one round of loads,
-// no barrier); more requests are scanned by the block, a pass per THREADS requests.
+// The line of all tiles of a call.  Up to 128 requests every warp holds the line by itself, request 32 i + l in lane l (no barrier);
+// more requests are scanned by the block, a pass per THREADS requests.
 constexpr int kLinePerLane = 4;
 template <int THREADS>
 struct AttnLine {
-  int64_t cost[kLinePerLane] = {}, before = 0;  // of this lane's requests, and of all requests before them
+  int64_t cost[kLinePerLane] = {}, end[kLinePerLane] = {};  // of this lane's requests: tiles, and place behind the last on the line
   int64_t total = 0;
 
   template <typename F>
   __device__ __forceinline__ void init(int nreq, F cost_of, int64_t* s_warp) {
     if (nreq <= 32 * kLinePerLane) {
       const int lane = threadIdx.x & 31;
-      int64_t own = 0;
 #pragma unroll
       for (int i = 0; i < kLinePerLane; ++i) {
-        const int r = lane * kLinePerLane + i;
+        if (32 * i >= nreq) break;  // uniform
+        const int r = 32 * i + lane;
         cost[i] = r < nreq ? cost_of(r) : 0;
-        own += cost[i];
-      }
-      int64_t v = own;
+        int64_t v = cost[i];
 #pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int64_t u = __shfl_up_sync(0xffffffffu, v, o);
-        if (lane >= o) v += u;
+        for (int o = 1; o < 32; o <<= 1) {
+          const int64_t u = __shfl_up_sync(0xffffffffu, v, o);
+          if (lane >= o) v += u;
+        }
+        end[i] = total + v;
+        total = __shfl_sync(0xffffffffu, end[i], 31);
       }
-      before = v - own;
-      total = __shfl_sync(0xffffffffu, v, 31);
     } else {
       int64_t sum = 0;
       for (int r = threadIdx.x; r < nreq; r += THREADS) sum += cost_of(r);
@@ -145,17 +145,14 @@ struct AttnLine {
   __device__ __forceinline__ int locate(int nreq, F cost_of, int64_t off, int64_t* s_warp, int64_t* s_found, int64_t* start) const {
     if (off >= total) return -1;
     if (nreq <= 32 * kLinePerLane) {
-      int64_t at = before;
       int found = -1;
       int64_t found_at = 0;
 #pragma unroll
-      for (int i = 0; i < kLinePerLane; ++i) {
-        if (off >= at && off < at + cost[i]) {
-          found = (int)(threadIdx.x & 31) * kLinePerLane + i;
-          found_at = at;
+      for (int i = 0; i < kLinePerLane; ++i)
+        if (off < end[i] && off >= end[i] - cost[i]) {
+          found = 32 * i + (int)(threadIdx.x & 31);
+          found_at = end[i] - cost[i];
         }
-        at += cost[i];
-      }
       const int src = __ffs(__ballot_sync(0xffffffffu, found >= 0)) - 1;
       *start = __shfl_sync(0xffffffffu, found_at, src);
       return __shfl_sync(0xffffffffu, found, src);
@@ -267,7 +264,9 @@ __global__ void __launch_bounds__(kAttnThreads, AttnCfg<D, FP8>::kCtasPerSm) att
   __shared__ int64_t s_warp[32], s_found[2];
   __shared__ float s_m[kAttnWarps][kAttnRows], s_l[kAttnWarps][kAttnRows];
   __shared__ uint32_t s_mask[kAttnWarps][C::kStages];
-  grid_dependency_wait();
+  // The chunk kernel of the same call has waited for everything before the call when it let this grid start, and the two touch
+  // different rows: this one need not wait for it to begin, only to end (so that whatever waits for this grid has waited for both).
+  if (!p.beside) grid_dependency_wait();
   grid_launch_dependents();
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t4 = lane & 3;
 
@@ -279,17 +278,16 @@ __global__ void __launch_bounds__(kAttnThreads, AttnCfg<D, FP8>::kCtasPerSm) att
   int64_t off = blockIdx.x * share;
   const int64_t off_end = min(total, off + share);
   if (tid == 0) p.cuts[blockIdx.x].c_last = -1;  // (until the first unit says otherwise)
-  if (off >= off_end) return;
-  int64_t req_start;
-  int r = line.locate(p.nreq, cost_of, off, s_warp, s_found, &req_start);
-  if (r < 0) return;
-  AttnReq rq = attn_request(p, r);
+  int64_t req_start = 0;
+  int r = off < off_end ? line.locate(p.nreq, cost_of, off, s_warp, s_found, &req_start) : -1;
+  AttnReq rq{};
+  if (r >= 0) rq = attn_request(p, r);
   bool first = true;
 
   uint8_t* ring = smem + warp * (C::kStages * C::kStageBytes);
   const uint32_t ring_u = attn_smem(ring);
 
-  while (off < off_end) {
+  while (r >= 0 && off < off_end) {
     // ---- the unit that tile `off` belongs to
     const int tiles = attn_tiles(rq), n_rt = (rq.rows + kAttnRows - 1) / kAttnRows;
     int64_t rem;
@@ -669,18 +667,20 @@ __global__ void __launch_bounds__(kAttnThreads, AttnCfg<D, FP8>::kCtasPerSm) att
     if (off < off_end && off - req_start >= attn_cost(p, rq)) {
       req_start = off;
       do {
-        if (++r >= p.nreq) return;  // (cannot be: off lies before the end of the line)
-        rq = attn_request(p, r);
-      } while (attn_cost(p, rq) == 0);
+        if (++r >= p.nreq) r = -1;  // (cannot be: off lies before the end of the line)
+        else rq = attn_request(p, r);
+      } while (r >= 0 && attn_cost(p, rq) == 0);
     }
   }
+  if (p.beside) grid_dependency_wait();
 }
 
 // Joins the parts of the unit that the border in front of CTA b's share cuts, if it is the unit's first border.
 constexpr int kCombineThreads = 512;
 constexpr int kJoinBatch = 8;
 // CTA whose border makes the n-th cut, or -1; by the whole block.
-__device__ __forceinline__ int nth_cut(const AttnCut* cuts, int ctas, int n) {
+__device__ __forceinline__ int nth_cut(const AttnCut* cuts, int ctas, int cuts_at_most, int n) {
+  if (cuts_at_most >= ctas - 1) return cuts[n + 1].c_last >= 0 ? n + 1 : -1;  // a block per border
   __shared__ int s_count[kCombineThreads / 32], s_cta;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   if (threadIdx.x == 0) s_cta = -1;

@@ -752,49 +752,60 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
           else
             form(mm, ChunkNo{});
         };
-        if (ok && j > 0) form_any(m);
-        // (also the point from which both warps have read their scores, over which the weights are stored)
-        const bool renew = sum > kChunkMaxSum || m == -INFINITY;  // (always in a segment's first tile, rarely later)
-        if (pair_any(pair, !ok || renew)) {
-          if (pair_any(pair, !ok)) {  // a wait ran out: both warps leave together, neither is left at a barrier
-            ok = false;
+        // A new maximum is taken first in a segment's first tile, and later when the sum asks for one.  (The vote is also the point
+        // from which both warps have read their scores, over which the weights are stored.)
+        bool renew = j == 0, again = renew, stop = false;  // stop: a wait ran out, and both warps leave together
+        if (again) stop = pair_any(pair, !ok);
+#pragma unroll 1
+        while (!stop) {
+          if (again) {
+            float mx = -INFINITY;
+#pragma unroll 1
+            for (int b = 0; b < 2; ++b) {
+              float s[32];
+              tmem_ld32(ts + part * 64 + b * 32, s);
+              tmem_ld_wait();
+              if (masked) {
+                const uint32_t see = chunk_see(b ? there.y : there.x, k0 + b * 32, lim);
+                chunk_mask(s, see);
+                chunk_mask(s + 16, see >> 16);
+              }
+#pragma unroll
+              for (int e = 0; e < 32; e += 2) mx = max3(mx, s[e], s[e + 1]);
+            }
+            // (a row's maximum changes by its own scores alone, so that a row does not depend on its neighbours)
+            mx = pair_join(mx, [](float a, float b) { return fmaxf(a, b); });
+            const bool own = j == 0 || pair_join(renew ? 1.f : 0.f, [](float a, float b) { return fmaxf(a, b); }) != 0.f;
+            const float n = own ? fmaxf(m, mx * sc) : m;
+            const float f = n == -INFINITY || m == n ? 1.f : ex2(m - n);
+            if (j > 0) {
+              // the accumulator holds the tiles before this one (the commit that signalled these scores follows their product)
+#pragma unroll 1
+              for (int b = 0; b < D / 2; b += 16) {
+                float o[16];
+                tmem_ld16(to + b, o);
+                tmem_ld_wait();
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[e] *= f;
+                tmem_st16(to + b, reinterpret_cast<const uint32_t*>(o));
+              }
+            }
+            l *= f;
+            m = n;
+          }
+          if (ok) form_any(m);
+          if (again) {
+            pair_sync(pair);
             break;
           }
-          float mx = -INFINITY;
-#pragma unroll 1
-          for (int b = 0; b < 2; ++b) {
-            float s[32];
-            tmem_ld32(ts + part * 64 + b * 32, s);
-            tmem_ld_wait();
-            if (masked) {
-              const uint32_t see = chunk_see(b ? there.y : there.x, k0 + b * 32, lim);
-              chunk_mask(s, see);
-              chunk_mask(s + 16, see >> 16);
-            }
-#pragma unroll
-            for (int e = 0; e < 32; e += 2) mx = max3(mx, s[e], s[e + 1]);
-          }
-          // (a row's maximum changes by its own scores alone, so that a row does not depend on its neighbours)
-          mx = pair_join(mx, [](float a, float b) { return fmaxf(a, b); });
-          const bool own = j == 0 || pair_join(renew ? 1.f : 0.f, [](float a, float b) { return fmaxf(a, b); }) != 0.f;
-          const float n = own ? fmaxf(m, mx * sc) : m;
-          const float f = n == -INFINITY || m == n ? 1.f : ex2(m - n);
-          if (j > 0) {
-            // the accumulator holds the tiles before this one (the commit that signalled these scores follows their product)
-#pragma unroll 1
-            for (int b = 0; b < D / 2; b += 16) {
-              float o[16];
-              tmem_ld16(to + b, o);
-              tmem_ld_wait();
-#pragma unroll
-              for (int e = 0; e < 16; ++e) o[e] *= f;
-              tmem_st16(to + b, reinterpret_cast<const uint32_t*>(o));
-            }
-          }
-          l *= f;
-          m = n;
-          form_any(m);
-          pair_sync(pair);
+          renew = sum > kChunkMaxSum || m == -INFINITY;
+          again = pair_any(pair, !ok || renew);
+          if (!again) break;
+          stop = pair_any(pair, !ok);
+        }
+        if (stop) {
+          ok = false;
+          break;
         }
         l += sum;
         tmem_st16(ts + part * 32, pk);
@@ -903,11 +914,11 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
 // Joins 16 rows of the chunk unit that the border in front of CTA b's share cuts, if it is the unit's first border.
 constexpr int kChunkJoinRows = 16;
 template <int D>
-__device__ __forceinline__ void chunk_join(const ChunkParams& c, int b, int y) {
+__device__ __forceinline__ void chunk_join(const ChunkParams& c, int b, int row0) {
   const AttendParams& p = c.a;
   const AttnCut cut = c.cuts[b];
-  const int row = y * kChunkJoinRows + threadIdx.x % kChunkJoinRows;
-  if (cut.c_last < 0 || row >= cut.rows) return;
+  const int row = row0 + threadIdx.x % kChunkJoinRows;
+  if (row >= cut.rows) return;
   const int c_last = cut.c_last, dt = group_div(p, cut.sub0 + row), tok = cut.tok0 + dt, head = cut.head0 + cut.sub0 + row - dt * p.group;
   for (int d4 = threadIdx.x / kChunkJoinRows; d4 < D / 4; d4 += kCombineThreads / kChunkJoinRows) {
     JoinSum sum;
@@ -927,21 +938,21 @@ __device__ __forceinline__ void chunk_join(const ChunkParams& c, int b, int y) {
   }
 }
 
-// Joins what CTA borders cut and reports on the requests; the last kernel of a call.  Blocks: 16 rows of a cut unit of the chunk kernel
-// each, cut units of the rows kernel, then sixteen requests each.  There are as many blocks as units could be cut - no more than there
+// Joins what CTA borders cut and reports on the requests; the last kernel of a call.  Blocks: `pieces` for each cut unit of the chunk
+// kernel (16 rows at a time; few cuts are spread over more blocks), cut units of the rows kernel, then sixteen requests each.  There are as many blocks as units could be cut - no more than there
 // are units or borders - and block n looks for the n-th cut among those that the CTAs recorded.
 template <int D>
-__global__ void __launch_bounds__(kCombineThreads) attend_join_kernel(const ChunkParams c, const int chunk_ctas, const int chunk_joins, const int rows_ctas,
-                                                                      const int rows_joins) {
+__global__ void __launch_bounds__(kCombineThreads) attend_join_kernel(const ChunkParams c, const int chunk_ctas, const int chunk_joins, const int pieces,
+                                                                      const int rows_ctas, const int rows_joins) {
   grid_launch_dependents();
   grid_dependency_wait();
-  constexpr int kPieces = kChunkRows / kChunkJoinRows;
   int b = blockIdx.x;
-  if (b < chunk_joins * kPieces) {
-    const int cta = nth_cut(c.cuts, chunk_ctas, b / kPieces);
-    if (cta >= 0) chunk_join<D>(c, cta, b % kPieces);
-  } else if ((b -= chunk_joins * kPieces) < rows_joins) {
-    const int cta = nth_cut(c.a.cuts, rows_ctas, b);
+  if (b < chunk_joins * pieces) {
+    const int cta = nth_cut(c.cuts, chunk_ctas, chunk_joins, b / pieces);
+    if (cta >= 0)
+      for (int row0 = (b % pieces) * kChunkJoinRows; row0 < kChunkRows; row0 += pieces * kChunkJoinRows) chunk_join<D>(c, cta, row0);
+  } else if ((b -= chunk_joins * pieces) < rows_joins) {
+    const int cta = nth_cut(c.a.cuts, rows_ctas, rows_joins, b);
     if (cta >= 0) rows_join<D>(c.a, cta);
   } else {
     attend_report(c.a, b - rows_joins, chunk_ctas > 0 ? c.errors : nullptr, chunk_ctas, c.min_rows);

@@ -240,6 +240,7 @@ static ms_status attend_launch(memstore* s, ChunkParams& c, int64_t max_rows, cu
   const bool rows = !chunks || p.nreq > 1;
   c.min_rows = rows ? kChunkMinRows : 0;
   p.max_rows = chunks ? c.min_rows : 0x7fffffff;
+  p.beside = chunks;
   int chunk_ctas = 0, rows_ctas = 0;
   if constexpr (D == 64 || D == 128) {
     if (chunks) {
@@ -258,9 +259,10 @@ static ms_status attend_launch(memstore* s, ChunkParams& c, int64_t max_rows, cu
   const int64_t all_rows = (int64_t)p.n_tokens * p.group;
   const int chunk_joins = (int)std::max<int64_t>(0, std::min<int64_t>(chunk_ctas - 1, p.n_kv * (all_rows / kChunkRows + p.nreq)));
   const int rows_joins = (int)std::max<int64_t>(0, std::min<int64_t>(rows_ctas - 1, p.n_kv * (all_rows / kAttnRows + p.nreq)));
-  const int blocks = chunk_joins * (kChunkRows / kChunkJoinRows) + rows_joins + checks;
+  const int pieces = chunk_joins <= 32 ? kChunkRows / kChunkJoinRows : 4;
+  const int blocks = chunk_joins * pieces + rows_joins + checks;
   if (blocks > 0) {
-    MS_CUDA(s, launch_dependent(attend_join_kernel<D>, dim3((unsigned)blocks), dim3(kCombineThreads), 0, st, c, chunk_ctas, chunk_joins, rows_ctas, rows_joins));
+    MS_CUDA(s, launch_dependent(attend_join_kernel<D>, dim3((unsigned)blocks), dim3(kCombineThreads), 0, st, c, chunk_ctas, chunk_joins, pieces, rows_ctas, rows_joins));
     s->kernels_launched++;
   }
   return MS_OK;
