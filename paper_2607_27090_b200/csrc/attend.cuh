@@ -8,12 +8,13 @@
 // an m16n8k16 product are (token, query head) pairs that share a K/V head, so a cache row is read once for all heads of its
 // group; the legacy matrix instructions are far from their limit here.
 //
-// Work split: a unit is (request, K/V head, 16 rows) x all its tiles of 64 keys.  The tiles of all units are numbered one after
+// Work split: a unit is (request, K/V head, 16 rows) x all its tiles of 64 keys (128 where cache rows are
+// at most 128 bytes).  The tiles of all units are numbered one after
 // another and every CTA of one resident wave takes an equal share of that line, wherever unit borders fall: ragged lengths
 // balance exactly, and a CTA leaves at most two unfinished units (its first and its last), which attend_combine_kernel joins.
 // The workspace therefore depends on the number of CTAs alone.  Every order of summation follows from the lengths: results are
 // the same on every run.
-// Inside a CTA each warp streams its own 16 of the 64 keys through a private ring (cp.async), with running statistics of its
+// Inside a CTA each warp streams its own quarter of a tile's keys through a private ring (cp.async), with running statistics of its
 // own: no barrier inside a unit; the four warps join at its end.
 #pragma once
 #include "blocks.cuh"
@@ -24,10 +25,8 @@ namespace ms {
 constexpr int kAttnRows = 16;      // query rows of a unit
 constexpr int kAttnWarps = 4;
 constexpr int kAttnThreads = kAttnWarps * 32;
-constexpr int kAttnWarpKeys = 16;  // keys of a warp in a tile
-constexpr int kAttnTileKeys = kAttnWarps * kAttnWarpKeys;
 constexpr int kAttnMaxGroup = 1024;
-constexpr int kAttnMaxCtasPerSm = 3;
+constexpr int kAttnMaxCtasPerSm = 2;
 constexpr int32_t kAttnMaxLen = 1 << 30;  // (key numbers stay inside 32 bits)
 
 // What the border in front of a CTA's share cuts, written by that CTA: the unit to join when the border is the unit's first one.
@@ -62,6 +61,7 @@ struct AttendParams {
   int32_t* status;
   int32_t max_rows;  // requests with more rows per K/V head are served by the kernel for chunks
   int32_t min_share; // fewest tiles a CTA takes
+  int32_t tile_shift; // log2 of the keys of a tile
   int32_t beside;    // the kernel before this one is the same call's chunk kernel
   float* part_o;     // [CTAs][2][kAttnRows][head_dim]
   float2* part_ml;   // [CTAs][2][kAttnRows]
@@ -87,10 +87,10 @@ __device__ __forceinline__ AttnReq attn_request(const AttendParams& p, int r) {
   return a;
 }
 // Tiles of one unit of the request (one at least, so that rows without keys are written too), and of all its units.
-__device__ __forceinline__ int attn_tiles(const AttnReq& a) { return max(1, (a.keys + kAttnTileKeys - 1) / kAttnTileKeys); }
+__device__ __forceinline__ int attn_tiles(const AttendParams& p, const AttnReq& a) { return max(1, (a.keys + (1 << p.tile_shift) - 1) >> p.tile_shift); }
 __device__ __forceinline__ int64_t attn_cost(const AttendParams& p, const AttnReq& a) {
   if (a.n == 0 || a.rows > p.max_rows) return 0;
-  return (int64_t)((a.rows + kAttnRows - 1) / kAttnRows) * p.n_kv * attn_tiles(a);
+  return (int64_t)((a.rows + kAttnRows - 1) / kAttnRows) * p.n_kv * attn_tiles(p, a);
 }
 
 // a / b and a % b; 64-bit division only where it is needed
@@ -228,9 +228,14 @@ __device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
 
 template <int D, bool FP8>
 struct AttnCfg {
+  // Keys of a warp in a tile: 32 while rows are at most 128 bytes.  The work around the products (maximum, waits, table look-ups) is per
+  // group of keys and the products of two groups of 16 overlap: an 8-bit cache with head_dim 128 reads 5.3 TB/s instead of 3.8.
+  static constexpr int kKeys = D * (FP8 ? 1 : 2) <= 128 ? 32 : 16;
+  static constexpr int kTileKeys = kAttnWarps * kKeys;
+  static constexpr int kGroups = kKeys / 16, kST = 2 * kGroups;       // products of 16 keys, score fragments of 8 keys
   static constexpr int kRowBytes = D * (FP8 ? 1 : 2);
   static constexpr int kChunks = kRowBytes / 16;                      // 16-byte chunks of a cache row
-  static constexpr int kTileBytes = kAttnWarpKeys * kRowBytes;        // K or V of a warp's 16 keys
+  static constexpr int kTileBytes = kKeys * kRowBytes;                // K or V of a warp's keys of a tile
   static constexpr int kStageBytes = 2 * kTileBytes;
   static constexpr int kWant = 96 * 1024 / (kAttnWarps * kStageBytes);
   static constexpr int kStages = kWant < 3 ? 3 : kWant > 8 ? 8 : kWant;
@@ -260,6 +265,7 @@ template <int D, bool FP8>
 __global__ void __launch_bounds__(kAttnThreads, AttnCfg<D, FP8>::kCtasPerSm) attend_rows_kernel(const AttendParams p) {
   using C = AttnCfg<D, FP8>;
   constexpr int kSteps = D / 16, kNT = D / 8;
+  constexpr uint32_t kAllKeys = C::kKeys == 32 ? 0xffffffffu : (1u << (C::kKeys & 31)) - 1u;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ int64_t s_warp[32], s_found[2];
   __shared__ float s_m[kAttnWarps][kAttnRows], s_l[kAttnWarps][kAttnRows];
@@ -289,7 +295,7 @@ __global__ void __launch_bounds__(kAttnThreads, AttnCfg<D, FP8>::kCtasPerSm) att
 
   while (r >= 0 && off < off_end) {
     // ---- the unit that tile `off` belongs to
-    const int tiles = attn_tiles(rq), n_rt = (rq.rows + kAttnRows - 1) / kAttnRows;
+    const int tiles = attn_tiles(p, rq), n_rt = (rq.rows + kAttnRows - 1) / kAttnRows;
     int64_t rem;
     const int64_t u = attn_div(off - req_start, tiles, &rem);  // row tile fastest, so that the row tiles of a K/V head follow one another
     const int t0 = (int)rem;
@@ -312,7 +318,7 @@ __global__ void __launch_bounds__(kAttnThreads, AttnCfg<D, FP8>::kCtasPerSm) att
     const int pos0 = rq.len - rq.n;  // position of the request's first new token
     const int last_pos = pos0 + tok0 + group_div(p, sub0 + rows - 1);
     const int key_end = min(rq.keys, last_pos + 1);  // keys that any row of the unit may see
-    const int n_it = min(t1, (key_end + kAttnTileKeys - 1) / kAttnTileKeys) - t0;  // <= 0: nothing to read
+    const int n_it = min(t1, (key_end + C::kTileKeys - 1) / C::kTileKeys) - t0;  // <= 0: nothing to read
     // last key of this thread's two rows (rows behind the unit's last follow the last one)
     const int lim0 = pos0 + tok0 + group_div(p, sub0 + min(g, rows - 1)), lim1 = pos0 + tok0 + group_div(p, sub0 + min(g + 8, rows - 1));
     const int lim_min = pos0 + tok0;
@@ -321,7 +327,7 @@ __global__ void __launch_bounds__(kAttnThreads, AttnCfg<D, FP8>::kCtasPerSm) att
     const uint8_t* kh = p.k_cache + kvh * p.head_stride;
     const uint8_t* vh = p.v_cache + kvh * p.head_stride;
     // lane's key of iteration i, and its table entry (fetched one iteration before it is needed)
-    auto key_of = [&](int i) { return (t0 + i) * kAttnTileKeys + warp * kAttnWarpKeys + (lane & 15); };
+    auto key_of = [&](int i) { return (t0 + i) * C::kTileKeys + warp * C::kKeys + (lane & (C::kKeys - 1)); };
     auto entry_of = [&](int i) {
       const int key = key_of(i);
       return i < n_it && key < key_end ? __ldg(table + attn_page(p, key)) : -1;
@@ -331,17 +337,17 @@ __global__ void __launch_bounds__(kAttnThreads, AttnCfg<D, FP8>::kCtasPerSm) att
         const int key = key_of(i);
         const bool live = blk >= 0 && blk < p.num_blocks;
         const int64_t at = live ? blk * p.block_stride + attn_in_page(p, key) * p.token_stride : 0;
-        const uint32_t mask = __ballot_sync(0xffffffffu, live) & 0xffffu;
+        const uint32_t mask = __ballot_sync(0xffffffffu, live) & kAllKeys;
         const int st = i % C::kStages;
         if (lane == 0) s_mask[warp][st] = mask;
         const uint32_t dst = ring_u + st * C::kStageBytes;
-        constexpr int kPer = kAttnWarpKeys * C::kChunks / 32 > 0 ? kAttnWarpKeys * C::kChunks / 32 : 1;
+        constexpr int kPer = C::kKeys * C::kChunks / 32 > 0 ? C::kKeys * C::kChunks / 32 : 1;
 #pragma unroll
         for (int j = 0; j < kPer; ++j) {
-          const int idx = j * 32 + lane, row = (idx / C::kChunks) & 15, ch = idx % C::kChunks;
+          const int idx = j * 32 + lane, row = (idx / C::kChunks) & (C::kKeys - 1), ch = idx % C::kChunks;
           const int64_t ro = __shfl_sync(0xffffffffu, at, row);
           const bool ok = (mask >> row) & 1u;
-          if (kAttnWarpKeys * C::kChunks >= 32 || idx < kAttnWarpKeys * C::kChunks) {
+          if (C::kKeys * C::kChunks >= 32 || idx < C::kKeys * C::kChunks) {
             cp_async16(dst + attn_swz<C::kChunks, FP8, false>(row, ch), kh + ro + ch * 16, ok);
             cp_async16(dst + C::kTileBytes + attn_swz<C::kChunks, FP8, true>(row, ch), vh + ro + ch * 16, ok);
           }
@@ -418,30 +424,33 @@ __global__ void __launch_bounds__(kAttnThreads, AttnCfg<D, FP8>::kCtasPerSm) att
         issue(i + C::kStages - 1, blk);
       }
       const int st = i % C::kStages;
-      const int k0 = (t0 + i) * kAttnTileKeys + warp * kAttnWarpKeys;
+      const int k0 = (t0 + i) * C::kTileKeys + warp * C::kKeys;
       const uint32_t mask = s_mask[warp][st];
       if (k0 >= key_end) continue;  // (uniform in the warp)
       const uint32_t kt = ring_u + st * C::kStageBytes, vt = kt + C::kTileBytes;
 
-      // ---- scores of 16 keys
-      float s[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+      // ---- scores of the warp's keys
+      float s[C::kST][4];
+#pragma unroll
+      for (int nt = 0; nt < C::kST; ++nt) s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
       if constexpr (!FP8) {
         const int kr = (lane & 7) + ((lane >> 4) << 3), kc = (lane >> 3) & 1;
 #pragma unroll
-        for (int k = 0; k < kSteps; ++k) {
-          uint32_t b[4];
-          ldsm4(kt + attn_swz<C::kChunks, false, false>(kr, 2 * k + kc), b);
-          mma16816<false>(s[0], qf[k], b[0], b[1]);
-          mma16816<false>(s[1], qf[k], b[2], b[3]);
-        }
+        for (int k = 0; k < kSteps; ++k)
+#pragma unroll
+          for (int gr = 0; gr < C::kGroups; ++gr) {
+            uint32_t b[4];
+            ldsm4(kt + attn_swz<C::kChunks, false, false>(gr * 16 + kr, 2 * k + kc), b);
+            mma16816<false>(s[2 * gr], qf[k], b[0], b[1]);
+            mma16816<false>(s[2 * gr + 1], qf[k], b[2], b[3]);
+          }
       } else {
         const uint8_t* kp = ring + st * C::kStageBytes;
 #pragma unroll
-        for (int nt = 0; nt < 2; ++nt) {
-          const int row = nt * 8 + g;
+        for (int kb = 0; kb < kSteps / C::kSPB; ++kb)
 #pragma unroll
-          for (int kb = 0; kb < kSteps / C::kSPB; ++kb) {
-            const int byte = kb * 64 + C::kKB * t4;
+          for (int nt = 0; nt < C::kST; ++nt) {
+            const int row = nt * 8 + g, byte = kb * 64 + C::kKB * t4;
             const uint8_t* src = kp + attn_swz<C::kChunks, true, false>(row, byte >> 4) + (byte & 15);
             uint32_t w[4];
             if constexpr (C::kKB == 16) {
@@ -460,13 +469,12 @@ __global__ void __launch_bounds__(kAttnThreads, AttnCfg<D, FP8>::kCtasPerSm) att
               mma16816<true>(s[nt], qf[kb * C::kSPB + q], b0, b1);
             }
           }
-        }
       }
       // ---- mask, running maximum and sum
-      const bool causal = k0 + kAttnWarpKeys - 1 > lim_min;  // some row ends inside or before this group
-      if (causal || mask != 0xffffu) {
+      const bool causal = k0 + C::kKeys - 1 > lim_min;  // some row ends inside or before these keys
+      if (causal || mask != kAllKeys) {
 #pragma unroll
-        for (int nt = 0; nt < 2; ++nt)
+        for (int nt = 0; nt < C::kST; ++nt)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
             const int c = nt * 8 + 2 * t4 + e;
@@ -475,7 +483,12 @@ __global__ void __launch_bounds__(kAttnThreads, AttnCfg<D, FP8>::kCtasPerSm) att
             if (!there || k0 + c > lim1) s[nt][2 + e] = -INFINITY;
           }
       }
-      float x0 = fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[1][0], s[1][1])), x1 = fmaxf(fmaxf(s[0][2], s[0][3]), fmaxf(s[1][2], s[1][3]));
+      float x0 = -INFINITY, x1 = -INFINITY;
+#pragma unroll
+      for (int nt = 0; nt < C::kST; ++nt) {
+        x0 = fmaxf(x0, fmaxf(s[nt][0], s[nt][1]));
+        x1 = fmaxf(x1, fmaxf(s[nt][2], s[nt][3]));
+      }
       x0 = fmaxf(x0, __shfl_xor_sync(0xffffffffu, x0, 1));
       x1 = fmaxf(x1, __shfl_xor_sync(0xffffffffu, x1, 1));
       x0 = fmaxf(x0, __shfl_xor_sync(0xffffffffu, x0, 2));
@@ -497,19 +510,19 @@ __global__ void __launch_bounds__(kAttnThreads, AttnCfg<D, FP8>::kCtasPerSm) att
         m1 = n1;
       }
       const float b0 = m0 == -INFINITY ? 0.f : m0, b1 = m1 == -INFINITY ? 0.f : m1;
-      float w[2][4];
 #pragma unroll
-      for (int nt = 0; nt < 2; ++nt)
+      for (int nt = 0; nt < C::kST; ++nt) {  // the scores become weights
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          w[nt][e] = ex2(fmaf(s[nt][e], sc0, -b0));
-          w[nt][2 + e] = ex2(fmaf(s[nt][2 + e], sc1, -b1));
+          s[nt][e] = ex2(fmaf(s[nt][e], sc0, -b0));
+          s[nt][2 + e] = ex2(fmaf(s[nt][2 + e], sc1, -b1));
         }
-      l0 += (w[0][0] + w[0][1]) + (w[1][0] + w[1][1]);
-      l1 += (w[0][2] + w[0][3]) + (w[1][2] + w[1][3]);
+        l0 += s[nt][0] + s[nt][1];
+        l1 += s[nt][2] + s[nt][3];
+      }
 
-      // ---- a value that is not finite at a key that some row must not see would reach that row as 0 * inf: such groups
-      // (only the last ones of a chunk can be) are summed key by key
+      // ---- a value that is not finite at a key that some row must not see would reach that row as 0 * inf: such keys (only a chunk's
+      // last ones can be) are summed one by one
       bool by_key = false;
       if (causal) {
         const uint4* vp = reinterpret_cast<const uint4*>(ring + st * C::kStageBytes + C::kTileBytes);
@@ -529,72 +542,79 @@ __global__ void __launch_bounds__(kAttnThreads, AttnCfg<D, FP8>::kCtasPerSm) att
       }
       if (by_key) {
         const uint8_t* vp = ring + st * C::kStageBytes + C::kTileBytes;
-#pragma unroll 1
-        for (int c = 0; c < kAttnWarpKeys; ++c) {
-          const int from = (lane & 28) | ((c & 7) >> 1);
-          const float e0 = __shfl_sync(0xffffffffu, c & 8 ? w[1][0] : w[0][0], from), e1 = __shfl_sync(0xffffffffu, c & 8 ? w[1][1] : w[0][1], from);
-          const float e2 = __shfl_sync(0xffffffffu, c & 8 ? w[1][2] : w[0][2], from), e3 = __shfl_sync(0xffffffffu, c & 8 ? w[1][3] : w[0][3], from);
-          const float w0 = c & 1 ? e1 : e0, w1 = c & 1 ? e3 : e2;
-          const bool there = (mask >> c) & 1u, see0 = there && k0 + c <= lim0, see1 = there && k0 + c <= lim1;
 #pragma unroll
-          for (int n = 0; n < kNT; ++n) {
-            float v0, v1;
-            if constexpr (!FP8) {
-              const int d = 8 * n + 2 * t4;
-              const uint32_t x = *reinterpret_cast<const uint32_t*>(vp + attn_swz<C::kChunks, false, true>(c, d >> 3) + (d & 7) * 2);
-              v0 = bf16lo(x), v1 = bf16hi(x);
-            } else {
-              constexpr int kVB = D >= 32 ? 4 : D / 8;
-              const int d = (n / kVB) * (8 * kVB) + 2 * t4 * kVB + n % kVB;
-              const uint32_t x0b = vp[attn_swz<C::kChunks, true, true>(c, d >> 4) + (d & 15)];
-              const uint32_t x1b = vp[attn_swz<C::kChunks, true, true>(c, (d + kVB) >> 4) + ((d + kVB) & 15)];
-              uint32_t h, unused;
-              e4m3x4_half2(x0b | (x1b << 8), h, unused);
-              const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
-              v0 = f.x, v1 = f.y;
+        for (int nt = 0; nt < C::kST; ++nt)
+#pragma unroll 1
+          for (int c8 = 0; c8 < 8; ++c8) {
+            const int c = nt * 8 + c8, from = (lane & 28) | (c8 >> 1);
+            const float e0 = __shfl_sync(0xffffffffu, s[nt][0], from), e1 = __shfl_sync(0xffffffffu, s[nt][1], from);
+            const float e2 = __shfl_sync(0xffffffffu, s[nt][2], from), e3 = __shfl_sync(0xffffffffu, s[nt][3], from);
+            const float w0 = c & 1 ? e1 : e0, w1 = c & 1 ? e3 : e2;
+            const bool there = (mask >> c) & 1u, see0 = there && k0 + c <= lim0, see1 = there && k0 + c <= lim1;
+#pragma unroll
+            for (int n = 0; n < kNT; ++n) {
+              float v0, v1;
+              if constexpr (!FP8) {
+                const int d = 8 * n + 2 * t4;
+                const uint32_t x = *reinterpret_cast<const uint32_t*>(vp + attn_swz<C::kChunks, false, true>(c, d >> 3) + (d & 7) * 2);
+                v0 = bf16lo(x), v1 = bf16hi(x);
+              } else {
+                constexpr int kVB = D >= 32 ? 4 : D / 8;
+                const int d = (n / kVB) * (8 * kVB) + 2 * t4 * kVB + n % kVB;
+                const uint32_t x0b = vp[attn_swz<C::kChunks, true, true>(c, d >> 4) + (d & 15)];
+                const uint32_t x1b = vp[attn_swz<C::kChunks, true, true>(c, (d + kVB) >> 4) + ((d + kVB) & 15)];
+                uint32_t h, unused;
+                e4m3x4_half2(x0b | (x1b << 8), h, unused);
+                const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
+                v0 = f.x, v1 = f.y;
+              }
+              if (see0) o[n][0] = fmaf(w0, v0, o[n][0]), o[n][1] = fmaf(w0, v1, o[n][1]);
+              if (see1) o[n][2] = fmaf(w1, v0, o[n][2]), o[n][3] = fmaf(w1, v1, o[n][3]);
             }
-            if (see0) o[n][0] = fmaf(w0, v0, o[n][0]), o[n][1] = fmaf(w0, v1, o[n][1]);
-            if (see1) o[n][2] = fmaf(w1, v0, o[n][2]), o[n][3] = fmaf(w1, v1, o[n][3]);
           }
-        }
         continue;
       }
 
       // ---- O += P V (P rounded to the type of V)
-      if constexpr (!FP8) {
-        const uint32_t pa[4] = {pack_bf16(w[0][0], w[0][1]), pack_bf16(w[0][2], w[0][3]), pack_bf16(w[1][0], w[1][1]), pack_bf16(w[1][2], w[1][3])};
-        const int vr = lane & 15, vc = lane >> 4;
 #pragma unroll
-        for (int n = 0; n < kNT; n += 2) {
-          uint32_t b[4];
-          ldsm4t(vt + attn_swz<C::kChunks, false, true>(vr, n + vc), b);
-          mma16816<false>(o[n], pa, b[0], b[1]);
-          mma16816<false>(o[n + 1], pa, b[2], b[3]);
-        }
-      } else {
-        const uint32_t pa[4] = {pack_half(w[0][0], w[0][1]), pack_half(w[0][2], w[0][3]), pack_half(w[1][0], w[1][1]), pack_half(w[1][2], w[1][3])};
-        const uint8_t* vp = ring + st * C::kStageBytes + C::kTileBytes;
-        // a thread takes kVB neighbouring elements of four key rows: column c of product n holds element (n / kVB) * 8 kVB + c kVB + n % kVB
-        constexpr int kVB = D >= 32 ? 4 : D / 8;
+      for (int gr = 0; gr < C::kGroups; ++gr) {
+        const float* wa = s[2 * gr];
+        const float* wb = s[2 * gr + 1];
+        if constexpr (!FP8) {
+          const uint32_t pa[4] = {pack_bf16(wa[0], wa[1]), pack_bf16(wa[2], wa[3]), pack_bf16(wb[0], wb[1]), pack_bf16(wb[2], wb[3])};
+          const int vr = gr * 16 + (lane & 15), vc = lane >> 4;
 #pragma unroll
-        for (int jj = 0; jj < kNT / kVB; ++jj) {
-          const int d = jj * 8 * kVB + g * kVB;
-          uint32_t x[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int row = 2 * t4 + (e & 1) + (e >> 1) * 8;
-            const uint8_t* src = vp + attn_swz<C::kChunks, true, true>(row, d >> 4) + (d & 15);
-            if constexpr (kVB == 4) x[e] = *reinterpret_cast<const uint32_t*>(src);
-            else x[e] = *reinterpret_cast<const uint16_t*>(src);
+          for (int n = 0; n < kNT; n += 2) {
+            uint32_t b[4];
+            ldsm4t(vt + attn_swz<C::kChunks, false, true>(vr, n + vc), b);
+            mma16816<false>(o[n], pa, b[0], b[1]);
+            mma16816<false>(o[n + 1], pa, b[2], b[3]);
           }
+        } else {
+          const uint32_t pa[4] = {pack_half(wa[0], wa[1]), pack_half(wa[2], wa[3]), pack_half(wb[0], wb[1]), pack_half(wb[2], wb[3])};
+          const uint8_t* vp = ring + st * C::kStageBytes + C::kTileBytes;
+          // a thread takes kVB neighbouring elements of four key rows: column c of product n holds element (n / kVB) * 8 kVB + c kVB + n % kVB
+          constexpr int kVB = D >= 32 ? 4 : D / 8;
 #pragma unroll
-          for (int h = 0; h < kVB / 2; ++h) {  // bytes 2h, 2h + 1 of the rows, paired by key
-            const uint32_t lo = __byte_perm(x[0], x[1], h ? 0x7362 : 0x5140), hi = __byte_perm(x[2], x[3], h ? 0x7362 : 0x5140);
-            uint32_t l0h, l1h, h0h, h1h;
-            e4m3x4_half2(lo, l0h, l1h);
-            e4m3x4_half2(hi, h0h, h1h);
-            mma16816<true>(o[jj * kVB + 2 * h], pa, l0h, h0h);
-            mma16816<true>(o[jj * kVB + 2 * h + 1], pa, l1h, h1h);
+          for (int jj = 0; jj < kNT / kVB; ++jj) {
+            const int d = jj * 8 * kVB + g * kVB;
+            uint32_t x[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int row = gr * 16 + 2 * t4 + (e & 1) + (e >> 1) * 8;
+              const uint8_t* src = vp + attn_swz<C::kChunks, true, true>(row, d >> 4) + (d & 15);
+              if constexpr (kVB == 4) x[e] = *reinterpret_cast<const uint32_t*>(src);
+              else x[e] = *reinterpret_cast<const uint16_t*>(src);
+            }
+#pragma unroll
+            for (int h = 0; h < kVB / 2; ++h) {  // bytes 2h, 2h + 1 of the rows, paired by key
+              const uint32_t lo = __byte_perm(x[0], x[1], h ? 0x7362 : 0x5140), hi = __byte_perm(x[2], x[3], h ? 0x7362 : 0x5140);
+              uint32_t l0h, l1h, h0h, h1h;
+              e4m3x4_half2(lo, l0h, l1h);
+              e4m3x4_half2(hi, h0h, h1h);
+              mma16816<true>(o[jj * kVB + 2 * h], pa, l0h, h0h);
+              mma16816<true>(o[jj * kVB + 2 * h + 1], pa, l1h, h1h);
+            }
           }
         }
       }

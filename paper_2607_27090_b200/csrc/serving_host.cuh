@@ -241,6 +241,7 @@ static ms_status attend_launch(memstore* s, ChunkParams& c, int64_t max_rows, cu
   c.min_rows = rows ? kChunkMinRows : 0;
   p.max_rows = chunks ? c.min_rows : 0x7fffffff;
   p.beside = chunks;
+  p.tile_shift = __builtin_ctz((unsigned)AttnCfg<D, FP8>::kTileKeys);
   int chunk_ctas = 0, rows_ctas = 0;
   if constexpr (D == 64 || D == 128) {
     if (chunks) {
