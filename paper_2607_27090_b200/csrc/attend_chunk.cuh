@@ -11,7 +11,7 @@
 //   warps 0-7, 8-15  queries (scaled to fp16 for an 8-bit cache), weights and epilogue of rows 0-127, 128-255: two threads share a row,
 //                    64 of the tile's keys each (16 warps: a single warp per scheduler cannot keep the exponentials' unit busy)
 //   warps 16-19      loads: K and V tiles of 128 keys through a ring of 5 buffers, gathered through the block table with cp.async
-//                    (8-bit: loaded, converted to fp16 exactly, stored)
+//                    (8-bit: the codes go to a place of the loading thread's own, a tile ahead, and are converted to fp16, exactly, from there)
 //   warp 20          TMEM allocation, tcgen05.mma issue by one elected lane
 //   warp 21          walks the CTA's share of the line and describes its units to the other roles (warps 22, 23 complete the warpgroup)
 // Work split: as in attend.cuh, the tiles of all units (causal: only as many as a unit's last row sees) form one line of which every
@@ -36,12 +36,14 @@ constexpr int kChunkMaskRing = 8;     // (a tile's masks are read at most three 
 constexpr uint32_t kChunkSpinLimit = 1u << 26;  // polls (a second or more)
 constexpr float kChunkMaxSum = 16384.f;  // sum of 64 weights (and so a weight) that is tolerated without taking a new maximum
 
-template <int D>
+template <int D, bool FP8>
 struct ChunkCfg {
+  static constexpr int kStages = FP8 ? 4 : kChunkStages;             // an 8-bit cache gives one tile's place to codes on their way
   static constexpr int kHalves = D / 64;                             // 128-byte column blocks of a 16-bit row
   static constexpr int kTileBytes = kChunkKeys * D * 2;              // K or V tile, 16 bits per element
   static constexpr int kQBytes = kChunkRows * D * 2;
-  static constexpr int kRingBytes = kChunkStages * kTileBytes;
+  static constexpr int kRawBytes = FP8 ? kTileBytes : 0;             // two tiles of codes
+  static constexpr int kRingBytes = kStages * kTileBytes + kRawBytes;
   static constexpr int kSmemBytes = 1024 + kQBytes + kRingBytes + 2048;  // alignment, tiles, barriers and small arrays
   static_assert(kSmemBytes <= 232448, "shared memory of a CTA");
   static constexpr int kColO = 2 * kChunkKeys;                       // TMEM: S0, S1 (128 columns each), O0, O1 (D columns each)
@@ -269,7 +271,7 @@ struct ChunkNo {
 
 template <int D, bool FP8>
 __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const ChunkParams c) {
-  using C = ChunkCfg<D>;
+  using C = ChunkCfg<D, FP8>;
   const AttendParams& p = c.a;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
@@ -298,7 +300,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
-    for (int s = 0; s < kChunkStages; ++s) {
+    for (int s = 0; s < C::kStages; ++s) {
       mbar_init(&kv_full[s], 4);
       mbar_init(&kv_empty[s], 1);
     }
@@ -362,8 +364,22 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
       fence_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(&kv_full[pub]);
-      if (++pub == kChunkStages) pub = 0;
+      if (++pub == C::kStages) pub = 0;
       --unpublished;
+    };
+    // 8-bit cache: this thread's 16-byte pieces of its warp's 32 rows, into a place that only it reads
+    constexpr int kLoads = 32 * D / 512;
+    uint8_t* raw = ring + C::kStages * C::kTileBytes + lt * 16;
+    int raw_in = 0, raw_out = 0;
+    auto raw_issue = [&](const uint8_t* base, int64_t at, uint32_t mask) {
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        const int idx = i * 32 + lane, rl = idx / (D / 16), ch = idx % (D / 16);
+        const int64_t ro = __shfl_sync(0xffffffffu, at, rl);
+        cp_async16(smem_u32(raw + (raw_in * kLoads + i) * 2048), base + ro + ch * 16, (mask >> rl) & 1u);
+      }
+      cp_async_commit();
+      raw_in ^= 1;
     };
     for (int n = 0; ok; ++n) {
       ok = unit_ready(n);
@@ -372,6 +388,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
       __syncwarp();
       if (u.nt < 0) break;
       unit_done(n);
+      if (u.nt == 0) continue;
       const int t_end = u.t0 + u.nt;
       // ---- tiles: K, V, K, V ...; a thread looks up key lt of the tile, a warp copies its own 32 keys
       const int32_t* table = p.tables + (int64_t)u.req * p.max_blocks;
@@ -379,18 +396,36 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
         const int key = t * kChunkKeys + lt;
         return key < u.key_end ? __ldg(table + attn_page(p, key)) : -1;
       };
-      int32_t nxt = entry_of(u.t0);
-      for (int t = u.t0; ok && t < t_end; ++t) {
-        const int32_t blk = nxt;
-        if (t + 1 < t_end) nxt = entry_of(t + 1);
-        const int key = t * kChunkKeys + lt;
+      // where the row of this thread's key starts (bytes from the base of K or V), and which of the warp's keys there are
+      auto row_of = [&](int32_t blk, int t, uint32_t* there) -> int64_t {
         const bool live = blk >= 0 && blk < p.num_blocks;
-        const int64_t at = live ? blk * p.block_stride + attn_in_page(p, key) * p.token_stride + u.kvh * p.head_stride : 0;
-        const uint32_t mask = __ballot_sync(0xffffffffu, live);
+        *there = __ballot_sync(0xffffffffu, live);
+        return live ? blk * p.block_stride + attn_in_page(p, t * kChunkKeys + lt) * p.token_stride + u.kvh * p.head_stride : 0;
+      };
+      uint32_t mask;
+      int64_t at = row_of(entry_of(u.t0), u.t0, &mask);
+      int32_t nxt = u.t0 + 1 < t_end ? entry_of(u.t0 + 1) : -1;
+      if constexpr (FP8) raw_issue(p.k_cache, at, mask);
+      for (int t = u.t0; ok && t < t_end; ++t) {
+        uint32_t next_mask = 0u;
+        int64_t next_at = 0;
+        if (t + 1 < t_end) {
+          next_at = row_of(nxt, t + 1, &next_mask);
+          nxt = t + 2 < t_end ? entry_of(t + 2) : -1;
+        }
         const bool causal = t * kChunkKeys + kChunkKeys - 1 > u.lim_min;
         if (lane == 0) s_masks[mask_at * 4 + w] = mask;
         bool bad = false;
         for (int kv = 0; kv < 2; ++kv) {
+          if constexpr (FP8) {  // the next tile's codes, then wait for this one's
+            if (kv == 0)
+              raw_issue(p.v_cache, at, mask);
+            else if (t + 1 < t_end)
+              raw_issue(p.k_cache, next_at, next_mask);
+            else
+              cp_async_commit();
+            cp_async_wait<1>();
+          }
           ok = chunk_wait(&kv_empty[stage], ph, abort_flag, limit);
           if (!ok) break;
           uint8_t* dst = ring + stage * C::kTileBytes;
@@ -406,18 +441,11 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
               for (int b = 0; b < C::kHalves; ++b) cp_async16(du + b * 16384 + chunk_swz(row, ch), base + ro + b * 128 + ch * 16, there);
             }
           } else {
-            constexpr int kLoads = 32 * D / 512;  // 16-byte loads per lane: the warp's 32 rows of D bytes
-            uint4 x[kLoads];
-#pragma unroll
-            for (int i = 0; i < kLoads; ++i) {
-              const int idx = i * 32 + lane, rl = idx / (D / 16), ch = idx % (D / 16);
-              const int64_t ro = __shfl_sync(0xffffffffu, at, rl);
-              x[i] = ((mask >> rl) & 1u) ? *reinterpret_cast<const uint4*>(base + ro + ch * 16) : make_uint4(0u, 0u, 0u, 0u);
-            }
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
               const int idx = i * 32 + lane, row = w * 32 + idx / (D / 16), ch = idx % (D / 16);
-              uint32_t y[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+              const uint4 x = *reinterpret_cast<const uint4*>(raw + (raw_out * kLoads + i) * 2048);
+              uint32_t y[4] = {x.x, x.y, x.z, x.w};
               if (kv && causal) {  // NaN codes become zeros here; the epilogue adds them to the rows that see them
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
@@ -435,6 +463,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
               *reinterpret_cast<uint4*>(d + chunk_swz(row, 2 * (ch & 3))) = lo;
               *reinterpret_cast<uint4*>(d + chunk_swz(row, 2 * (ch & 3) + 1)) = hi;
             }
+            raw_out ^= 1;
           }
           if (!FP8) cp_async_commit();
           ++unpublished;
@@ -474,12 +503,14 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
             cp_async_wait<1>();
             publish();
           }
-          if (++stage == kChunkStages) {
+          if (++stage == C::kStages) {
             stage = 0;
             ph ^= 1u;
           }
         }
         if (++mask_at == kChunkMaskRing) mask_at = 0;
+        at = next_at;
+        mask = next_mask;
       }
     }
     cp_async_wait<0>();
@@ -593,13 +624,13 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
           if (!ok) break;
           if (j < nt) {
             umma_commit_if(lead, &kv_empty[k_stage]);
-            if (++stage == kChunkStages) {
+            if (++stage == C::kStages) {
               stage = 0;
               ph ^= 1u;
             }
             v_stage = stage;
             v_ph = ph;
-            if (++stage == kChunkStages) {
+            if (++stage == C::kStages) {
               stage = 0;
               ph ^= 1u;
             }

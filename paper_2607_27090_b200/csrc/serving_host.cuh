@@ -224,7 +224,7 @@ static cudaError_t attend_prepare(int device) {
   if (done[device & 63]) return cudaSuccess;
   cudaError_t e = cudaFuncSetAttribute(attend_rows_kernel<D, FP8>, cudaFuncAttributeMaxDynamicSharedMemorySize, AttnCfg<D, FP8>::kSmemBytes);
   if constexpr (D == 64 || D == 128)
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(attend_chunk_kernel<D, FP8>, cudaFuncAttributeMaxDynamicSharedMemorySize, ChunkCfg<D>::kSmemBytes);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(attend_chunk_kernel<D, FP8>, cudaFuncAttributeMaxDynamicSharedMemorySize, (ChunkCfg<D, FP8>::kSmemBytes));
   if (e == cudaSuccess) done[device & 63] = true;
   return e;
 }
@@ -246,7 +246,7 @@ static ms_status attend_launch(memstore* s, ChunkParams& c, int64_t max_rows, cu
   if constexpr (D == 64 || D == 128) {
     if (chunks) {
       chunk_ctas = s->sm_count;
-      MS_CUDA(s, launch_dependent(attend_chunk_kernel<D, FP8>, dim3((unsigned)chunk_ctas), dim3(kChunkThreads), ChunkCfg<D>::kSmemBytes, st, c));
+      MS_CUDA(s, launch_dependent(attend_chunk_kernel<D, FP8>, dim3((unsigned)chunk_ctas), dim3(kChunkThreads), (ChunkCfg<D, FP8>::kSmemBytes), st, c));
       s->kernels_launched++;
     }
   }
