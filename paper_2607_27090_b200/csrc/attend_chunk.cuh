@@ -15,7 +15,8 @@
 //   warp 20          TMEM allocation, tcgen05.mma issue by one elected lane
 //   warp 21          walks the CTA's share of the line and describes its units to the other roles (warps 22, 23 complete the warpgroup)
 // Work split: as in attend.cuh, the tiles of all units (causal: only as many as a unit's last row sees) form one line of which every
-// CTA takes an equal share, so 64 units on 148 SMs balance as well as 6400.
+// CTA takes an equal share, so 64 units on 148 SMs balance as well as 6400.  Starting and ending a unit costs about as much as three of
+// its tiles; where there are more units than CTAs each unit takes three places on the line for that (else a CTA has one piece anyway).
 // Running maximum: the weights are formed with the maximum of the tiles before; no maximum is looked for unless the sum of a thread's 64
 // weights passes 2^14, when the row takes a new maximum, its weights are formed again and its accumulator is rescaled.  fp32 sums, and
 // weights of up to 2^14 in bf16 or fp16, lose nothing by that.
@@ -54,6 +55,8 @@ struct ChunkParams {
   AttendParams a;
   int32_t min_rows;   // requests with more rows than this are served here
   int32_t min_share;
+  int32_t step_tok, step_sub;  // kChunkRows / group and kChunkRows % group
+  int32_t unit_cost;  // places of the line that stand for a unit's set-up
   float* part_o;      // [CTAs][2][D / 4][kChunkRows][4]
   float2* part_ml;    // [CTAs][2][kChunkRows]
   AttnCut* cuts;      // [CTAs]
@@ -62,21 +65,34 @@ struct ChunkParams {
   int mute_producer;
 };
 
+// The row tiles of a request one after another: token and query head of the group of the tile's first row.
+struct ChunkWalk {
+  int tok = 0, sub = 0;
+  __device__ __forceinline__ void step(const ChunkParams& c) {
+    tok += c.step_tok;
+    sub += c.step_sub;
+    if (sub >= c.a.group) {
+      sub -= c.a.group;
+      ++tok;
+    }
+  }
+};
 // Tiles of a unit: up to the last key that its last row sees (one at least: rows without keys are written too).
-__device__ __forceinline__ int chunk_tiles(const AttendParams& p, const AttnReq& q, int rt) {
-  const int last_row = min((rt + 1) * kChunkRows, q.rows) - 1;
-  const int end = min(q.keys, q.len - q.n + last_row / p.group + 1);
-  return max(1, (end + kChunkKeys - 1) / kChunkKeys);
+__device__ __forceinline__ int chunk_tiles(const AttendParams& p, const AttnReq& q, const ChunkWalk& w) {
+  const int last = min(q.n - 1, w.tok + group_div(p, w.sub + kChunkRows - 1));
+  return max(1, (min(q.keys, q.len - q.n + last + 1) + kChunkKeys - 1) / kChunkKeys);
 }
 __device__ __forceinline__ int chunk_row_tiles(const AttnReq& q) { return (q.rows + kChunkRows - 1) / kChunkRows; }
-__device__ __forceinline__ int64_t chunk_head_tiles(const AttendParams& p, const AttnReq& q) {
+__device__ __forceinline__ int64_t chunk_head_cost(const ChunkParams& c, const AttnReq& q) {
   int64_t s = 0;
-  for (int rt = 0; rt < chunk_row_tiles(q); ++rt) s += chunk_tiles(p, q, rt);
+  ChunkWalk w;
+  const int n = chunk_row_tiles(q);
+  for (int rt = 0; rt < n; ++rt, w.step(c)) s += chunk_tiles(c.a, q, w) + c.unit_cost;
   return s;
 }
 __device__ __forceinline__ int64_t chunk_cost(const ChunkParams& c, const AttnReq& q) {
   if (q.n == 0 || q.rows <= c.min_rows) return 0;
-  return chunk_head_tiles(c.a, q) * c.a.n_kv;
+  return chunk_head_cost(c, q) * c.a.n_kv;
 }
 
 // What the roles need to know of a unit, in a small ring of shared memory: worked out once, ahead of its use.
@@ -93,13 +109,14 @@ struct __align__(16) ChunkUnit {
   int32_t whole;            // all tiles of the unit are here
 };
 
-// A piece of a unit that one CTA works on: tiles t0 .. t1 - 1 of it.
+// A unit, and the place on it where a CTA's share begins (the first unit_cost places stand for its set-up, then come its tiles).
 struct ChunkSeg {
-  int r, kvh, rt, t0, t1, tiles;
+  int r, kvh, rt, tiles, pos;
+  ChunkWalk w;
   AttnReq q;
 };
 
-// The unit that tile `off` of the line lies in, by the whole block; false when off lies behind the line.
+// The unit that place `off` of the line lies in; false when off lies behind the line.
 template <int THREADS>
 __device__ __forceinline__ bool chunk_locate(const ChunkParams& c, const AttnLine<THREADS>& line, int64_t off, int64_t* s_warp, int64_t* s_found,
                                              ChunkSeg* seg) {
@@ -107,22 +124,26 @@ __device__ __forceinline__ bool chunk_locate(const ChunkParams& c, const AttnLin
   seg->r = line.locate(c.a.nreq, [&](int i) { return chunk_cost(c, attn_request(c.a, i)); }, off, s_warp, s_found, &start);
   if (seg->r < 0) return false;
   seg->q = attn_request(c.a, seg->r);
-  seg->kvh = (int)attn_div(off - start, chunk_head_tiles(c.a, seg->q), &rem);
+  seg->kvh = (int)attn_div(off - start, chunk_head_cost(c, seg->q), &rem);
   seg->rt = 0;
+  seg->w = ChunkWalk();
   for (;;) {
-    seg->tiles = chunk_tiles(c.a, seg->q, seg->rt);
-    if (rem < seg->tiles) break;
-    rem -= seg->tiles;
+    seg->tiles = chunk_tiles(c.a, seg->q, seg->w);
+    if (rem < seg->tiles + c.unit_cost) break;
+    rem -= seg->tiles + c.unit_cost;
     ++seg->rt;
+    seg->w.step(c);
   }
-  seg->t0 = (int)rem;
+  seg->pos = (int)rem;
   return true;
 }
-// The unit after seg (t0 = 0); false behind the last request.
+// The unit after seg; false behind the last request.
 __device__ __forceinline__ bool chunk_next(const ChunkParams& c, ChunkSeg* seg) {
-  seg->t0 = 0;
+  seg->pos = 0;
+  seg->w.step(c);
   if (++seg->rt == chunk_row_tiles(seg->q)) {
     seg->rt = 0;
+    seg->w = ChunkWalk();
     if (++seg->kvh == c.a.n_kv) {
       seg->kvh = 0;
       do {
@@ -131,7 +152,7 @@ __device__ __forceinline__ bool chunk_next(const ChunkParams& c, ChunkSeg* seg) 
       } while (seg->q.n == 0 || seg->q.rows <= c.min_rows);
     }
   }
-  seg->tiles = chunk_tiles(c.a, seg->q, seg->rt);
+  seg->tiles = chunk_tiles(c.a, seg->q, seg->w);
   return true;
 }
 
@@ -521,36 +542,40 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
     if (warp == 21) {
       // ---------------------------------------------------------------- units
       if (p.nreq <= 32 * kLinePerLane) find();
-      auto next = [&] {
-        off += seg.t1 - seg.t0;
-        more = off < off_end && chunk_next(c, &seg);
-      };
       bool ok = true;
       for (int n = 0; ok; ++n) {
         ChunkUnit u{};
         u.nt = -1;
-        if (more) {
-          const int row0 = seg.rt * kChunkRows, tok0 = row0 / p.group;
-          seg.t1 = (int)min((int64_t)seg.tiles, seg.t0 + (off_end - off));
-          u.t0 = seg.t0;
-          u.t1 = seg.t1;
-          u.rows = min(kChunkRows, seg.q.rows - row0);
-          u.req = seg.r;
-          u.kvh = seg.kvh;
-          u.tok0 = seg.q.q0 + tok0;
-          u.sub0 = row0 - tok0 * p.group;
-          u.lim_min = seg.q.len - seg.q.n + tok0;
-          u.key_end = min(seg.q.keys, u.lim_min + group_div(p, u.sub0 + u.rows - 1) + 1);
-          u.keys = seg.q.keys;
-          u.nt = u.key_end <= 0 ? 0 : seg.t1 - seg.t0;
-          u.whole = seg.t0 == 0 && seg.t1 == seg.tiles;
+        int64_t begin = off;
+        int pos = 0, tiles = 0;
+        while (more && u.nt < 0) {
+          begin = off;
+          pos = seg.pos;
+          tiles = seg.tiles;
+          const int here = (int)min((int64_t)(tiles + c.unit_cost - pos), off_end - off);  // places of this CTA on the unit
+          u.t0 = max(0, pos - c.unit_cost);
+          u.t1 = max(0, pos + here - c.unit_cost);
+          if (u.t1 > u.t0) {
+            u.rows = min(kChunkRows, seg.q.rows - seg.rt * kChunkRows);
+            u.req = seg.r;
+            u.kvh = seg.kvh;
+            u.tok0 = seg.q.q0 + seg.w.tok;
+            u.sub0 = seg.w.sub;
+            u.lim_min = seg.q.len - seg.q.n + seg.w.tok;
+            u.key_end = min(seg.q.keys, u.lim_min + group_div(p, u.sub0 + u.rows - 1) + 1);
+            u.keys = seg.q.keys;
+            u.nt = u.key_end <= 0 ? 0 : u.t1 - u.t0;
+            u.whole = u.t0 == 0 && u.t1 == tiles;
+          }
+          off += here;
+          more = off < off_end && chunk_next(c, &seg);
         }
         if (n == 0 && lane == 0) {
           AttnCut cut{};
           cut.c_last = -1;
-          if (more && seg.t0 != 0 && share >= seg.t0) {
+          if (u.nt >= 0 && u.t0 != 0 && share >= u.t0) {  // the border before this CTA cuts the unit, and is the first that does
             int64_t rem;
-            cut.c_last = (int)attn_div(off - seg.t0 + seg.tiles - 1, share, &rem);
+            cut.c_last = (int)attn_div(begin - pos + tiles + c.unit_cost - 1, share, &rem);
             cut.rows = u.rows;
             cut.tok0 = u.tok0;
             cut.sub0 = u.sub0;
@@ -565,7 +590,6 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
           mbar_arrive(&u_full[n % kChunkUnits]);
         }
         if (u.nt < 0) break;
-        next();
       }
     } else if (warp == 20) {
       const bool lead = elect_one();

@@ -241,6 +241,10 @@ static ms_status attend_launch(memstore* s, ChunkParams& c, int64_t max_rows, cu
   c.min_rows = rows ? kChunkMinRows : 0;
   p.max_rows = chunks ? c.min_rows : 0x7fffffff;
   p.beside = chunks;
+  c.step_tok = kChunkRows / p.group;
+  c.step_sub = kChunkRows % p.group;
+  const int64_t all_rows = (int64_t)p.n_tokens * p.group, chunk_units = p.n_kv * (all_rows / kChunkRows + p.nreq);  // (or fewer)
+  c.unit_cost = chunk_units > s->sm_count ? 3 : 0;
   p.tile_shift = __builtin_ctz((unsigned)AttnCfg<D, FP8>::kTileKeys);
   int chunk_ctas = 0, rows_ctas = 0;
   if constexpr (D == 64 || D == 128) {
@@ -257,8 +261,7 @@ static ms_status attend_launch(memstore* s, ChunkParams& c, int64_t max_rows, cu
   }
   const int checks = p.status ? (p.nreq + kCombineThreads / 32 - 1) / (kCombineThreads / 32) : 0;
   // units that the call can have, and so cuts to join (each unit has one first border)
-  const int64_t all_rows = (int64_t)p.n_tokens * p.group;
-  const int chunk_joins = (int)std::max<int64_t>(0, std::min<int64_t>(chunk_ctas - 1, p.n_kv * (all_rows / kChunkRows + p.nreq)));
+  const int chunk_joins = (int)std::max<int64_t>(0, std::min<int64_t>(chunk_ctas - 1, chunk_units));
   const int rows_joins = (int)std::max<int64_t>(0, std::min<int64_t>(rows_ctas - 1, p.n_kv * (all_rows / kAttnRows + p.nreq)));
   const int pieces = chunk_joins <= 32 ? kChunkRows / kChunkJoinRows : 4;
   const int blocks = chunk_joins * pieces + rows_joins + checks;
