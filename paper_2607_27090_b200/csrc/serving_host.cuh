@@ -243,7 +243,7 @@ static ms_status attend_launch(memstore* s, ChunkParams& c, int64_t max_rows, cu
   p.beside = chunks;
   c.step_tok = kChunkRows / p.group;
   c.step_sub = kChunkRows % p.group;
-  const int64_t all_rows = (int64_t)p.n_tokens * p.group, chunk_units = p.n_kv * (all_rows / kChunkRows + p.nreq);  // (or fewer)
+  const int64_t all_rows = (int64_t)p.n_tokens * p.group, chunk_units = p.n_kv * (all_rows / kChunkRows + p.nreq);  // (about)
   c.unit_cost = chunk_units > s->sm_count ? 3 : 0;
   p.tile_shift = __builtin_ctz((unsigned)AttnCfg<D, FP8>::kTileKeys);
   int chunk_ctas = 0, rows_ctas = 0;
@@ -260,9 +260,10 @@ static ms_status attend_launch(memstore* s, ChunkParams& c, int64_t max_rows, cu
     s->kernels_launched++;
   }
   const int checks = p.status ? (p.nreq + kCombineThreads / 32 - 1) / (kCombineThreads / 32) : 0;
-  // units that the call can have, and so cuts to join (each unit has one first border)
-  const int chunk_joins = (int)std::max<int64_t>(0, std::min<int64_t>(chunk_ctas - 1, chunk_units));
-  const int rows_joins = (int)std::max<int64_t>(0, std::min<int64_t>(rows_ctas - 1, p.n_kv * (all_rows / kAttnRows + p.nreq)));
+  // units that the call can have at most, whatever the lengths on the device say, and so cuts to join (each unit has one first border)
+  const int64_t units = (int64_t)p.n_kv * p.nreq;
+  const int chunk_joins = (int)std::max<int64_t>(0, std::min<int64_t>(chunk_ctas - 1, units * (all_rows / kChunkRows + 1)));
+  const int rows_joins = (int)std::max<int64_t>(0, std::min<int64_t>(rows_ctas - 1, units * (all_rows / kAttnRows + 1)));
   const int pieces = chunk_joins <= 32 ? kChunkRows / kChunkJoinRows : 4;
   const int blocks = chunk_joins * pieces + rows_joins + checks;
   if (blocks > 0) {

@@ -348,6 +348,92 @@ def test_attend_lengths_around_tile_borders(fp8, len_, n):
     ms.close()
 
 
+@pytest.mark.parametrize("fp8,d", [(False, 64), (True, 64), (False, 128), (True, 128)])
+@pytest.mark.parametrize("seed", range(6))
+def test_attend_random_batches(fp8, d, seed):
+    """Seeded batches of chunks and single tokens: many and few units, group sizes that divide 256 and that do not, pages of any size,
+    units that several CTAs share."""
+    rng = random.Random(1000 * d + 10 * seed + fp8)
+    hk = rng.choice([1, 2, 3])
+    hq = hk * rng.choice([1, 3, 4, 5, 7, 12, 16])
+    nreq, bs = rng.choice([1, 2, 7, 19]), rng.choice([16, 16, 8, 24, 64, 11])
+    q_hi = rng.choice([40, 300, 900]) if nreq < 7 else rng.choice([5, 60, 200])
+    q = [rng.choice([0, 1, rng.randint(0, q_hi), rng.randint(0, q_hi)]) for _ in range(nreq)]
+    lens = [rng.choice([n, n + rng.randint(0, 2500), max(0, n - rng.randint(0, 40))]) for n in q]
+    q_start = [0] + [int(x) for x in np.cumsum(q)]
+    tables, nb = paged(rng, lens, bs)
+    cache, gen = fill_cache(1, nb, bs, hk, d, fp8, rng.choice(["NHD", "HND"]), seed)
+    ms = store(hk, d)
+    x = (rng.choice([0.3, 2.0, 6.0]) * torch.randn((q_start[-1] + 1, hq, d), generator=gen, device=DEV)).to(torch.bfloat16)
+    check_attend(ms, cache, x, q_start, lens, tables, max_q_len=rng.choice([0, max(q), 1]))  # (the bound may be wrong)
+    ms.close()
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("n,len_", [(200, 150), (300, 0), (130, 129), (64, 1), (40, 40), (700, 3), (65, 128), (257, 129)])
+def test_attend_chunks_whose_first_rows_have_no_keys(fp8, n, len_):
+    hk, d, hq = 2, 128, 8
+    tables, nb = paged(random.Random(n), [len_], 16)
+    cache, gen = fill_cache(1, nb, 16, hk, d, fp8, "NHD", n)
+    ms = store(hk, d)
+    q = torch.randn((n, hq, d), generator=gen, device=DEV).to(torch.bfloat16)
+    out, lse = check_attend(ms, cache, q, [0, n], [len_], tables)
+    assert (out[: max(0, n - len_)] == 0).all() and (lse[: max(0, n - len_)] == -math.inf).all()
+    ms.close()
+
+
+def test_attend_chunks_over_tables_with_holes():
+    bs, lens, q_start = 16, [700, 500, 300], [0, 90, 290, 300]
+    tables, nb = paged(random.Random(6), lens, bs, width_extra=0)
+    tables[0, 3], tables[0, 40], tables[1, 31], tables[1, 0] = -1, nb, nb + 5, -(2**31)
+    short = tables[:, :40].contiguous()  # request 0 has 44 blocks
+    cache, gen = fill_cache(1, nb, bs, 2, 128, False, "NHD", 6)
+    ms = store(2, 128)
+    q = torch.randn((300, 8, 128), generator=gen, device=DEV).to(torch.bfloat16)
+    check_attend(ms, cache, q, q_start, lens, tables, want_status=[8, 8, 0])
+    check_attend(ms, cache, q, q_start, lens, short, want_status=[12, 8, 0])
+    ms.close()
+
+
+def test_attend_scores_that_grow_along_the_keys():
+    """Every tile raises the running maximum (by far more than the weights' slack), or lowers it: accumulators are rescaled each time."""
+    n, len_, hk, d = 70, 1500, 1, 128
+    for fp8 in (False, True):
+        for sign in (1.0, -1.0):
+            tables, nb = paged(random.Random(8), [len_], 16)
+            cache, gen = fill_cache(1, nb, 16, hk, d, fp8, "NHD", 3, k_scale=1.0, v_scale=0.03)
+            q = torch.zeros((n, 4, d), device=DEV)
+            q[..., 0] = 1.0 + torch.arange(n, device=DEV)[:, None] / n
+            for j in range(len_):
+                blk, off = int(tables[0, j // 16]), j % 16
+                val = round(sign * (j - 750) / 4.0)
+                k = torch.zeros(d, device=DEV)
+                k[0] = val
+                cache.k[0, blk, off, 0] = k.to(ref.F8).view(torch.uint8) if fp8 else k.to(torch.bfloat16)
+            ms = store(hk, d)
+            check_attend(ms, cache, q.to(torch.bfloat16), [0, n], [len_], tables, scale=1.0)
+            check_attend(ms, cache, q[:2].to(torch.bfloat16), [0, 2], [len_], tables, scale=1.0)
+            ms.close()
+
+
+def test_attend_reports_a_wait_that_ran_out_and_works_again():
+    """The chunk kernel's loading role issues nothing and every wait gives up after a few thousand polls: the call returns, the status
+    says so, and the next call is right."""
+    lens, q_start = [700, 50], [0, 100, 101]
+    tables, nb = paged(random.Random(9), lens, 16)
+    cache, gen = fill_cache(1, nb, 16, 2, 128, False, "NHD", 9)
+    ms = store(2, 128)
+    q = torch.randn((101, 8, 128), generator=gen, device=DEV).to(torch.bfloat16)
+    status = i32([0, 0])
+    ms.test_hooks(wait_poll_limit=3000, mute_producers=True)
+    ms.attend(0, q, cache, i32(q_start), i32(lens), tables, out_status=status)
+    torch.cuda.synchronize()
+    assert status.tolist() == [32, 0]  # (the single token is served by the other kernel)
+    ms.test_hooks()
+    check_attend(ms, cache, q, q_start, lens, tables)
+    ms.close()
+
+
 def test_attend_many_requests_and_empty_ones():
     rng = random.Random(3)
     q_start, lens = random_case(rng, 700, 3, 90)
