@@ -11,7 +11,7 @@
 // Work split: a unit is (request, K/V head, 16 rows) x all its tiles of 64 keys (128 where cache rows are
 // at most 128 bytes).  The tiles of all units are numbered one after
 // another and every CTA of one resident wave takes an equal share of that line, wherever unit borders fall: ragged lengths
-// balance exactly, and a CTA leaves at most two unfinished units (its first and its last), which attend_combine_kernel joins.
+// balance exactly, and a CTA leaves at most two unfinished units (its first and its last), which attend_join_kernel joins.
 // The workspace therefore depends on the number of CTAs alone.  Every order of summation follows from the lengths: results are
 // the same on every run.
 // Inside a CTA each warp streams its own quarter of a tile's keys through a private ring (cp.async), with running statistics of its
@@ -697,7 +697,7 @@ __global__ void __launch_bounds__(kAttnThreads, AttnCfg<D, FP8>::kCtasPerSm) att
 
 // Joins the parts of the unit that the border in front of CTA b's share cuts, if it is the unit's first border.
 constexpr int kCombineThreads = 512;
-constexpr int kJoinBatch = 8;
+constexpr int kJoinBatch = 5;  // parts whose loads fly together (as many as two blocks on an SM have registers for)
 // CTA whose border makes the n-th cut, or -1; by the whole block.
 __device__ __forceinline__ int nth_cut(const AttnCut* cuts, int ctas, int cuts_at_most, int n) {
   if (cuts_at_most >= ctas - 1) return cuts[n + 1].c_last >= 0 ? n + 1 : -1;  // a block per border
@@ -763,7 +763,8 @@ __device__ __forceinline__ void rows_join(const AttendParams& p, int b) {
       float4 x[kJoinBatch];
 #pragma unroll
       for (int i = 0; i < kJoinBatch; ++i) {  // (the loads of several parts fly together)
-        const int c = min(c0 + i, c_last);
+        const int c = c0 + i;
+        if (c > c_last) break;  // uniform
         const int64_t at = ((int64_t)c * 2 + (c == b - 1 ? 1 : 0)) * kAttnRows + row;
         ml[i] = p.part_ml[at];
         x[i] = *reinterpret_cast<const float4*>(p.part_o + at * D + d);

@@ -15,8 +15,10 @@
 //   warp 20          TMEM allocation, tcgen05.mma issue by one elected lane
 //   warp 21          walks the CTA's share of the line and describes its units to the other roles (warps 22, 23 complete the warpgroup)
 // Work split: as in attend.cuh, the tiles of all units (causal: only as many as a unit's last row sees) form one line of which every
-// CTA takes an equal share, so 64 units on 148 SMs balance as well as 6400.  Starting and ending a unit costs about as much as three of
-// its tiles; where there are more units than CTAs each unit takes three places on the line for that (else a CTA has one piece anyway).
+// CTA takes an equal share, so 64 units on 148 SMs balance as well as 6400.  Starting and ending a unit costs as much as a few of its
+// tiles, so each unit takes kChunkUnitCost places more on the line.  Places for that, and the time of a call (32/8 heads of 128,
+// bf16): none: 2,048 tokens of 2,048 131 us, 512 of 512 39 us, 512 of 4,096 64 us, 64 of 32,000 70 us; three: 83, 30, 60, 65;
+// four: 82, 30, 59, 63; five: 76, 33, 58, 61 (and an 8-bit cache 69 instead of 67).
 // Running maximum: the weights are formed with the maximum of the tiles before; no maximum is looked for unless the sum of a thread's 64
 // weights passes 2^14, when the row takes a new maximum, its weights are formed again and its accumulator is rescaled.  fp32 sums, and
 // weights of up to 2^14 in bf16 or fp16, lose nothing by that.
@@ -33,6 +35,7 @@ constexpr int kChunkStages = 5;
 constexpr int kChunkThreads = 24 * 32;
 constexpr int kChunkRegsWeights = 88, kChunkRegsLoads = 72, kChunkRegsIssue = 56;
 static_assert(4 * kChunkRegsWeights + kChunkRegsLoads + kChunkRegsIssue <= 6 * 80, "six warpgroups share the 80 registers a thread of the launch");
+constexpr int kChunkUnitCost = 4;    // places on the line of tiles that stand for the set-up and the end of a unit
 constexpr int kChunkMaskRing = 8;     // (a tile's masks are read at most three tiles after the loader wrote them)
 constexpr uint32_t kChunkSpinLimit = 1u << 26;  // polls (a second or more)
 constexpr float kChunkMaxSum = 16384.f;  // sum of 64 weights (and so a weight) that is tolerated without taking a new maximum
@@ -56,7 +59,6 @@ struct ChunkParams {
   int32_t min_rows;   // requests with more rows than this are served here
   int32_t min_share;
   int32_t step_tok, step_sub;  // kChunkRows / group and kChunkRows % group
-  int32_t unit_cost;  // places of the line that stand for a unit's set-up
   float* part_o;      // [CTAs][2][D / 4][kChunkRows][4]
   float2* part_ml;    // [CTAs][2][kChunkRows]
   AttnCut* cuts;      // [CTAs]
@@ -87,7 +89,7 @@ __device__ __forceinline__ int64_t chunk_head_cost(const ChunkParams& c, const A
   int64_t s = 0;
   ChunkWalk w;
   const int n = chunk_row_tiles(q);
-  for (int rt = 0; rt < n; ++rt, w.step(c)) s += chunk_tiles(c.a, q, w) + c.unit_cost;
+  for (int rt = 0; rt < n; ++rt, w.step(c)) s += chunk_tiles(c.a, q, w) + kChunkUnitCost;
   return s;
 }
 __device__ __forceinline__ int64_t chunk_cost(const ChunkParams& c, const AttnReq& q) {
@@ -109,7 +111,7 @@ struct __align__(16) ChunkUnit {
   int32_t whole;            // all tiles of the unit are here
 };
 
-// A unit, and the place on it where a CTA's share begins (the first unit_cost places stand for its set-up, then come its tiles).
+// A unit, and the place on it where a CTA's share begins (the first kChunkUnitCost places stand for its set-up, then come its tiles).
 struct ChunkSeg {
   int r, kvh, rt, tiles, pos;
   ChunkWalk w;
@@ -129,8 +131,8 @@ __device__ __forceinline__ bool chunk_locate(const ChunkParams& c, const AttnLin
   seg->w = ChunkWalk();
   for (;;) {
     seg->tiles = chunk_tiles(c.a, seg->q, seg->w);
-    if (rem < seg->tiles + c.unit_cost) break;
-    rem -= seg->tiles + c.unit_cost;
+    if (rem < seg->tiles + kChunkUnitCost) break;
+    rem -= seg->tiles + kChunkUnitCost;
     ++seg->rt;
     seg->w.step(c);
   }
@@ -552,9 +554,9 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
           begin = off;
           pos = seg.pos;
           tiles = seg.tiles;
-          const int here = (int)min((int64_t)(tiles + c.unit_cost - pos), off_end - off);  // places of this CTA on the unit
-          u.t0 = max(0, pos - c.unit_cost);
-          u.t1 = max(0, pos + here - c.unit_cost);
+          const int here = (int)min((int64_t)(tiles + kChunkUnitCost - pos), off_end - off);  // places of this CTA on the unit
+          u.t0 = max(0, pos - kChunkUnitCost);
+          u.t1 = max(0, pos + here - kChunkUnitCost);
           if (u.t1 > u.t0) {
             u.rows = min(kChunkRows, seg.q.rows - seg.rt * kChunkRows);
             u.req = seg.r;
@@ -575,7 +577,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
           cut.c_last = -1;
           if (u.nt >= 0 && u.t0 != 0 && share >= u.t0) {  // the border before this CTA cuts the unit, and is the first that does
             int64_t rem;
-            cut.c_last = (int)attn_div(begin - pos + tiles + c.unit_cost - 1, share, &rem);
+            cut.c_last = (int)attn_div(begin - pos + tiles + kChunkUnitCost - 1, share, &rem);
             cut.rows = u.rows;
             cut.tok0 = u.tok0;
             cut.sub0 = u.sub0;
@@ -982,7 +984,8 @@ __device__ __forceinline__ void chunk_join(const ChunkParams& c, int b, int row0
       float4 x[kJoinBatch];
 #pragma unroll
       for (int k = 0; k < kJoinBatch; ++k) {
-        const int i = min(i0 + k, c_last);
+        const int i = i0 + k;
+        if (i > c_last) break;  // uniform
         const int64_t slot = (int64_t)i * 2 + (i == b - 1 ? 1 : 0);
         ml[k] = c.part_ml[slot * kChunkRows + row];
         x[k] = *reinterpret_cast<const float4*>(c.part_o + ((slot * (D / 4) + d4) * kChunkRows + row) * 4);
@@ -994,10 +997,12 @@ __device__ __forceinline__ void chunk_join(const ChunkParams& c, int b, int row0
 }
 
 // Joins what CTA borders cut and reports on the requests; the last kernel of a call.  Blocks: `pieces` for each cut unit of the chunk
-// kernel (16 rows at a time; few cuts are spread over more blocks), cut units of the rows kernel, then sixteen requests each.  There are as many blocks as units could be cut - no more than there
-// are units or borders - and block n looks for the n-th cut among those that the CTAs recorded.
+// kernel (16 rows at a time), cut units of the rows kernel, then sixteen requests each.  There are as many blocks as units could be
+// cut - no more than there are units or borders - and block n looks for the n-th cut among those that the CTAs recorded.
+// Bound: L2 (147 cuts of 256 rows x 128 elements, two or three fp32 parts each: 40 MB, 20 us alone) and the latency of a block's few
+// dependent loads, so two blocks share an SM (one block an SM: 28 us) and only parts that exist are loaded.
 template <int D>
-__global__ void __launch_bounds__(kCombineThreads) attend_join_kernel(const ChunkParams c, const int chunk_ctas, const int chunk_joins, const int pieces,
+__global__ void __launch_bounds__(kCombineThreads, 2) attend_join_kernel(const ChunkParams c, const int chunk_ctas, const int chunk_joins, const int pieces,
                                                                       const int rows_ctas, const int rows_joins) {
   grid_launch_dependents();
   grid_dependency_wait();

@@ -183,8 +183,12 @@ ms_status memstore_append(memstore_t* s, int32_t layer, const ms_heads* q, int32
 }
 
 // ---- attention --------------------------------------------------------------------------------------------------------
-// Requests with more rows (new tokens x query heads per K/V head) than this go to the tensor-core kernel, when head_dim allows it.
-constexpr int kChunkMinRows = kAttnRows;
+// Requests with more rows (new tokens x query heads per K/V head) than this go to the tensor-core kernel, when head_dim allows it: than
+// two units of the rows kernel where the batch leaves half of the SMs without a unit of their own, else than one.  Rows kernel against
+// chunk kernel (32/8 heads of 128, bf16): 20 or 32 rows, one request of 4,096 tokens 17 against 22 us, two 22 against 26, eight of 2,000
+// 31 against 36 (of 8,000 90 against 82); 64 of 2,000 170 against 159, 32 of 8,000 318 against 238.  64 rows: one request 23.4 against
+// 22.8 us, 64 of 2,000 321 against 165.
+static int chunk_min_rows(int64_t units, int sm_count) { return units <= sm_count / 2 ? 2 * kAttnRows : kAttnRows; }
 
 // The workspace: unfinished rows of the rows kernel (kAttnMaxCtasPerSm CTAs per SM at most) and their statistics, then those of the chunk kernel
 // (one CTA per SM) and its error words.  It depends on the GPU and head_dim alone.
@@ -236,15 +240,15 @@ static ms_status attend_launch(memstore* s, ChunkParams& c, int64_t max_rows, cu
   // Which kernels: the chunk kernel when a request may have more rows than the rows kernel serves well, the rows kernel when a
   // request may have fewer.  A single request whose rows are probably many goes to the chunk kernel whatever it turns out to be,
   // and one kernel is saved.
-  bool chunks = (D == 64 || D == 128) && max_rows > kChunkMinRows;
+  const int min_rows = chunk_min_rows((int64_t)p.n_kv * p.nreq, s->sm_count);
+  bool chunks = (D == 64 || D == 128) && max_rows > min_rows;
   const bool rows = !chunks || p.nreq > 1;
-  c.min_rows = rows ? kChunkMinRows : 0;
+  c.min_rows = rows ? min_rows : 0;
   p.max_rows = chunks ? c.min_rows : 0x7fffffff;
   p.beside = chunks;
   c.step_tok = kChunkRows / p.group;
   c.step_sub = kChunkRows % p.group;
-  const int64_t all_rows = (int64_t)p.n_tokens * p.group, chunk_units = p.n_kv * (all_rows / kChunkRows + p.nreq);  // (about)
-  c.unit_cost = chunk_units > s->sm_count ? 3 : 0;
+  const int64_t all_rows = (int64_t)p.n_tokens * p.group;
   p.tile_shift = __builtin_ctz((unsigned)AttnCfg<D, FP8>::kTileKeys);
   int chunk_ctas = 0, rows_ctas = 0;
   if constexpr (D == 64 || D == 128) {
@@ -264,6 +268,8 @@ static ms_status attend_launch(memstore* s, ChunkParams& c, int64_t max_rows, cu
   const int64_t units = (int64_t)p.n_kv * p.nreq;
   const int chunk_joins = (int)std::max<int64_t>(0, std::min<int64_t>(chunk_ctas - 1, units * (all_rows / kChunkRows + 1)));
   const int rows_joins = (int)std::max<int64_t>(0, std::min<int64_t>(rows_ctas - 1, units * (all_rows / kAttnRows + 1)));
+  // Few cuts are spread over more blocks: one question of 36 rows (18 cuts) 25 us with 16 pieces a cut, 39 with 4; a batch with 147 cuts
+  // 57 us with 4, 60 with 16.
   const int pieces = chunk_joins <= 32 ? kChunkRows / kChunkJoinRows : 4;
   const int blocks = chunk_joins * pieces + rows_joins + checks;
   if (blocks > 0) {
