@@ -405,7 +405,8 @@ ms_status memstore_serve_host(memstore_t* store, const void* query, int32_t user
  * after another along the token axis (q_start).  These calls use no scratch of the store: memstore_attend works in a
  * workspace that the caller gives, so calls on different streams or in different CUDA graphs do not disturb one another
  * as long as their arguments differ.  They run on the store's device whichever device is current, and may be captured
- * from their first call on.
+ * from their first call on.  Numbers of requests, tokens, entries per table and (query head, token) rows per K/V head are at most
+ * 2^30 in a call (MS_ERR_UNSUPPORTED).
  */
 
 /* A [tokens][heads][head_dim] bf16 array: element (t, h, d) at base[t * token_stride + h * head_stride + d].  base 16-byte

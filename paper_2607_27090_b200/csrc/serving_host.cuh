@@ -6,6 +6,13 @@ static_assert(kReqTableShort == MS_REQ_BLOCK_TABLE_SHORT && kReqBadBlock == MS_R
                   kReqBadLength == MS_REQ_BAD_LENGTH,
               "status bits of the kernels and the header");
 
+// Counts are at most 2^30, so that the kernels' 32-bit loops end before they wrap.
+constexpr int32_t kMaxCount = 1 << 30;
+static ms_status check_counts(memstore* s, int32_t a, int32_t b, int32_t c) {
+  const int32_t most = std::max(a, std::max(b, c));
+  return most <= kMaxCount ? MS_OK : fail(s, MS_ERR_UNSUPPORTED, "a count of %d is more than 2^30", most);
+}
+
 static ms_status check_geometry(memstore* s, const ms_paged_cache* c) {
   if (!c || c->block_size <= 0 || c->num_blocks <= 0) return fail(s, MS_ERR_INVALID_ARG, "bad cache description");
   return MS_OK;
@@ -52,6 +59,7 @@ ms_status memstore_grow_blocks(memstore_t* s, const int32_t* start_lens, const i
   if (rc != MS_OK) return rc;
   if (nreq < 0 || max_blocks < 0 || n_free < 0 || token_capacity < 0)
     return fail(s, MS_ERR_INVALID_ARG, "nreq=%d max_blocks=%d n_free=%d token_capacity=%d", nreq, max_blocks, n_free, token_capacity);
+  if ((rc = check_counts(s, nreq, max_blocks, token_capacity)) != MS_OK) return rc;
   if (!n_taken || !out_q_start || !out_n_taken || (n_free > 0 && !free_blocks) ||
       (nreq > 0 && (!start_lens || !new_lens || !out_seq_lens || !out_status || (max_blocks > 0 && !block_tables))))
     return fail(s, MS_ERR_INVALID_ARG, "null request arrays");
@@ -95,6 +103,7 @@ ms_status memstore_release_blocks(memstore_t* s, const int32_t* release, int32_t
   ms_status rc = check_geometry(s, cache);
   if (rc != MS_OK) return rc;
   if (nreq < 0 || max_blocks < 0 || n_free < 0) return fail(s, MS_ERR_INVALID_ARG, "nreq=%d max_blocks=%d n_free=%d", nreq, max_blocks, n_free);
+  if ((rc = check_counts(s, nreq, max_blocks, 0)) != MS_OK) return rc;
   if (nreq == 0) return MS_OK;
   if (!seq_lens || !n_taken || (n_free > 0 && !free_blocks) || (max_blocks > 0 && !block_tables)) return fail(s, MS_ERR_INVALID_ARG, "null request arrays");
   DeviceGuard g(s->cfg.device);
@@ -113,6 +122,7 @@ ms_status memstore_append(memstore_t* s, int32_t layer, const ms_heads* q, int32
   const memstore_config& c = s->cfg;
   if (n_tokens < 0 || n_q_heads < 0 || n_q_heads > (1 << 16)) return fail(s, MS_ERR_INVALID_ARG, "n_tokens=%d n_q_heads=%d", n_tokens, n_q_heads);
   ms_status rc = check_cache(s, cache, layer, false);
+  if (rc == MS_OK) rc = check_counts(s, n_tokens, 0, 0);
   if (rc == MS_OK) rc = check_heads(s, k, n_tokens, c.n_kv_heads, false, "k");
   if (rc == MS_OK) rc = check_heads(s, v, n_tokens, c.n_kv_heads, false, "v");
   if (rc == MS_OK && n_q_heads > 0) rc = check_heads(s, q, n_tokens, n_q_heads, false, "q");
@@ -268,7 +278,7 @@ static ms_status attend_launch(memstore* s, ChunkParams& c, int64_t max_rows, cu
   const int64_t units = (int64_t)p.n_kv * p.nreq;
   const int chunk_joins = (int)std::max<int64_t>(0, std::min<int64_t>(chunk_ctas - 1, units * (all_rows / kChunkRows + 1)));
   const int rows_joins = (int)std::max<int64_t>(0, std::min<int64_t>(rows_ctas - 1, units * (all_rows / kAttnRows + 1)));
-  // Few cuts are spread over more blocks: one question of 36 rows (18 cuts) 25 us with 16 pieces a cut, 39 with 4; a batch with 147 cuts
+  // Few cuts are spread over more blocks: 61 tokens of one request (8 cuts) 25 us with 16 pieces a cut, 39 with 4; a batch with 147 cuts
   // 57 us with 4, 60 with 16.
   const int pieces = chunk_joins <= 32 ? kChunkRows / kChunkJoinRows : 4;
   const int blocks = chunk_joins * pieces + rows_joins + checks;
@@ -296,9 +306,10 @@ ms_status memstore_attend(memstore_t* s, int32_t layer, const ms_heads* q, int32
     return fail(s, MS_ERR_INVALID_ARG, "%d query heads for %d K/V heads", n_q_heads, c.n_kv_heads);
   const int32_t group = n_q_heads / c.n_kv_heads;
   if (group > kAttnMaxGroup) return fail(s, MS_ERR_UNSUPPORTED, "%d query heads per K/V head (at most %d)", group, kAttnMaxGroup);
-  if ((int64_t)n_tokens * group > 0x7fffffff - 256) return fail(s, MS_ERR_UNSUPPORTED, "%d tokens of %d heads", n_tokens, n_q_heads);
+  if ((int64_t)n_tokens * group > kMaxCount) return fail(s, MS_ERR_UNSUPPORTED, "%d tokens of %d heads", n_tokens, n_q_heads);
   if (!(scale >= 0.f) || !std::isfinite(scale)) return fail(s, MS_ERR_INVALID_ARG, "scale must be positive and finite, or 0 for the default");
   ms_status rc = check_cache(s, cache, layer, true);
+  if (rc == MS_OK) rc = check_counts(s, nreq, max_blocks, 0);
   if (rc == MS_OK) rc = check_heads(s, q, n_tokens, n_q_heads, false, "q");
   if (rc == MS_OK) rc = check_heads(s, out, n_tokens, n_q_heads, true, "out");
   if (rc != MS_OK) return rc;
@@ -340,13 +351,13 @@ ms_status memstore_attend(memstore_t* s, int32_t layer, const ms_heads* q, int32
   p.v_scale = fp8 ? cache->v_scale : 1.f;
   p.lse = out_lse;
   p.status = out_status;
-  p.min_share = 2;
+  p.min_share = 2;  // (one decode request of 2,033 tokens: 1 tile per CTA at least 12.6 us, 2 11.2, 4 10.9; long batches do not care)
   const AttendLayout w = attend_layout(s);
   char* base = (char*)workspace;
   p.part_o = (float*)(base + w.rows_o);
   p.part_ml = (float2*)(base + w.rows_ml);
   p.cuts = (AttnCut*)(base + w.rows_cuts);
-  cp.min_share = 1;
+  cp.min_share = 1;  // (61 tokens of one request: 24 us, with two or three tiles 32)
   cp.part_o = (float*)(base + w.chunk_o);
   cp.part_ml = (float2*)(base + w.chunk_ml);
   cp.cuts = (AttnCut*)(base + w.chunk_cuts);

@@ -747,3 +747,25 @@ def test_refusals():
     ms.append(0, q[:0], k[:0], k[:0], pos[:0], slots[:0], cache)
     torch.cuda.synchronize()
     ms.close()
+
+
+def test_counts_that_would_wrap_are_refused():
+    """Loops over counts near 2^31 would wrap; such calls are refused before anything is launched."""
+    ms = store(2, 64, 2)
+    cache = PagedCache.allocate(2, 4, 16, 2, 64, DEV)
+    ln, tb, qs, big = i32([3]), i32([[0]]), i32([0, 3]), (1 << 30) + 1
+    out, c = GrownBlocks(qs, ln, None, None, ln, ln), cache._struct()
+    for capacity in (big, 2**31 - 1):
+        with pytest.raises(M.MemStoreError) as e:
+            ms.grow_blocks(ln, ln, tb, cache, ln, ln, capacity, out=out)
+        assert e.value.code == 2 and "2^30" in str(e.value)
+    lib, h, at = ms._lib, ms._h, ln.data_ptr()
+    x = M._Heads(torch.zeros(3 * 4 * 64, dtype=torch.bfloat16, device=DEV).data_ptr(), 256, 64)
+    work = torch.empty(ms.attend_workspace_bytes(), dtype=torch.uint8, device=DEV)
+    assert lib.memstore_release_blocks(h, None, at, 1, at, big, c, at, 1, at, None, 0) == 2
+    assert lib.memstore_release_blocks(h, None, at, big, at, 1, c, at, 1, at, None, 0) == 2
+    assert lib.memstore_append(h, 0, None, 0, x, x, at, at, big, c, None, None, 0) == 2
+    for n_tokens, nreq, blocks in ((big, 1, 1), (big // 2 + 1, 1, 1), (3, big, 1), (3, 1, big)):
+        assert lib.memstore_attend(h, 0, x, 4, n_tokens, at, at, nreq, at, blocks, c, 0.0, 0, x, None, None, work.data_ptr(), work.numel(), 0) == 2
+    torch.cuda.synchronize()
+    ms.close()
