@@ -769,3 +769,71 @@ def test_counts_that_would_wrap_are_refused():
         assert lib.memstore_attend(h, 0, x, 4, n_tokens, at, at, nreq, at, blocks, c, 0.0, 0, x, None, None, work.data_ptr(), work.numel(), 0) == 2
     torch.cuda.synchronize()
     ms.close()
+
+
+@pytest.mark.parametrize("d,hq,hk,fp8", [(128, 8, 2, False), (128, 16, 1, True), (64, 4, 1, False), (64, 20, 4, True)])
+@pytest.mark.parametrize("nreq,lens_hi", [(1, 2500), (5, 900), (90, 300)])
+def test_attend_rows_on_both_sides_of_the_choice_of_kernels(d, hq, hk, fp8, nreq, lens_hi):
+    """Requests of 16, 17, 32, 33 and more rows, in batches that leave SMs without a unit and in batches that do not."""
+    rng, group = random.Random(nreq * d + hq), hq // hk
+    ns = [rows // group + extra for rows in (16, 32) for extra in (0, 1)] + [1, 64 // group]
+    ms = store(hk, d)
+    for shift in range(1 if nreq > 1 else len(ns)):
+        n = [ns[(r + shift) % len(ns)] for r in range(nreq)]
+        lens = [m + rng.randint(0, lens_hi) for m in n]
+        tables, nb = paged(rng, lens, 16)
+        cache, gen = fill_cache(1, nb, 16, hk, d, fp8, "NHD", nreq)
+        q_start = [0] + [int(x) for x in np.cumsum(n)]
+        q = torch.randn((q_start[-1], hq, d), generator=gen, device=DEV).to(torch.bfloat16)
+        for bound in (0, max(n)):
+            check_attend(ms, cache, q, q_start, lens, tables, max_q_len=bound)
+    ms.close()
+
+
+def test_attend_from_two_threads_and_two_graphs_at_once():
+    """Calls that overlap on the GPU: two host threads on streams of their own, then two captured graphs replayed side by side."""
+    import threading
+
+    rng = random.Random(5)
+    ms = store(4, 128)
+    work = []
+    for i in range(2):
+        q_start, lens = random_case(rng, 30, 90, 2500)
+        tables, nb = paged(rng, lens, 16)
+        cache, gen = fill_cache(1, nb, 16, 4, 128, bool(i), "NHD", 50 + i)
+        q = torch.randn((q_start[-1], 16, 128), generator=gen, device=DEV).to(torch.bfloat16)
+        a = (0, q, cache, i32(q_start), i32(lens), tables)
+        want, lse = check_attend(ms, cache, q, q_start, lens, tables)
+        work.append((a, want, lse, torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    got = [[], []]
+
+    def serve(i):
+        a, _, _, st = work[i]
+        with torch.cuda.stream(st):
+            for _ in range(20):
+                got[i].append(ms.attend(*a, want_lse=True))
+
+    threads = [threading.Thread(target=serve, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert len(got[i]) == 20 and all(torch.equal(o, work[i][1]) and torch.equal(l, work[i][2]) for o, l, _ in got[i])
+    graphs = []
+    for a, *_ in work:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            out, lse, _ = ms.attend(*a, want_lse=True)
+        graphs.append((g, out, lse))
+    for _ in range(10):
+        for (g, out, lse), w in zip(graphs, work):
+            with torch.cuda.stream(w[3]):
+                out.zero_()
+                g.replay()
+    torch.cuda.synchronize()
+    for (g, out, lse), w in zip(graphs, work):
+        assert torch.equal(out, w[1]) and torch.equal(lse, w[2])
+    ms.close()
