@@ -413,7 +413,13 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
       __syncwarp();
       if (u.nt < 0) break;
       unit_done(n);
-      if (u.nt == 0) continue;
+      if (u.nt == 0) {
+        // A tile that has been held back (see below) goes out now: after a few units without keys the next description waits for the
+        // weights of the last unit that had some, and those wait for this tile.
+        cp_async_wait<0>();
+        while (unpublished > 0) publish();
+        continue;
+      }
       const int t_end = u.t0 + u.nt;
       // ---- tiles: K, V, K, V ...; a thread looks up key lt of the tile, a warp copies its own 32 keys
       const int32_t* table = p.tables + (int64_t)u.req * p.max_blocks;

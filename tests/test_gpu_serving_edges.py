@@ -1,0 +1,70 @@
+"""GPU tests of the serving calls where several things meet: units with and without keys in one CTA's share, long tails of small
+weights, scales at the ends of their range, calls back to back on one stream, time-outs that nobody asked about."""
+import math
+import random
+
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+if torch.cuda.is_available():
+    import serving_ref as ref
+    from test_gpu_serving import DEV, check_attend, fill_cache, i32, paged, store
+
+
+# ------------------------------------------------------------------------------------------------ units without keys
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("first,empty", [([(65, 128)], 12), ([(65, 128)], 3), ([(65, 256), (200, 200), (97, 128), (33, 384)], 30)])
+def test_attend_chunks_without_keys_behind_chunks_whose_last_tile_every_row_sees(fp8, d, first, empty):
+    """Prompts that found no blocks (their rows see no key) beside a chunk whose last unit ends with a tile that all its rows see."""
+    hk, hq = 8, 32
+    q = [n for n, _ in first] + [1000] * empty
+    lens = [n for _, n in first] + [0] * empty
+    q_start = [0] + [int(x) for x in np.cumsum(q)]
+    tables, nb = paged(random.Random(d), lens, 16)
+    cache, gen = fill_cache(1, nb, 16, hk, d, fp8, "NHD", d)
+    ms = store(hk, d)
+    x = torch.randn((q_start[-1], hq, d), generator=gen, device=DEV).to(torch.bfloat16)
+    out, lse = check_attend(ms, cache, x, q_start, lens, tables)
+    a = q_start[len(first)]
+    assert (out[a:] == 0).all() and (lse[a:] == -math.inf).all()
+    ms.close()
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("d", [64, 128])
+def test_attend_chunks_without_keys_behind_chunks_with_short_tables(fp8, d):
+    """The table ends long before the rows' positions, so that every tile of the unit is one that all rows see."""
+    hk, hq, bs = 4, 16, 16
+    q, lens = [70, 600, 600, 64, 600, 600, 600, 600], [900, 0, 0, 800, 0, 0, 0, 0]
+    q_start = [0] + [int(x) for x in np.cumsum(q)]
+    tables, nb = paged(random.Random(d), lens, bs)
+    cache, gen = fill_cache(1, nb, bs, hk, d, fp8, "NHD", d + 1)
+    ms = store(hk, d)
+    x = torch.randn((q_start[-1], hq, d), generator=gen, device=DEV).to(torch.bfloat16)
+    for width in (8, 16, 31):
+        check_attend(ms, cache, x, q_start, lens, tables[:, :width].contiguous(), want_status=[4, 0, 0, 4, 0, 0, 0, 0])
+    ms.close()
+
+
+@pytest.mark.parametrize("fp8,d", [(False, 64), (True, 64), (False, 128), (True, 128)])
+@pytest.mark.parametrize("seed", range(4))
+def test_attend_random_batches_with_many_units_without_keys(fp8, d, seed):
+    rng = random.Random(7000 + 10 * seed + d + fp8)
+    hk = rng.choice([1, 2, 4])
+    hq = hk * rng.choice([1, 4, 6, 64 // hk**2])
+    q, lens = [], []
+    for _ in range(rng.choice([6, 40, 140])):  # (more than 128 requests are located by the whole block)
+        n = rng.choice([1, 33, 65, 97, 129, 200])
+        q.append(n)
+        lens.append(rng.choice([0, 0, 0, 0, n, n + 63, 128 * rng.randint(1, 5)]))
+    q_start = [0] + [int(x) for x in np.cumsum(q)]
+    tables, nb = paged(rng, lens, 16)
+    cache, gen = fill_cache(1, nb, 16, hk, d, fp8, rng.choice(["NHD", "HND"]), seed)
+    ms = store(hk, d)
+    x = torch.randn((q_start[-1], hq, d), generator=gen, device=DEV).to(torch.bfloat16)
+    check_attend(ms, cache, x, q_start, lens, tables)
+    ms.close()
