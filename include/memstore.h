@@ -501,6 +501,7 @@ ms_status memstore_append(memstore_t* store, int32_t layer, const ms_heads* q, i
  *   out_lse       device fp32 [n_tokens][n_q_heads] or NULL
  *   out_status    device int32 [nreq] or NULL: MS_REQ_BAD_LENGTH (q_start[r] .. q_start[r+1] is no range of rows, or seq_len is not in
  *                 [0, 2^30]: the request is left out), MS_REQ_BLOCK_TABLE_SHORT, MS_REQ_BAD_BLOCK_ID, MS_REQ_KERNEL_TIMEOUT
+ *                 (which kernel_timeouts of memstore_stats reports too, whether or not there is an out_status)
  *   workspace     device, 256-byte aligned, memstore_attend_workspace() bytes or more; its contents need not be kept or
  *                 cleared between calls, but calls that may overlap on the GPU need workspaces of their own
  */
@@ -519,7 +520,8 @@ typedef struct {
   int64_t kernels_launched; /* kernels of this library enqueued so far */
   int64_t arena_bytes, embedding_bytes;
   int64_t host_kv_tokens_used;
-  int64_t kernel_timeouts; /* 1 if a bounded wait inside the tensor-core scoring kernel ever ran out (results of that call are invalid) */
+  int64_t kernel_timeouts; /* 1 if a bounded wait inside the tensor-core scoring kernel or the chunk kernel of memstore_attend ever
+                              ran out (results of that call are invalid) */
   int64_t filter_fixups;   /* queries of the tensor-core retrieve path that were re-scanned exactly because the filter's margin
                               check failed (more groups within rounding of the k-th score than the margin keeps) */
   int64_t n_removed_facts;  /* facts taken out by memstore_remove_fact */
@@ -591,7 +593,7 @@ ms_status memstore_reserve(memstore_t* store, int32_t nq, int32_t k, int32_t nre
 
 /*
  * Test aid (no counterpart in the paper).  The kernels of this library that wait on a barrier (the bulk-async staged
- * copy kernel, the tensor-core scoring kernel) bound every wait and report a time-out - MS_REQ_KERNEL_TIMEOUT in the
+ * copy kernel, the tensor-core scoring kernel, the attention's chunk kernel) bound every wait and report a time-out - MS_REQ_KERNEL_TIMEOUT in the
  * requests' status words, kernel_timeouts in the statistics - instead of hanging.  That path cannot be reached by
  * valid inputs, so this call lets a test reach it without any fault: with mute_producers != 0 the producer role of
  * those kernels issues nothing at all (no copy is ever in flight), and with wait_poll_limit != 0 every wait gives up

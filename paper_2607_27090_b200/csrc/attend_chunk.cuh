@@ -65,6 +65,7 @@ struct ChunkParams {
   float2* part_ml;    // [CTAs][2][kChunkRows]
   AttnCut* cuts;      // [CTAs]
   int32_t* errors;    // [CTAs]: 1 when a wait ran out
+  int32_t* timed_out; // of the store: set to 1 when one did, for whoever asks for no status
   uint32_t spin_limit;
   int mute_producer;
 };
@@ -969,7 +970,10 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
   if (*abort_flag) {
     for (int w = 0; w < 4096; ++w) __nanosleep(256);  // let products and copies that may still be in flight end
   }
-  if (tid == 0) c.errors[blockIdx.x] = *abort_flag;
+  if (tid == 0) {
+    c.errors[blockIdx.x] = *abort_flag;
+    if (*abort_flag) *c.timed_out = 1;
+  }
   if (warp == 20) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(C::kTmemCols) : "memory");

@@ -67,6 +67,8 @@ struct memstore {
   uint32_t* tc_fix_tickets = nullptr;
   uint32_t* tc_n_fixups = nullptr;  // queries the fix-up kernel has redone since creation
   int* tc_error = nullptr;
+  int* attn_timed_out = nullptr;  // 1 when a wait of the attention's chunk kernel ran out
+  bool attn_chunks = false;       // that kernel has been launched
   uint32_t* serve_flag_dev = nullptr;  // memstore_serve_host, early return: device address of the pinned flag word, while its call runs
   uint32_t serve_seq = 0;              // value the flag takes for the current request
   // candidate rows emitted by the filter kernel (see score_gemm.cuh)
@@ -625,7 +627,7 @@ ms_status memstore_create(const memstore_config* config, memstore_t** out) {
             cudaMalloc(&s->facts_d, (size_t)rows * sizeof(FactRec)) == cudaSuccess &&
             cudaMalloc(&s->user_count_d, (size_t)config->n_users * sizeof(int32_t)) == cudaSuccess &&
             cudaMalloc(&s->inv_freq_d, (size_t)(config->head_dim / 2) * sizeof(float)) == cudaSuccess &&
-            cudaMalloc(&s->ctrl, sizeof(InjectCtrl)) == cudaSuccess;
+            cudaMalloc(&s->ctrl, sizeof(InjectCtrl)) == cudaSuccess && cudaMalloc(&s->attn_timed_out, sizeof(int)) == cudaSuccess;
   if (!ok) {
     cudaGetLastError();
     return bail(MS_ERR_OOM);
@@ -639,7 +641,7 @@ ms_status memstore_create(const memstore_config* config, memstore_t** out) {
     f[i] = config->inv_freq_override ? config->inv_freq_override[i] : (float)std::pow(config->rope_theta, -(double)(2 * i) / (double)R);
   ok = cudaMemcpy(s->inv_freq_d, f.data(), f.size() * sizeof(float), cudaMemcpyHostToDevice) == cudaSuccess &&
        cudaMemset(s->user_count_d, 0, (size_t)config->n_users * sizeof(int32_t)) == cudaSuccess &&
-       cudaMemset(s->ctrl, 0, sizeof(InjectCtrl)) == cudaSuccess &&
+       cudaMemset(s->ctrl, 0, sizeof(InjectCtrl)) == cudaSuccess && cudaMemset(s->attn_timed_out, 0, sizeof(int)) == cudaSuccess &&
        cudaEventCreateWithFlags(&s->last_done, cudaEventDisableTiming) == cudaSuccess;
   if (!ok) {
     cudaGetLastError();
@@ -672,6 +674,7 @@ ms_status memstore_destroy(memstore_t* s) {
     cudaFree(s->user_count_d);
     cudaFree(s->inv_freq_d);
     cudaFree(s->ctrl);
+    cudaFree(s->attn_timed_out);
     cudaFree(s->scores);
     cudaFree(s->tickets);
     cudaFree(s->tc_gmax);
@@ -1753,13 +1756,19 @@ ms_status memstore_stats(memstore_t* s, memstore_stats_t* out) {
   out->filter_fixups = 0;
   out->filter_fixup_overflows = 0;
   out->filter_list_queries = out->filter_list_rows = out->filter_list_fallbacks = 0;
+  if (s->attn_chunks) {
+    DeviceGuard g(s->cfg.device);
+    int flag = 0;
+    MS_CUDA(s, cudaMemcpy(&flag, s->attn_timed_out, sizeof flag, cudaMemcpyDeviceToHost));
+    out->kernel_timeouts = flag;
+  }
   if (s->tc_error) {
     DeviceGuard g(s->cfg.device);
     int flags[2] = {0, 0};
     uint32_t fix = 0;
     MS_CUDA(s, cudaMemcpy(flags, s->tc_error, sizeof flags, cudaMemcpyDeviceToHost));
     MS_CUDA(s, cudaMemcpy(&fix, s->tc_n_fixups, sizeof fix, cudaMemcpyDeviceToHost));
-    out->kernel_timeouts = flags[0];
+    out->kernel_timeouts |= flags[0];
     out->filter_fixup_overflows = flags[1];
     out->filter_fixups = fix;
     unsigned long long ls[3] = {0, 0, 0};
@@ -1852,9 +1861,10 @@ ms_status memstore_test_hooks(memstore_t* s, uint32_t wait_poll_limit, int32_t m
   std::lock_guard<std::recursive_mutex> lock(s->mu);
   s->test_spin_limit = wait_poll_limit;
   s->test_mute_producers = mute_producers ? 1 : 0;
-  if (!wait_poll_limit && !mute_producers && s->tc_error) {  // back to normal: forget a time-out that a test provoked
+  if (!wait_poll_limit && !mute_producers) {  // back to normal: forget a time-out that a test provoked
     DeviceGuard g(s->cfg.device);
-    MS_CUDA(s, cudaMemset(s->tc_error, 0, sizeof(int)));
+    MS_CUDA(s, cudaMemset(s->attn_timed_out, 0, sizeof(int)));
+    if (s->tc_error) MS_CUDA(s, cudaMemset(s->tc_error, 0, sizeof(int)));
   }
   return MS_OK;
 }

@@ -1,5 +1,6 @@
 // Host side of the serving calls (memstore_grow_blocks, memstore_release_blocks, memstore_append, memstore_attend); included by
-// memstore.cu inside extern "C".  None of them uses scratch of the store.
+// memstore.cu inside extern "C".  None of them uses scratch of the store
+// (memstore_attend sets one word of it when a wait ran out).
 
 static_assert(kReqTableShort == MS_REQ_BLOCK_TABLE_SHORT && kReqBadBlock == MS_REQ_BAD_BLOCK_ID && kReqPosOverflow == MS_REQ_POSITION_OVERFLOW &&
                   kReqTimeout == MS_REQ_KERNEL_TIMEOUT && kReqBadStart == MS_REQ_BAD_START && kReqNoBlocks == MS_REQ_NO_BLOCKS &&
@@ -266,6 +267,7 @@ static ms_status attend_launch(memstore* s, ChunkParams& c, int64_t max_rows, cu
       chunk_ctas = s->sm_count;
       MS_CUDA(s, launch_dependent(attend_chunk_kernel<D, FP8>, dim3((unsigned)chunk_ctas), dim3(kChunkThreads), (ChunkCfg<D, FP8>::kSmemBytes), st, c));
       s->kernels_launched++;
+      s->attn_chunks = true;
     }
   }
   if (rows) {
@@ -362,6 +364,7 @@ ms_status memstore_attend(memstore_t* s, int32_t layer, const ms_heads* q, int32
   cp.part_ml = (float2*)(base + w.chunk_ml);
   cp.cuts = (AttnCut*)(base + w.chunk_cuts);
   cp.errors = (int32_t*)(base + w.errors);
+  cp.timed_out = s->attn_timed_out;
   cp.spin_limit = s->test_spin_limit;
   cp.mute_producer = s->test_mute_producers;
   const int64_t max_rows = (int64_t)(max_q_len > 0 && max_q_len < n_tokens ? max_q_len : n_tokens) * group;

@@ -68,3 +68,29 @@ def test_attend_random_batches_with_many_units_without_keys(fp8, d, seed):
     x = torch.randn((q_start[-1], hq, d), generator=gen, device=DEV).to(torch.bfloat16)
     check_attend(ms, cache, x, q_start, lens, tables)
     ms.close()
+
+
+# ------------------------------------------------------------------------------------------------ time-outs
+@pytest.mark.parametrize("nreq", [1, 2])
+def test_attend_counts_a_wait_that_ran_out_when_nobody_asks_for_the_status(nreq):
+    q_start, lens = [0, 100, 101][: nreq + 1], [700, 50][:nreq]
+    tables, nb = paged(random.Random(9), lens, 16)
+    cache, gen = fill_cache(1, nb, 16, 2, 128, False, "NHD", 9)
+    ms = store(2, 128)
+    q = torch.randn((q_start[-1], 8, 128), generator=gen, device=DEV).to(torch.bfloat16)
+    assert ms.stats()["kernel_timeouts"] == 0
+    ms.attend(0, q, cache, i32(q_start), i32(lens), tables)
+    torch.cuda.synchronize()
+    assert ms.stats()["kernel_timeouts"] == 0
+    ms.test_hooks(wait_poll_limit=3000, mute_producers=True)
+    ms.attend(0, q, cache, i32(q_start), i32(lens), tables)
+    torch.cuda.synchronize()
+    assert ms.stats()["kernel_timeouts"] == 1
+    ms.attend(0, q[-1:], cache, i32([0, 1]), i32([50]), tables[-1:])  # (no kernel with waits of its own: the word stays)
+    torch.cuda.synchronize()
+    assert ms.stats()["kernel_timeouts"] == 1
+    ms.test_hooks()
+    assert ms.stats()["kernel_timeouts"] == 0
+    check_attend(ms, cache, q, q_start, lens, tables)
+    assert ms.stats()["kernel_timeouts"] == 0
+    ms.close()
