@@ -485,8 +485,8 @@ ms_status memstore_append(memstore_t* store, int32_t layer, const ms_heads* q, i
  * them): row i is at position p = seq_len - n_new + i and attends to the keys at positions 0 .. p.  With g = n_q_heads /
  * n_kv_heads query heads per K/V head, for query head h:
  *   s_j = scale * q . K[j][h / g],  out = sum_j exp(s_j - lse) V[j][h / g],  lse = ln sum_j exp(s_j)      (j = 0 .. p)
- * Scores, maxima, sums and accumulators are fp32; the weights are rounded to the type of the matrix product (bf16, or fp16
- * with an 8-bit cache).  A row without keys (p < 0) gives zeros and lse = -infinity.  Whatever the cache holds behind a
+ * Scores, maxima, sums and accumulators are fp32; the weights exp(s_j - max) are rounded to the type of the matrix product: bf16, or
+ * fp16 with an 8-bit cache, where a weight below 2^-18 of the row's largest may be off by 2^-29 of it instead of 2^-12 of itself.  A row without keys (p < 0) gives zeros and lse = -infinity.  Whatever the cache holds behind a
  * row's last key, NaN and infinities included, does not reach that row.
  *   q, out        bf16 [n_tokens][n_q_heads][head_dim] (rotated queries); rows outside every request are neither read nor written.
  *                 out must not overlap q unless it is q itself (same base and strides)

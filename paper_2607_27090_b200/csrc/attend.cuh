@@ -248,6 +248,11 @@ struct AttnCfg {
   // product's inner dimension is free as long as q follows it)
   static constexpr int kKB = D >= 64 ? 16 : D / 4;
   static constexpr int kSPB = kKB / 4;
+  // Weights are formed as 2^(score - maximum + kLift) (the statistics keep maximum - kLift).  fp16 weights of at most 1 would
+  // use half of the type's range: one below 2^-14 would lose bits and one below 2^-25 would vanish, and the many small weights of a long
+  // context behind one large score would be gone while the sum counts them.  Lifted by 14 the largest is 2^14 (65,504 is the limit) and
+  // the step of the smallest 2^-38 of it.  bf16 has the range of fp32.
+  static constexpr float kLift = FP8 ? 14.f : 0.f;
 };
 
 // Byte offset of chunk c of row r in a warp's K or V tile; the chunks are permuted so that the lanes of a matrix load hit
@@ -494,7 +499,7 @@ __global__ void __launch_bounds__(kAttnThreads, AttnCfg<D, FP8>::kCtasPerSm) att
       x1 = fmaxf(x1, __shfl_xor_sync(0xffffffffu, x1, 1));
       x0 = fmaxf(x0, __shfl_xor_sync(0xffffffffu, x0, 2));
       x1 = fmaxf(x1, __shfl_xor_sync(0xffffffffu, x1, 2));
-      const float n0 = fmaxf(m0, x0 * sc0), n1 = fmaxf(m1, x1 * sc1);
+      const float n0 = fmaxf(m0, fmaf(x0, sc0, -C::kLift)), n1 = fmaxf(m1, fmaf(x1, sc1, -C::kLift));
       if (__any_sync(0xffffffffu, n0 != m0 || n1 != m1)) {
         // (a maximum of minus infinity: nothing has been summed yet, any finite stand-in gives weights of zero)
         const float a0 = n0 == -INFINITY ? 1.f : ex2(m0 - n0), a1 = n1 == -INFINITY ? 1.f : ex2(m1 - n1);
@@ -576,7 +581,8 @@ __global__ void __launch_bounds__(kAttnThreads, AttnCfg<D, FP8>::kCtasPerSm) att
         continue;
       }
 
-      // ---- O += P V (P rounded to the type of V)
+      // ---- O += P V.  P is rounded to the type of the product (half a step is 2^-9 of a bf16 weight, 2^-12 of an fp16 one): the matrix
+      // instructions take 16-bit operands, and V has no more bits than that itself.  l holds the unrounded weights.
 #pragma unroll
       for (int gr = 0; gr < C::kGroups; ++gr) {
         const float* wa = s[2 * gr];

@@ -22,8 +22,8 @@
 // bf16): none: 2,048 tokens of 2,048 131 us, 512 of 512 39 us, 512 of 4,096 64 us, 64 of 32,000 70 us; three: 83, 30, 60, 65;
 // four: 82, 30, 59, 63; five: 76, 33, 58, 61 (and an 8-bit cache 69 instead of 67).
 // Running maximum: the weights are formed with the maximum of the tiles before; no maximum is looked for unless the sum of a thread's 64
-// weights passes 2^14, when the row takes a new maximum, its weights are formed again and its accumulator is rescaled.  fp32 sums, and
-// weights of up to 2^14 in bf16 or fp16, lose nothing by that.
+// weights passes 2^14 (8-bit cache: 61,440), when the row takes a new maximum, its weights are formed again and its accumulator is
+// rescaled.  fp32 sums, and weights of that size in bf16 or fp16, lose nothing by that.
 // Every wait is bounded; when one runs out the CTA reports it, frees its tensor memory and leaves.
 #pragma once
 #include "attend.cuh"
@@ -40,7 +40,6 @@ static_assert(4 * kChunkRegsWeights + kChunkRegsLoads + kChunkRegsIssue <= 6 * 8
 constexpr int kChunkUnitCost = 4;    // places on the line of tiles that stand for the set-up and the end of a unit
 constexpr int kChunkMaskRing = 8;     // (a tile's masks are read at most three tiles after the loader wrote them)
 constexpr uint32_t kChunkSpinLimit = 1u << 26;  // polls (a second or more)
-constexpr float kChunkMaxSum = 16384.f;  // sum of 64 weights (and so a weight) that is tolerated without taking a new maximum
 
 template <int D, bool FP8>
 struct ChunkCfg {
@@ -54,6 +53,12 @@ struct ChunkCfg {
   static_assert(kSmemBytes <= 232448, "shared memory of a CTA");
   static constexpr int kColO = 2 * kChunkKeys;                       // TMEM: S0, S1 (128 columns each), O0, O1 (D columns each)
   static constexpr int kTmemCols = 512;
+  // Sum of 64 weights (and so a weight) that is tolerated without taking a new maximum, and what the exponents are lifted by when one is
+  // taken (see AttnCfg::kLift).  fp16 weights stay below 65,504; what the lift takes from the room above it is paid in new maxima where
+  // scores spread: 512 tokens of 4,096 in an 8-bit cache (32/8 heads of 128, scores of standard deviation 1 / 2 / 3 / 5) take 66.7 / 66.7 /
+  // 67.8 / 80.5 us without a lift, 66.6 / 66.8 / 71.6 / 82.8 with 4, 66.6 / 67.4 / 77.0 / 84.1 with 6, 66.6 / 71.7 / 82.0 / 85.0 with 8.
+  static constexpr float kMaxSum = FP8 ? 61440.f : 16384.f;
+  static constexpr float kLift = FP8 ? 4.f : 0.f;
 };
 
 struct ChunkParams {
@@ -842,7 +847,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
             // (a row's maximum changes by its own scores alone, so that a row does not depend on its neighbours)
             mx = pair_join(mx, [](float a, float b) { return fmaxf(a, b); });
             const bool own = j == 0 || pair_join(renew ? 1.f : 0.f, [](float a, float b) { return fmaxf(a, b); }) != 0.f;
-            const float n = own ? fmaxf(m, mx * sc) : m;
+            const float n = own ? fmaxf(m, fmaf(mx, sc, -C::kLift)) : m;
             const float f = n == -INFINITY || m == n ? 1.f : ex2(m - n);
             if (j > 0) {
               // the accumulator holds the tiles before this one (the commit that signalled these scores follows their product)
@@ -864,7 +869,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
             pair_sync(pair);
             break;
           }
-          renew = sum > kChunkMaxSum || m == -INFINITY;
+          renew = sum > C::kMaxSum || m == -INFINITY;
           again = pair_any(pair, !ok || renew);
           if (!again) break;
           stop = pair_any(pair, !ok);

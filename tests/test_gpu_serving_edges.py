@@ -94,3 +94,49 @@ def test_attend_counts_a_wait_that_ran_out_when_nobody_asks_for_the_status(nreq)
     check_attend(ms, cache, q, q_start, lens, tables)
     assert ms.stats()["kernel_timeouts"] == 0
     ms.close()
+
+
+# ------------------------------------------------------------------------------------------------ long tails of small weights
+@pytest.mark.parametrize("d,n", [(16, 1), (128, 1), (128, 3), (256, 2), (64, 70), (128, 70), (128, 300)])
+@pytest.mark.parametrize("drop", [12.0, 16.6, 18.3])
+def test_attend_small_weights_behind_large_ones_count_in_an_8_bit_cache(d, n, drop):
+    """Eight keys far above 8,000 others, whose weights are 2^-17 to 2^-26 of theirs: the others decide the output, because the large
+    keys' values are zero.  300 requests over the same blocks, so that whole units stay in one CTA.
+
+    Bound: an fp16 weight is off by 2^-11 of itself (2^-12 would do) or, below 2^-14, by 2^-25. The exponents are lifted by 14 in the
+    kernel for few rows and by 4 in the one for chunks, so the row's largest weight is at least 2^14 or 2^4, and that is 2^-39 or 2^-29 of
+    it a key. Beside it the fp32 errors of a score (ds) and the rounding of the output."""
+    hk, hq, bs, len_, nreq = 1, 4, 16, 8000 + n, 300
+    tables, nb = paged(random.Random(d + n), [len_], bs)
+    cache, gen = fill_cache(1, nb, bs, hk, d, True, "NHD", 3, k_scale=1.0, v_scale=0.03)
+    # keys: the first coordinate carries the score, the others are noise that only small elements of q look at
+    k = torch.randn((nb, bs, hk, d), generator=gen, device=DEV)
+    v = 8.0 + 4.0 * torch.rand((nb, bs, hk, d), generator=gen, device=DEV)
+    k[..., 0] = 0.0
+    for page in tables[0, :8].tolist():  # (a key of every warp's share of a tile)
+        k[page, 5] = 0.0
+        k[page, 5, 0, 0] = 16.0
+        v[page, 5] = 0.0
+    cache.k[0], cache.v[0] = k.to(ref.F8).view(torch.uint8), v.to(ref.F8).view(torch.uint8)
+    q = (0.02 * torch.randn((n, hq, d), generator=gen, device=DEV)).to(torch.bfloat16)
+    q[..., 0] = drop / 16.0
+    ms = store(hk, d)
+    out, lse, _ = ms.attend(0, q.repeat(nreq, 1, 1), cache, i32(range(0, n * nreq + 1, n)), i32([len_] * nreq), tables.repeat(nreq, 1), scale=1.0,
+                            want_lse=True)  # fmt: skip
+    step = 2.0**-29 if n >= 70 else 2.0**-39
+    out, lse = out.unflatten(0, (nreq, n)).double(), lse.unflatten(0, (nreq, n)).double()
+    kk, vv, _ = ref.cache_rows(cache, 0, tables[0], len_, nb)
+    see = torch.arange(len_, device=DEV)[None] <= torch.arange(len_ - n, len_, device=DEV)[:, None]
+    for h in range(hq):
+        s = torch.where(see, q[:, h].double() @ kk[:, 0].T, -math.inf)
+        m = s.amax(1, keepdim=True)
+        w = torch.exp(s - m)
+        l = w.sum(1, keepdim=True)
+        want = (w @ vv[:, 0]) / l
+        ds = (q[:, h].double().abs() @ kk[:, 0].abs().T).amax() * (d + 8) * ref.U_F32 + 2.0**-20
+        tol = 2.0**-8 * want + (2.0**-11 + 3 * ds) * want + step * (see.double() @ vv[:, 0]) / l
+        err = (out[:, :, h] - want).abs().amax(0)
+        assert (err <= tol).all(), (h, (err / tol).max().item(), (err / want).max().item())
+        want_lse = (m + torch.log(l))[:, 0]
+        assert ((lse[:, :, h] - want_lse).abs().amax(0) <= 2 * ds + 4 * ref.U_F32 * want_lse.abs() + 2.0**-20).all()
+    ms.close()
