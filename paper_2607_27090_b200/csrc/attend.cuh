@@ -63,7 +63,7 @@ struct AttendParams {
   int32_t max_rows;  // requests with more rows per K/V head are served by the kernel for chunks
   int32_t min_share; // fewest tiles a CTA takes
   int32_t tile_shift; // log2 of the keys of a tile
-  int32_t beside;    // the kernel before this one is the same call's chunk kernel
+  unsigned long long* gate;  // not nullptr: the kernel before this one is the same call's chunk kernel (see gate_open)
   float* part_o;     // [CTAs][2][kAttnRows][head_dim]
   float2* part_ml;   // [CTAs][2][kAttnRows]
   AttnCut* cuts;     // [CTAs]
@@ -227,6 +227,26 @@ __device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
+// The rows kernel of a call starts beside the call's chunk kernel. Everything before the call has completed by then, since every CTA of
+// the chunk kernel has waited for it before it lets this grid start - but what those kernels wrote is visible here only through a wait of
+// this grid's own, which would last until the chunk kernel ends, or through a chain from a thread that has waited: CTA 0 of the chunk
+// kernel stores kGateOpen with release semantics behind its wait and before its trigger, a thread of each CTA here loads it with acquire
+// semantics, and the block's barrier passes it on.  The word is in the workspace and is cleared by the call's join kernel.  Where it is
+// not found open (it always should be), the CTA waits for the chunk kernel to end, which is always right.
+constexpr unsigned long long kGateOpen = 0x6761746520697321ull;
+constexpr int kGatePolls = 256;
+__device__ __forceinline__ void open_gate(unsigned long long* gate) {
+  asm volatile("st.release.gpu.global.u64 [%0], %1;" ::"l"(gate), "l"(kGateOpen) : "memory");
+}
+__device__ __forceinline__ bool gate_open(const unsigned long long* gate) {
+  for (int i = 0; i < kGatePolls; ++i) {
+    unsigned long long v;
+    asm volatile("ld.acquire.gpu.global.u64 %0, [%1];" : "=l"(v) : "l"(gate) : "memory");
+    if (v == kGateOpen) return true;
+  }
+  return false;
+}
+
 template <int D, bool FP8>
 struct AttnCfg {
   // Keys of a warp in a tile: 32 while rows are at most 128 bytes.  The work around the products (maximum, waits, table look-ups) is per
@@ -276,9 +296,9 @@ __global__ void __launch_bounds__(kAttnThreads, AttnCfg<D, FP8>::kCtasPerSm) att
   __shared__ int64_t s_warp[32], s_found[2];
   __shared__ float s_m[kAttnWarps][kAttnRows], s_l[kAttnWarps][kAttnRows];
   __shared__ uint32_t s_mask[kAttnWarps][C::kStages];
-  // The chunk kernel of the same call has waited for everything before the call when it let this grid start, and the two touch
-  // different rows: this one need not wait for it to begin, only to end (so that whatever waits for this grid has waited for both).
-  if (!p.beside) grid_dependency_wait();
+  // (beside the chunk kernel of its call this one need not wait for that kernel to begin, only to end: the two touch different rows, and
+  // whatever waits for this grid has then waited for both)
+  if (!p.gate || !__syncthreads_and(threadIdx.x != 0 || gate_open(p.gate))) grid_dependency_wait();
   grid_launch_dependents();
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t4 = lane & 3;
 
@@ -699,7 +719,7 @@ __global__ void __launch_bounds__(kAttnThreads, AttnCfg<D, FP8>::kCtasPerSm) att
       } while (r >= 0 && attn_cost(p, rq) == 0);
     }
   }
-  if (p.beside) grid_dependency_wait();
+  if (p.gate) grid_dependency_wait();
 }
 
 // Joins the parts of the unit that the border in front of CTA b's share cuts, if it is the unit's first border.

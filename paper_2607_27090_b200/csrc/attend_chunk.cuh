@@ -348,6 +348,10 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_async_smem();
+    if (p.gate && blockIdx.x == 0) {
+      grid_dependency_wait();
+      open_gate(p.gate);
+    }
   }
   grid_dependency_wait();  // (before tensor memory is taken: a kernel before this one may still hold it)
   grid_launch_dependents();
@@ -1023,6 +1027,7 @@ __global__ void __launch_bounds__(kCombineThreads, 2) attend_join_kernel(const C
                                                                       const int rows_ctas, const int rows_joins) {
   grid_launch_dependents();
   grid_dependency_wait();
+  if (c.a.gate && blockIdx.x == 0 && threadIdx.x == 0) *c.a.gate = 0;
   int b = blockIdx.x;
   if (b < chunk_joins * pieces) {
     const int cta = nth_cut(c.cuts, chunk_ctas, chunk_joins, b / pieces);

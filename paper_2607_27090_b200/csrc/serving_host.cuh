@@ -202,9 +202,9 @@ ms_status memstore_append(memstore_t* s, int32_t layer, const ms_heads* q, int32
 static int chunk_min_rows(int64_t units, int sm_count) { return units <= sm_count / 2 ? 2 * kAttnRows : kAttnRows; }
 
 // The workspace: unfinished rows of the rows kernel (kAttnMaxCtasPerSm CTAs per SM at most) and their statistics, then those of the chunk kernel
-// (one CTA per SM) and its error words.  It depends on the GPU and head_dim alone.
+// (one CTA per SM), its error words and the gate between the two.  It depends on the GPU and head_dim alone.
 struct AttendLayout {
-  size_t rows_o, rows_ml, rows_cuts, chunk_o, chunk_ml, chunk_cuts, errors, bytes;
+  size_t rows_o, rows_ml, rows_cuts, chunk_o, chunk_ml, chunk_cuts, errors, gate, bytes;
 };
 static bool attend_has_chunks(int head_dim) { return head_dim == 64 || head_dim == 128; }
 static AttendLayout attend_layout(const memstore* s) {
@@ -224,6 +224,7 @@ static AttendLayout attend_layout(const memstore* s) {
     w.chunk_ml = take(sms * 2 * kChunkRows * 8);
     w.chunk_cuts = take(sms * sizeof(AttnCut));
     w.errors = take(sms * 4);
+    w.gate = take(8);
   }
   w.bytes = at;
   return w;
@@ -256,7 +257,7 @@ static ms_status attend_launch(memstore* s, ChunkParams& c, int64_t max_rows, cu
   const bool rows = !chunks || p.nreq > 1;
   c.min_rows = rows ? min_rows : 0;
   p.max_rows = chunks ? c.min_rows : 0x7fffffff;
-  p.beside = chunks;
+  if (!chunks || !rows) p.gate = nullptr;  // (with both kernels there is a unit, so a join kernel too, which clears the word)
   c.step_tok = kChunkRows / p.group;
   c.step_sub = kChunkRows % p.group;
   const int64_t all_rows = (int64_t)p.n_tokens * p.group;
@@ -364,6 +365,7 @@ ms_status memstore_attend(memstore_t* s, int32_t layer, const ms_heads* q, int32
   cp.part_ml = (float2*)(base + w.chunk_ml);
   cp.cuts = (AttnCut*)(base + w.chunk_cuts);
   cp.errors = (int32_t*)(base + w.errors);
+  p.gate = (unsigned long long*)(base + w.gate);
   cp.timed_out = s->attn_timed_out;
   cp.spin_limit = s->test_spin_limit;
   cp.mute_producer = s->test_mute_producers;

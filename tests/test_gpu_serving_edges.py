@@ -140,3 +140,64 @@ def test_attend_small_weights_behind_large_ones_count_in_an_8_bit_cache(d, n, dr
         want_lse = (m + torch.log(l))[:, 0]
         assert ((lse[:, :, h] - want_lse).abs().amax(0) <= 2 * ds + 4 * ref.U_F32 * want_lse.abs() + 2.0**-20).all()
     ms.close()
+
+
+# ------------------------------------------------------------------------------------------------ calls back to back
+@pytest.mark.parametrize("fp8,d", [(False, 128), (True, 128), (False, 64)])
+def test_layers_back_to_back_read_what_the_calls_before_them_wrote(fp8, d):
+    """Mixed batches (both attention kernels) layer after layer on one stream, nothing waited for in between: lengths, tables, queries and
+    cache rows of a call are written by the calls just before it, into buffers that the call before read.  The same steps with a
+    synchronise after every call give the same bits; eagerly and from a replayed graph."""
+    L, hk, hq, bs, steps = 4, 4, 16, 16, 3
+    rng = random.Random(d + fp8)
+    new = [[rng.choice([1, 1, 2, rng.randint(30, 200)]) for _ in range(20)] for _ in range(steps)]
+    T = max(sum(n) for n in new)
+    total = [sum(x) for x in zip(*new)]
+    width = max(-(-t // bs) for t in total) + 1
+    nb = sum(-(-t // bs) for t in total) + 5
+    gen = torch.Generator(device=DEV).manual_seed(11)
+    qkv = torch.randn((steps, L, T, (hq + 2 * hk) * d), generator=gen, device=DEV).to(torch.bfloat16)
+    news = [i32(n) for n in new]
+    ms = store(hk, d, L)
+
+    def run(wait, graph=False):
+        from paper_2607_27090_b200.memstore import GrownBlocks, PagedCache
+
+        cache = PagedCache.allocate(L, nb, bs, hk, d, DEV, fp8=fp8, k_scale=0.02, v_scale=0.03)
+        tables, free, taken = i32(np.full((20, width), -1)), i32(rng_ids), i32([0])
+        lens = i32([0] * 20)
+        g = GrownBlocks(i32([0] * 21), lens, i32([0] * T), torch.zeros(T, dtype=torch.int64, device=DEV), taken, i32([0] * 20))
+        buf, q, out = torch.zeros_like(qkv[0, 0]), torch.zeros((T, hq, d), dtype=torch.bfloat16, device=DEV), torch.zeros((steps, L, T, hq, d), dtype=torch.bfloat16, device=DEV)
+        workspace = torch.full((ms.attend_workspace_bytes(),), 255, dtype=torch.uint8, device=DEV)  # (any contents will do)
+
+        def body():
+            for s in range(steps):
+                ms.grow_blocks(lens, news[s], tables, cache, free, taken, T, out=g)
+                for layer in range(L):
+                    buf.copy_(qkv[s, layer])
+                    h = buf.unflatten(1, (hq + 2 * hk, d))
+                    ms.append(layer, h[:, :hq], h[:, hq : hq + hk], h[:, hq + hk :], g.positions, g.slots, cache, q_out=q)
+                    ms.attend(layer, q, cache, g.q_start, g.seq_lens, tables, out=out[s, layer], workspace=workspace)
+                    if wait:
+                        torch.cuda.synchronize()
+
+        if graph:
+            cg = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(cg):
+                body()
+            for t, v in ((tables, -1), (taken, 0), (lens, 0)):
+                t.fill_(v)
+            cg.replay()
+        else:
+            body()
+        torch.cuda.synchronize()
+        return out
+
+    rng_ids = list(range(nb))
+    rng.shuffle(rng_ids)
+    want = run(True)
+    assert want.float().abs().amax(dim=(2, 3, 4)).min() > 0
+    for _ in range(4):
+        assert torch.equal(run(False), want)
+    assert torch.equal(run(False, graph=True), want)
+    ms.close()
