@@ -659,10 +659,17 @@ class MemStore:
             self._workspace_bytes = int(self._lib.memstore_attend_workspace(self._h))
         return self._workspace_bytes
 
+    def _capturing(self) -> bool:
+        """Whether the current stream of the store's device is being captured (torch asks about the current device's)."""
+        if torch._C._cuda_getDevice() == self._index:
+            return torch._C._cuda_isCurrentStreamCapturing()
+        with torch.cuda.device(self._index):
+            return torch._C._cuda_isCurrentStreamCapturing()
+
     def _workspace(self, raw: int, stream) -> torch.Tensor:
         """Workspace of an attend call: calls on one stream follow one another and share one; a capture gets its own from the
         graph's pool (its replays may run beside anything), and so does a stream given by the caller."""
-        if stream is not None or torch._C._cuda_isCurrentStreamCapturing():
+        if stream is not None or self._capturing():
             return self._empty(stream, (self.attend_workspace_bytes(), torch.uint8))[0]
         w = self._workspaces.get(raw)
         if w is None:
