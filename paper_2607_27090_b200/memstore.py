@@ -668,20 +668,24 @@ class MemStore:
 
     def _workspace(self, raw: int, stream) -> torch.Tensor:
         """Workspace of an attend call: calls on one stream follow one another and share one; a capture gets its own from the
-        graph's pool (its replays may run beside anything), and so does a stream given by the caller."""
+        graph's pool (its replays may run beside anything), and so does a stream given by the caller.  A workspace is kept for the
+        default stream and torch's own, which live as long as the process: another library's stream may be destroyed with work in flight
+        and its handle come back for a new one."""
         if stream is not None or self._capturing():
             return self._empty(stream, (self.attend_workspace_bytes(), torch.uint8))[0]
         w = self._workspaces.get(raw)
         if w is None:
-            w = self._workspaces[raw] = self._empty(None, (self.attend_workspace_bytes(), torch.uint8))[0]
+            w = self._empty(None, (self.attend_workspace_bytes(), torch.uint8))[0]
+            if raw == 0 or torch.cuda.current_stream(self._index).stream_id != raw:  # (the id of an external stream is its handle)
+                self._workspaces[raw] = w
         return w
 
     def attend(self, layer: int, q, cache: PagedCache, q_start, seq_lens, block_tables, scale: float = 0.0, max_q_len: int = 0, out=None,
                want_lse: bool = False, out_lse=None, out_status=None, workspace=None, stream=None):  # fmt: skip
         """Attention of the new tokens ``q`` [T, n_q_heads, d] (rows ``q_start[r] .. q_start[r+1] - 1`` are the last tokens
         of request r's ``seq_lens[r]`` cached ones) over ``layer`` of the cache.  Returns (out, lse or None, out_status).
-        ``workspace``: a uint8 tensor of ``attend_workspace_bytes()``; by default the store keeps one per current stream, and
-        captures and calls with ``stream`` get one of their own."""
+        ``workspace``: a uint8 tensor of ``attend_workspace_bytes()``; by default the store keeps one for
+        each of torch's streams that is current in a call; captures, calls with ``stream`` and external streams get one of their own."""
         (T, n_q, _), nreq, i32, ptr = q.shape, seq_lens.shape[0], torch.int32, self._ptr
         if block_tables.dim() != 2 or block_tables.shape[0] != nreq:
             raise ValueError(f"block_tables must have shape ({nreq}, max_blocks), got {tuple(block_tables.shape)}")

@@ -43,3 +43,15 @@ def test_a_capture_on_the_stores_device_gets_a_workspace_of_its_own_whichever_de
     assert s._workspace(0, None) is not kept
     m.capturing, m.device = {0}, 0  # a capture on another device has nothing to do with this store
     assert s._workspace(0, None) is kept
+
+
+def test_workspaces_are_kept_for_the_streams_that_stay(monkeypatch):
+    m, s = Machine(monkeypatch), bare_store()
+    ids = {0: 0, 0x7F00AA10: 3, 0x7F00BB20: 0x7F00BB20}  # handle -> id: the default stream, one of torch's pool, an external one
+    current = {}
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: current["stream"])
+    for handle, stays in ((0, True), (0x7F00AA10, True), (0x7F00BB20, False)):
+        current["stream"] = type("Stream", (), {"stream_id": ids[handle]})
+        first = s._workspace(handle, None)
+        assert (s._workspace(handle, None) is first) == stays and (handle in s._workspaces) == stays
+    assert m.device == 0

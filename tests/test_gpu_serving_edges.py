@@ -201,3 +201,32 @@ def test_layers_back_to_back_read_what_the_calls_before_them_wrote(fp8, d):
         assert torch.equal(run(False), want)
     assert torch.equal(run(False, graph=True), want)
     ms.close()
+
+
+# ------------------------------------------------------------------------------------------------ workspaces
+def test_attend_on_an_external_stream_keeps_no_workspace_for_it():
+    import ctypes
+
+    driver = ctypes.CDLL("libcuda.so.1")
+    lens, q_start = [700, 50], [0, 100, 101]
+    tables, nb = paged(random.Random(9), lens, 16)
+    cache, gen = fill_cache(1, nb, 16, 2, 128, False, "NHD", 9)
+    ms = store(2, 128)
+    q = torch.randn((101, 8, 128), generator=gen, device=DEV).to(torch.bfloat16)
+    qs, ln = i32(q_start), i32(lens)
+    want, _, _ = ms.attend(0, q, cache, qs, ln, tables)
+    torch.cuda.synchronize()
+    kept = len(ms._workspaces)
+    with torch.cuda.stream(torch.cuda.Stream()):
+        assert torch.equal(ms.attend(0, q, cache, qs, ln, tables)[0], want)
+    assert len(ms._workspaces) == kept + 1  # one of torch's own streams
+    torch.cuda.synchronize()
+    for _ in range(3):
+        handle = ctypes.c_void_p()
+        assert driver.cuStreamCreate(ctypes.byref(handle), 1) == 0
+        with torch.cuda.stream(torch.cuda.ExternalStream(handle.value)):
+            outs = [ms.attend(0, q, cache, qs, ln, tables)[0] for _ in range(3)]
+        torch.cuda.synchronize()
+        assert driver.cuStreamDestroy_v2(handle) == 0
+        assert all(torch.equal(o, want) for o in outs) and len(ms._workspaces) == kept + 1
+    ms.close()
