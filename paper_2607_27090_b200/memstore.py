@@ -328,6 +328,7 @@ class MemStore:
         if getattr(self, "_h", None) is not None and self._h.value:
             self._lib.memstore_destroy(self._h)
             self._h = C.c_void_p()
+            self._workspaces.clear()
 
     def __del__(self):
         try:

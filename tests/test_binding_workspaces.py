@@ -1,4 +1,6 @@
 """CPU-only: which attention workspace the binding uses (the device calls are replaced; nothing is launched)."""
+import ctypes
+
 import torch
 
 from paper_2607_27090_b200 import memstore as M
@@ -55,3 +57,15 @@ def test_workspaces_are_kept_for_the_streams_that_stay(monkeypatch):
         first = s._workspace(handle, None)
         assert (s._workspace(handle, None) is first) == stays and (handle in s._workspaces) == stays
     assert m.device == 0
+
+
+def test_close_gives_the_workspaces_back(monkeypatch):
+    m, s = Machine(monkeypatch), bare_store()
+    destroyed = []
+    s._h, s._lib = ctypes.c_void_p(1), type("Lib", (), {"memstore_destroy": staticmethod(lambda h: destroyed.append(h.value))})
+    s._workspace(0, None)
+    assert s._workspaces
+    s.close()
+    assert destroyed == [1] and not s._workspaces
+    s.close()
+    assert destroyed == [1] and m.device == 0
