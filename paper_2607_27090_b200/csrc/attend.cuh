@@ -218,6 +218,11 @@ __device__ __forceinline__ float ex2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+// The factor of a row's scores when the row was scaled by the inverse of the power of two with this exponent field; never zero or infinite
+// (minus infinity, a masked score, times zero and zero times infinity would be NaN).
+__device__ __forceinline__ float attn_scale(float scale_log2, int field) {
+  return fminf(fmaxf(scale_log2 * __uint_as_float((uint32_t)field << 23), 1.17549435e-38f), 3.40282347e+38f);
+}
 // four e4m3 codes as four fp16 (exact), two to a word
 __device__ __forceinline__ void e4m3x4_half2(uint32_t u, uint32_t& lo, uint32_t& hi) {
   asm("{ .reg .b16 a, b; mov.b32 {a, b}, %2; cvt.rn.f16x2.e4m3x2 %0, a; cvt.rn.f16x2.e4m3x2 %1, b; }" : "=r"(lo), "=r"(hi) : "r"(u));
@@ -423,8 +428,8 @@ __global__ void __launch_bounds__(kAttnThreads, AttnCfg<D, FP8>::kCtasPerSm) att
         // exponent field of the maximum -> the fields of the power of two, 127 + 14 - (field - 127), and of its inverse
         const int ea = min(max(268 - (int)(__float_as_uint(ma) >> 23), 13), 227), eb = min(max(268 - (int)(__float_as_uint(mb) >> 23), 13), 227);
         const float fa = __uint_as_float((uint32_t)ea << 23), fb = __uint_as_float((uint32_t)eb << 23);
-        sc0 *= __uint_as_float((uint32_t)(254 - ea) << 23);
-        sc1 *= __uint_as_float((uint32_t)(254 - eb) << 23);
+        sc0 = attn_scale(sc0, 254 - ea);
+        sc1 = attn_scale(sc1, 254 - eb);
 #pragma unroll
         for (int k = 0; k < kSteps; ++k) {
           qf[k][0] = pack_half(bf16lo(qf[k][0]) * fa, bf16hi(qf[k][0]) * fa);

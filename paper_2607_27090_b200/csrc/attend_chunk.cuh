@@ -786,7 +786,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
         ok = chunk_wait(&s_full[h], s_ph, abort_flag, limit);
         s_ph ^= 1u;
         tc_fence_after();
-        if (FP8 && j == 0) sc = p.scale_log2 * __uint_as_float((uint32_t)s_qexp[row] << 23);
+        if (FP8 && j == 0) sc = attn_scale(p.scale_log2, s_qexp[row]);
         const int k0 = (t0 + j) * kChunkKeys + part * 64;
         const uint2 there = *reinterpret_cast<const uint2*>(s_masks + mask_at * 4 + part * 2);
         if (v_causal) look_at_v();  // (of the tile before: its product with V was issued before these scores)

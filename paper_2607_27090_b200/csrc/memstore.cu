@@ -4,6 +4,7 @@
 #include "../../include/memstore.h"
 
 #include <atomic>
+#include <cfloat>
 #include <chrono>
 #include <cmath>
 #include <cstdarg>

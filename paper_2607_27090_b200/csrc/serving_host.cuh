@@ -350,7 +350,8 @@ ms_status memstore_attend(memstore_t* s, int32_t layer, const ms_heads* q, int32
   p.block_size = cache->block_size;
   p.block_shift = (p.block_size & (p.block_size - 1)) ? -1 : __builtin_ctz((unsigned)p.block_size);
   const double sc = scale > 0.f ? (double)scale : 1.0 / std::sqrt((double)c.head_dim);
-  p.scale_log2 = (float)(sc * 1.4426950408889634 * (fp8 ? (double)cache->k_scale : 1.0));
+  // (a scale of zero would turn the minus infinity of a masked score into NaN, an infinite one a score of zero)
+  p.scale_log2 = (float)std::min(std::max(sc * 1.4426950408889634 * (fp8 ? (double)cache->k_scale : 1.0), (double)FLT_MIN), (double)FLT_MAX);
   p.v_scale = fp8 ? cache->v_scale : 1.f;
   p.lse = out_lse;
   p.status = out_status;

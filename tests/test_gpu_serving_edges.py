@@ -203,6 +203,37 @@ def test_layers_back_to_back_read_what_the_calls_before_them_wrote(fp8, d):
     ms.close()
 
 
+# ------------------------------------------------------------------------------------------------ scales
+@pytest.mark.parametrize("n", [3, 100])
+@pytest.mark.parametrize("fp8", [False, True])
+def test_attend_scales_at_the_ends_of_their_range(fp8, n):
+    """Scales (and 8-bit scales) whose product with the powers of two inside leaves fp32: far too small ones give every key a row sees the
+    same weight, far too large ones give the key with the largest score all of it."""
+    hk, hq, d, len_ = 1, 4, 128, 300
+    tables, nb = paged(random.Random(2), [len_], 16)
+    cache, gen = fill_cache(1, nb, 16, hk, d, fp8, "NHD", 5, k_scale=1.0)
+    q = torch.randn((n, hq, d), generator=gen, device=DEV).to(torch.bfloat16)
+    q[0, 0] = 0.0  # (a row of zeros scales by the largest power of two)
+    q[1, 1] *= 2.0**-90
+    ms = store(hk, d)
+    qs, ln = i32([0, n]), i32([len_])
+    k, v, _ = ref.cache_rows(cache, 0, tables[0], len_, nb)
+    seen = torch.arange(len_ - n + 1, len_ + 1, device=DEV).double()
+    mean = torch.cumsum(v[:, 0], 0)[len_ - n :] / seen[:, None]
+    for scale, k_scale in ((1e-36, 1.0), (1.0e-44, 1.0)) + (((1e-30, 1e-20), (1e-20, 1e-38)) if fp8 else ()):
+        cache.k_scale = k_scale
+        out, lse, _ = ms.attend(0, q, cache, qs, ln, tables, scale=scale, want_lse=True)
+        # weights of one: fp32 sums of at most 300 values of magnitude 14 (0.03 * 448), one rounding to bf16
+        assert ((out.double() - mean[:, None]).abs() <= 2.0**-8 * mean[:, None].abs() + 300 * 14 * 2.0**-24).all()
+        assert ((lse.double() - seen.log()[:, None]).abs() <= 2.0**-18).all()
+    # every score of one tile's rows is infinite or zero: the row of zeros still sees all keys alike
+    cache.k_scale = 1.0
+    out, lse, _ = ms.attend(0, q, cache, qs, ln, tables, scale=3.0e38, want_lse=True)
+    assert ((out[0, 0].double() - mean[0]).abs() <= 2.0**-8 * mean[0].abs() + 300 * 14 * 2.0**-24).all()
+    assert abs(lse[0, 0].item() - math.log(len_ - n + 1)) <= 2.0**-18
+    ms.close()
+
+
 # ------------------------------------------------------------------------------------------------ workspaces
 def test_attend_on_an_external_stream_keeps_no_workspace_for_it():
     import ctypes
