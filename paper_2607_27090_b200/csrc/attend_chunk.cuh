@@ -2,13 +2,17 @@
 //
 // Mathematics as in attend.cuh (one pass, running maximum and sum).  Bound: the tensor cores - 4 * head_dim operations per (query row,
 // key) - with the exponentials close behind: a tile of 128 x 128 scores takes 2 x 512 tensor cycles (head_dim 128) and 1024 cycles
-// of the SM's 16 exponentials per cycle.  Measured: 2,047 tokens behind 11,653 with 40/8 heads of 128 485 us (1.10 PFLOP/s, 0.64 of
-// the measured product rate); a tile of 256 rows takes about 3,500 cycles against 2,048 of products: what is left is the chain
-// from a score's product over its weight to the second product, of which TMEM has room for one tile per half in flight.
+// of the SM's 16 exponentials per cycle.  (With head_dim 64 the products take half of that and the exponentials are the bound.)
+// Measured: 2,047 tokens behind 11,653 with 40/8 heads of 128 490 us in short runs at 1,965 MHz (1.08 PFLOP/s, 0.63 of the measured
+// product rate), 562 us (0.95) call after call, when the power limit holds the clock at 1,690 MHz; 512 tokens of 4,096 with 32/8 heads
+// 57 us (head_dim 64: 46, 8-bit cache: 67).  A tile of 256 rows takes about 3,500 cycles against 2,048 of products: what is left is the
+// chain of a half - scores out of TMEM, weights, their store over the scores, which the two warps of a row group do together (a barrier),
+// second product, next scores - with one score tile per half in flight.  (At head_dim 128 the accumulators and two score tiles fill
+// TMEM; at 64 a quarter is unused.)
 //
 // A unit is (request, K/V head, 256 rows): rows are (token, query head of the group) pairs, so K and V are read once for all heads
 // of a group.  Two halves of 128 rows work in turn: while the tensor cores multiply for one half, the other half's warps form its
-// weights.  Scores go to TMEM, a thread owns one row (no shuffles), the weights return to TMEM in the type of V over the scores'
+// weights.  Scores go to TMEM, two threads share a row (no shuffles), the weights return to TMEM in the type of V over the scores'
 // columns and are the A operand of the second product, whose accumulator stays in TMEM for the whole unit.
 //   warps 0-7, 8-15  queries (scaled to fp16 for an 8-bit cache), weights and epilogue of rows 0-127, 128-255: two threads share a row,
 //                    64 of the tile's keys each (16 warps: a single warp per scheduler cannot keep the exponentials' unit busy)
@@ -320,8 +324,9 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(u_empty + kChunkUnits);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   uint32_t* s_masks = tmem_slot + 4;           // [kChunkMaskRing][4]: keys of the tile that the table names
-  uint32_t* s_bad = s_masks + 4 * kChunkMaskRing;  // [kChunkMaskRing][4]: a loading warp's part of the V tile holds values that are not
-                                                   // finite // finite (looked for
+  // [kChunkMaskRing][4]: a loading warp's part of the V tile holds values that are not finite.  Looked for in causal tiles alone (0 for
+  // the others); may be read once the next tile's scores, or the unit's last accumulator, are there.
+  uint32_t* s_bad = s_masks + 4 * kChunkMaskRing;
   float* s_pair = reinterpret_cast<float*>(s_bad + 4 * kChunkMaskRing);  // [256]: exchange between the two threads of a row
   uint8_t* s_qexp = reinterpret_cast<uint8_t*>(s_pair + kChunkRows);  // [256], 8-bit cache: exponent fields of the rows' inverse powers of two
   int64_t* s_warp = reinterpret_cast<int64_t*>(s_qexp + kChunkRows);  // [32]
@@ -796,7 +801,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
         const bool masked = k0 + 63 > lim_min || (there.x & there.y) != 0xffffffffu;
         uint32_t pk[32];
         float sum = 0.f;
-        // weights of the 64 scores with maximum `mm`, packed, and their sum
+        // weights of the 64 scores with maximum `mm`, rounded to the 16 bits that the product takes (V has no more; half a step is
+        // 2^-9 of a bf16 weight, 2^-12 of an fp16 one) and packed, and the fp32 sum of the unrounded ones
         auto form = [&](float mm, auto with_mask) {
           const float sub = mm == -INFINITY ? 0.f : -mm;
           const f2 sc2 = f2_make(sc, sc), sub2 = f2_make(sub, sub);

@@ -640,7 +640,8 @@ class MemStore:
     def append(self, layer: int, q, k, v, positions, slots, cache: PagedCache, q_out=None, out_status=None, stream=None):
         """Rotate ``q`` [T, n_q_heads, d] (or None) and ``k`` [T, h, d] at ``positions`` (int32) and write K and V into
         ``layer`` of the cache at ``slots`` (int64, negative: not written).  Returns the rotated queries (``q_out``, a new
-        tensor unless given; it may be ``q`` itself, in place)."""
+        tensor unless given; it may be ``q`` itself, in place).  Rows of tokens without a position (padding) are not written: in a
+        new tensor they hold anything, NaN included."""
         T, n_q, hq, ho = k.shape[0], 0, None, None
         if q is not None:
             n_q = q.shape[1]
@@ -684,7 +685,9 @@ class MemStore:
     def attend(self, layer: int, q, cache: PagedCache, q_start, seq_lens, block_tables, scale: float = 0.0, max_q_len: int = 0, out=None,
                want_lse: bool = False, out_lse=None, out_status=None, workspace=None, stream=None):  # fmt: skip
         """Attention of the new tokens ``q`` [T, n_q_heads, d] (rows ``q_start[r] .. q_start[r+1] - 1`` are the last tokens
-        of request r's ``seq_lens[r]`` cached ones) over ``layer`` of the cache.  Returns (out, lse or None, out_status).
+        of request r's ``seq_lens[r]`` cached ones) over ``layer`` of the cache.  Returns (out, lse or None, ``out_status`` as given).
+        Rows outside every request (padding) are not written: in a new ``out`` or lse they hold anything, NaN included; a caller that
+        goes on with them gives buffers of its own.  A kernel's time-out shows in ``out_status`` and in ``stats()["kernel_timeouts"]``.
         ``workspace``: a uint8 tensor of ``attend_workspace_bytes()``; by default the store keeps one for
         each of torch's streams that is current in a call; captures, calls with ``stream`` and external streams get one of their own."""
         (T, n_q, _), nreq, i32, ptr = q.shape, seq_lens.shape[0], torch.int32, self._ptr
