@@ -406,7 +406,7 @@ ms_status memstore_serve_host(memstore_t* store, const void* query, int32_t user
  * workspace that the caller gives, so calls on different streams or in different CUDA graphs do not disturb one another
  * as long as their arguments differ.  They run on the store's device whichever device is current, and may be captured
  * from their first call on.  Numbers of requests, tokens, entries per table and (query head, token) rows per K/V head are at most
- * 2^30 in a call (MS_ERR_UNSUPPORTED).
+ * 2^30 in a call, requests of memstore_attend at most 2^26 (MS_ERR_UNSUPPORTED).
  */
 
 /* A [tokens][heads][head_dim] bf16 array: element (t, h, d) at base[t * token_stride + h * head_stride + d].  base 16-byte
@@ -486,8 +486,9 @@ ms_status memstore_append(memstore_t* store, int32_t layer, const ms_heads* q, i
  * n_kv_heads query heads per K/V head, for query head h:
  *   s_j = scale * q . K[j][h / g],  out = sum_j exp(s_j - lse) V[j][h / g],  lse = ln sum_j exp(s_j)      (j = 0 .. p)
  * Scores, maxima, sums and accumulators are fp32; the weights exp(s_j - max) are rounded to the type of the matrix product: bf16, or
- * fp16 with an 8-bit cache, where a weight below 2^-18 of the row's largest may be off by 2^-29 of it instead of 2^-12 of itself.  A row without keys (p < 0) gives zeros and lse = -infinity.  Whatever the cache holds behind a
- * row's last key, NaN and infinities included, does not reach that row.
+ * fp16 with an 8-bit cache, where a weight below 2^-18 of the row's largest may be off by 2^-29 of it instead of 2^-12 of itself.
+ * A row without keys (p < 0) gives zeros and lse = -infinity.  Whatever the cache holds behind a row's last key, NaN and infinities
+ * included, does not reach that row.
  *   q, out        bf16 [n_tokens][n_q_heads][head_dim] (rotated queries); rows outside every request are neither read nor written.
  *                 out must not overlap q unless it is q itself (same base and strides)
  *   q_start       device int32 [nreq + 1], non-decreasing, within [0, n_tokens]

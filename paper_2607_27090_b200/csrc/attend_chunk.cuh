@@ -151,7 +151,8 @@ __device__ __forceinline__ bool chunk_locate(const ChunkParams& c, const AttnLin
   seg->pos = (int)rem;
   return true;
 }
-// The unit after seg; false behind the last request.
+// The unit after seg; false behind the last request.  By a whole warp: the other roles of the CTA wait while requests of the other kernel
+// are passed over, 32 at a time (a million of them between two chunks: 4 ms).
 __device__ __forceinline__ bool chunk_next(const ChunkParams& c, ChunkSeg* seg) {
   seg->pos = 0;
   seg->w.step(c);
@@ -160,10 +161,20 @@ __device__ __forceinline__ bool chunk_next(const ChunkParams& c, ChunkSeg* seg) 
     seg->w = ChunkWalk();
     if (++seg->kvh == c.a.n_kv) {
       seg->kvh = 0;
-      do {
-        if (++seg->r >= c.a.nreq) return false;
-        seg->q = attn_request(c.a, seg->r);
-      } while (seg->q.n == 0 || seg->q.rows <= c.min_rows);
+      unsigned here = 0u;
+      for (++seg->r; seg->r < c.a.nreq; seg->r += 32) {
+        const int r = seg->r + (int)(threadIdx.x & 31);
+        bool chunk = false;
+        if (r < c.a.nreq) {
+          const AttnReq q = attn_request(c.a, r);
+          chunk = q.n != 0 && q.rows > c.min_rows;
+        }
+        here = __ballot_sync(0xffffffffu, chunk);
+        if (here) break;
+      }
+      if (!here) return false;
+      seg->r += __ffs(here) - 1;
+      seg->q = attn_request(c.a, seg->r);
     }
   }
   seg->tiles = chunk_tiles(c.a, seg->q, seg->w);

@@ -9,6 +9,9 @@ static_assert(kReqTableShort == MS_REQ_BLOCK_TABLE_SHORT && kReqBadBlock == MS_R
 
 // Counts are at most 2^30, so that the kernels' 32-bit loops end before they wrap.
 constexpr int32_t kMaxCount = 1 << 30;
+// Requests of an attention call: passing that many over takes the chunk kernel's describing warp 0.3 s (4 ns each), well inside the bound of
+// the other roles' waits.
+constexpr int32_t kMaxAttendReqs = 1 << 26;
 static ms_status check_counts(memstore* s, int32_t a, int32_t b, int32_t c) {
   const int32_t most = std::max(a, std::max(b, c));
   return most <= kMaxCount ? MS_OK : fail(s, MS_ERR_UNSUPPORTED, "a count of %d is more than 2^30", most);
@@ -313,6 +316,7 @@ ms_status memstore_attend(memstore_t* s, int32_t layer, const ms_heads* q, int32
   if (!(scale >= 0.f) || !std::isfinite(scale)) return fail(s, MS_ERR_INVALID_ARG, "scale must be positive and finite, or 0 for the default");
   ms_status rc = check_cache(s, cache, layer, true);
   if (rc == MS_OK) rc = check_counts(s, nreq, max_blocks, 0);
+  if (rc == MS_OK && nreq > kMaxAttendReqs) rc = fail(s, MS_ERR_UNSUPPORTED, "%d requests in one attention call (at most 2^26)", nreq);
   if (rc == MS_OK) rc = check_heads(s, q, n_tokens, n_q_heads, false, "q");
   if (rc == MS_OK) rc = check_heads(s, out, n_tokens, n_q_heads, true, "out");
   if (rc != MS_OK) return rc;

@@ -11,6 +11,7 @@ pytestmark = pytest.mark.gpu
 
 if torch.cuda.is_available():
     import serving_ref as ref
+    from paper_2607_27090_b200 import memstore as M
     from test_gpu_serving import DEV, check_attend, fill_cache, i32, paged, store
 
 
@@ -67,6 +68,35 @@ def test_attend_random_batches_with_many_units_without_keys(fp8, d, seed):
     ms = store(hk, d)
     x = torch.randn((q_start[-1], hq, d), generator=gen, device=DEV).to(torch.bfloat16)
     check_attend(ms, cache, x, q_start, lens, tables)
+    ms.close()
+
+
+def test_attend_two_chunks_with_many_requests_between_them():
+    """The unit after the first chunk's last one belongs to the last of 200,000 requests (no tokens in between, then a few); far more are refused."""
+    nreq, hk, hq, d, bs, n = 200_000, 2, 8, 128, 128, 700
+    cache, gen = fill_cache(1, 12, bs, hk, d, False, "NHD", 1)
+    tables = torch.full((nreq, 6), -1, dtype=torch.int32, device=DEV)
+    tables[0], tables[-1] = torch.arange(6, device=DEV), torch.arange(6, 12, device=DEV)
+    ms = store(hk, d)
+    for middle in ({}, {70_000: 1, 70_031: 600, 70_032: 2, 130_000: 40}):
+        new = torch.zeros(nreq, dtype=torch.int64)
+        new[0] = new[-1] = n
+        for r, k in middle.items():
+            new[r] = k
+            tables[r] = torch.tensor([r % 12, 3, 5, 7, 9, 11], device=DEV)
+        lens = i32(torch.where(new > 0, torch.minimum(new + 60, torch.tensor(768)), 0).numpy())
+        q_start = torch.cat([torch.zeros(1, dtype=torch.int64), new.cumsum(0)])
+        q = torch.randn((int(q_start[-1]), hq, d), generator=gen, device=DEV).to(torch.bfloat16)
+        some = sorted([0, nreq - 1, *middle])
+        out, _, _ = ms.attend(0, q, cache, q_start.int().cuda(), lens, tables)
+        exact, _, tol, _ = ref.attend(q, cache, 0, [0, *new[some].cumsum(0).tolist()], lens[some].tolist(), tables[some], hk, 1.0 / math.sqrt(d), 9.0)
+        assert ((out.double() - exact).abs() <= tol).all()
+    torch.cuda.synchronize()
+    assert ms.stats()["kernel_timeouts"] == 0
+    x = M._Heads(q.data_ptr(), hq * d, d)
+    work = torch.empty(ms.attend_workspace_bytes(), dtype=torch.uint8, device=DEV)
+    at, c = lens.data_ptr(), cache._struct()
+    assert ms._lib.memstore_attend(ms._h, 0, x, hq, n, at, at, (1 << 26) + 1, at, 1, c, 0.0, 0, x, None, None, work.data_ptr(), work.numel(), 0) == 2
     ms.close()
 
 
