@@ -594,9 +594,9 @@ ms_status memstore_reserve(memstore_t* store, int32_t nq, int32_t k, int32_t nre
 
 /*
  * Test aid (no counterpart in the paper).  The kernels of this library that wait on a barrier (the bulk-async staged
- * copy kernel, the tensor-core scoring kernel, the attention's chunk kernel) bound every wait and report a time-out - MS_REQ_KERNEL_TIMEOUT in the
- * requests' status words, kernel_timeouts in the statistics - instead of hanging.  That path cannot be reached by
- * valid inputs, so this call lets a test reach it without any fault: with mute_producers != 0 the producer role of
+ * copy kernel, the tensor-core scoring kernel, the attention's chunk kernel) bound every wait and report a time-out -
+ * MS_REQ_KERNEL_TIMEOUT in the requests' status words, kernel_timeouts in the statistics - instead of hanging.  That path cannot be
+ * reached by valid inputs, so this call lets a test reach it without any fault: with mute_producers != 0 the producer role of
  * those kernels issues nothing at all (no copy is ever in flight), and with wait_poll_limit != 0 every wait gives up
  * after that many polls (a few thousand polls are a fraction of a millisecond).  The kernels then return normally
  * with the time-out reported; the call's outputs are unspecified but stay inside the caller's buffers.  (0, 0)

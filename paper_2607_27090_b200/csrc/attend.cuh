@@ -8,7 +8,8 @@
 // an m16n8k16 product are (token, query head) pairs that share a K/V head, so a cache row is read once for all heads of its
 // group; the legacy matrix instructions are far from their limit here.  Measured (GPU time, 32/8 heads of 128): 16 requests of
 // 16,384 tokens 160 us (6.7 TB/s), 100 of 900 67 us (5.5 TB/s), 100 of 500 - 1,300 71 us (5.2 TB/s); an 8-bit cache is held back by the
-// instructions that convert it: 16 of 32,768 185 us (5.8 TB/s), 16 of 7,000 - 32,700 116 - 125 us (5.1 - 5.6 TB/s).
+// instructions that convert it: 16 of 32,768 185 us (5.8 TB/s), 16 of 7,000 - 32,700 116 - 135 us on
+// different GPUs (4.8 - 5.6 TB/s).
 //
 // Work split: a unit is (request, K/V head, 16 rows) x all its tiles of 64 keys (128 where cache rows are at most 128 bytes: an
 // 8-bit cache with 64 keys a tile takes 168 us where 128 take 121).  The tiles of all units are numbered one after another and

@@ -59,7 +59,7 @@ struct ChunkCfg {
   static constexpr int kTmemCols = 512;
   // Sum of 64 weights (and so a weight) that is tolerated without taking a new maximum, and what the exponents are lifted by when one is
   // taken (see AttnCfg::kLift).  fp16 weights stay below 65,504; what the lift takes from the room above it is paid in new maxima where
-  // scores spread: 512 tokens of 4,096 in an 8-bit cache (32/8 heads of 128, scores of standard deviation 1 / 2 / 3 / 5) take 66.7 / 66.7 /
+  // scores spread: 512 tokens of 4,096 in an 8-bit cache (32/8 heads of 128, scores of standard deviation 1.5 / 3 / 4.5 / 7.5) take 66.7 / 66.7 /
   // 67.8 / 80.5 us without a lift, 66.6 / 66.8 / 71.6 / 82.8 with 4, 66.6 / 67.4 / 77.0 / 84.1 with 6, 66.6 / 71.7 / 82.0 / 85.0 with 8.
   static constexpr float kMaxSum = FP8 ? 61440.f : 16384.f;
   static constexpr float kLift = FP8 ? 4.f : 0.f;

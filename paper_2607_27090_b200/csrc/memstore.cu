@@ -1864,7 +1864,7 @@ ms_status memstore_test_hooks(memstore_t* s, uint32_t wait_poll_limit, int32_t m
   s->test_mute_producers = mute_producers ? 1 : 0;
   if (!wait_poll_limit && !mute_producers) {  // back to normal: forget a time-out that a test provoked
     DeviceGuard g(s->cfg.device);
-    MS_CUDA(s, cudaMemset(s->attn_timed_out, 0, sizeof(int)));
+    if (s->attn_chunks) MS_CUDA(s, cudaMemset(s->attn_timed_out, 0, sizeof(int)));
     if (s->tc_error) MS_CUDA(s, cudaMemset(s->tc_error, 0, sizeof(int)));
   }
   return MS_OK;
