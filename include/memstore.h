@@ -69,7 +69,8 @@ enum {
   MS_REQ_KERNEL_TIMEOUT = 32,    /* a bounded wait inside the copy kernel ran out: the cache contents of this call are incomplete */
   MS_REQ_BAD_START = 64,         /* start_pos < 0: no token of the request is placed */
   MS_REQ_NO_BLOCKS = 128,        /* memstore_grow_blocks / memstore_release_blocks: the free list cannot serve the request */
-  MS_REQ_BAD_LENGTH = 256        /* a negative number of tokens, or token rows outside the call's token arrays */
+  MS_REQ_BAD_LENGTH = 256,       /* a negative number of tokens, or token rows outside the call's token arrays */
+  MS_REQ_BAD_TREE = 512          /* memstore_plan_tree: a node whose parent does not come before it */
 };
 
 enum { MS_DTYPE_F32 = 0, MS_DTYPE_F16 = 1, MS_DTYPE_BF16 = 2 };
@@ -510,8 +511,135 @@ ms_status memstore_attend(memstore_t* store, int32_t layer, const ms_heads* q, i
                           const int32_t* seq_lens, int32_t nreq, const int32_t* block_tables, int32_t max_blocks,
                           const ms_paged_cache* cache, float scale, int32_t max_q_len, const ms_heads* out, float* out_lse,
                           int32_t* out_status, void* workspace, size_t workspace_bytes, ms_stream stream);
-/* Bytes of workspace that any memstore_attend call of this store needs (it depends on the GPU and head_dim, not on lengths). */
+/* Bytes of workspace that any memstore_attend, memstore_attend_tree or memstore_attend_blocks call of this store needs (it depends on the
+ * GPU and head_dim, not on lengths). */
 size_t memstore_attend_workspace(memstore_t* store);
+
+/*
+ * ---- drafted trees ---------------------------------------------------------------------------------------------------
+ * Several guesses of the tokens that follow are checked in one pass over the cache.  The new tokens of a request are then the nodes of
+ * a tree: node 0 is the token that is certain, node i > 0 hangs on a node before it (parent in [0, i - 1]) and stands for one guess of the
+ * token after that node.  Their keys and values lie in the cache one after another in node order (memstore_grow_blocks gives the slots),
+ * whatever their positions.  A step: memstore_grow_blocks, memstore_plan_tree, then per layer memstore_append (at the tree's positions) and
+ * memstore_attend_tree, and when the model has said what follows each node, memstore_accept.
+ */
+
+/*
+ * Positions and visibility masks of trees from parents.  A node's depth is its distance from a node without a parent (-1).
+ *   parents        device int32 [n_tokens]: node number of each node's parent in its request, -1: it hangs on the context
+ *   q_start        device int32 [nreq + 1]: nodes of request r are the rows q_start[r] .. q_start[r+1] - 1, at most 32 * mask_words
+ *   positions      device int32 [n_tokens]: of row q_start[r] the position of the request's first new token, as memstore_grow_blocks lists it;
+ *                  the others are not read
+ *   mask_words     1 to 128
+ *   out_positions  device int32 [n_tokens] or NULL: that position + depth, -1 for every node of a request where it is negative (a request that
+ *                  memstore_grow_blocks refused); may be positions itself
+ *   out_mask       device uint32 [n_tokens][mask_words] or NULL: bit j % 32 of word j / 32 of a row is set for the node itself and its ancestors
+ *   out_status     device int32 [nreq] or NULL: MS_REQ_BAD_LENGTH (no range of rows, or too many nodes: nothing is written for the request),
+ *                  MS_REQ_BAD_TREE (a parent outside [-1, i - 1]: the request's positions become -1 and its masks 0)
+ * Rows outside every request are not written.
+ */
+ms_status memstore_plan_tree(memstore_t* store, const int32_t* parents, int32_t n_tokens, const int32_t* q_start, int32_t nreq,
+                             const int32_t* positions, int32_t mask_words, int32_t* out_positions, uint32_t* out_mask, int32_t* out_status,
+                             ms_stream stream);
+
+/*
+ * memstore_attend with masks among the new tokens: row i of request r attends to all keys in front of the request's new tokens (the first
+ * seq_len - n_new of the cache) and to the key of new token j exactly where bit j % 32 of word j / 32 of tree_mask[q_start[r] + i] is set; any
+ * masks will do, a tree's are the ones of memstore_plan_tree.  A row that sees nothing gives zeros and lse = -infinity, and what the cache holds at keys
+ * that a row does not see, NaN and infinities included, does not reach it.  Everything else, the workspace among it, is as for memstore_attend.
+ *   tree_mask   device uint32 [n_tokens][mask_words], mask_words 1 to 128.  A request with more than 32 * mask_words new tokens is left out
+ *               (MS_REQ_BAD_LENGTH); bits of new tokens that the request does not have are not looked at
+ */
+ms_status memstore_attend_tree(memstore_t* store, int32_t layer, const ms_heads* q, int32_t n_q_heads, int32_t n_tokens, const int32_t* q_start,
+                               const int32_t* seq_lens, int32_t nreq, const uint32_t* tree_mask, int32_t mask_words, const int32_t* block_tables,
+                               int32_t max_blocks, const ms_paged_cache* cache, float scale, int32_t max_q_len, const ms_heads* out, float* out_lse,
+                               int32_t* out_status, void* workspace, size_t workspace_bytes, ms_stream stream);
+
+/*
+ * The part of each tree that the model confirms.  The walk starts at node 0 and goes from a node with the model's choice t to the node's child
+ * with token t (the lowest, if several have it) until there is none; the nodes on the way are accepted.  Their keys and values move, in
+ * every layer of the cache, to the places right behind the context (the i-th node to place start + i); the request's length becomes start + accepted, and blocks
+ * that it no longer reaches go back to the free list.
+ *   parents, tokens  device int32 [n_tokens]: the tree, and the token that each node guesses (that of node 0 is not looked at)
+ *   choices          device int32 [n_tokens]: the token that the model puts behind each node
+ *   positions        device int32 [n_tokens]: of row q_start[r] the position of node 0, as memstore_grow_blocks or memstore_plan_tree wrote it
+ *   seq_lens         device int32 [nreq]: tokens in the cache, the request's nodes included
+ *   block_tables     entries behind the new end are left as they are and name nothing of the request's any more
+ *   cache            all n_layers of it; the strides of an 8-bit cache are multiples of 16 (MS_ERR_UNSUPPORTED)
+ *   free_blocks      device int32 [n_free] or NULL: blocks go back by the rule of memstore_release_blocks; NULL: they stay with the request, and the caller
+ *                    sees to it that they are not given out a second time (memstore_grow_blocks would list new ones in their table entries)
+ *   n_taken          device int32 [1] (with free_blocks)
+ *   out_path         device int32 [n_tokens]: row q_start[r] + i holds the i-th accepted node, -1 behind the last
+ *   out_n_accepted   device int32 [nreq]: 0 for a request without nodes or that was left out, else 1 or more
+ *   out_next         device int32 [nreq]: the model's choice behind the last accepted node (the next step's node 0), -1 where none is accepted
+ *   out_seq_lens     device int32 [nreq]; may be seq_lens itself
+ *   out_n_taken      device int32 [1] (with free_blocks): *n_taken minus the blocks returned; may be n_taken itself
+ *   out_status       device int32 [nreq]: MS_REQ_BAD_START (node 0 has a negative position: the request is left as it is), MS_REQ_BAD_LENGTH (no range of
+ *                    rows, or the positions and lengths do not fit: likewise), MS_REQ_BLOCK_TABLE_SHORT, MS_REQ_BAD_BLOCK_ID (a place to read or
+ *                    write lies in a block that the table does not name: that row does not move; a block to return is not in the cache: it is dropped),
+ *                    MS_REQ_NO_BLOCKS (more blocks than *n_taken would go back: the request's are not returned, nor those of later ones)
+ * Blocks of the nodes must not be shared with other requests.  Requests are independent otherwise.
+ */
+ms_status memstore_accept(memstore_t* store, const int32_t* parents, const int32_t* tokens, const int32_t* choices, const int32_t* positions,
+                          int32_t n_tokens, const int32_t* q_start, const int32_t* seq_lens, int32_t nreq, const int32_t* block_tables,
+                          int32_t max_blocks, const ms_paged_cache* cache, int32_t* free_blocks, int32_t n_free, const int32_t* n_taken,
+                          int32_t* out_path, int32_t* out_n_accepted, int32_t* out_next, int32_t* out_seq_lens, int32_t* out_n_taken,
+                          int32_t* out_status, ms_stream stream);
+
+/*
+ * ---- selected blocks -------------------------------------------------------------------------------------------------
+ * In a long context a token reads the blocks that matter to it.  Every block of the cache has a summary per layer and K/V head: the smallest and the
+ * largest value of each coordinate over its keys, from which no key's score can stand out.  A step, per layer: memstore_append,
+ * memstore_summarize_blocks (the new tokens' blocks), memstore_select_blocks, memstore_attend_blocks.
+ */
+
+/*
+ * Form the summaries of the blocks that hold the requests' new tokens (their last q_start[r+1] - q_start[r] ones), from all keys that
+ * the blocks hold up to seq_len.
+ *   q_start     device int32 [nreq + 1], within [0, n_tokens], or NULL: every block of every request (after an injection; n_tokens is not looked at)
+ *   cache       layer `layer` of its keys; the strides of an 8-bit cache are multiples of 16 (MS_ERR_UNSUPPORTED)
+ *   summaries   device bf16 [num_blocks][n_kv_heads][2][head_dim] of this layer, 16-byte aligned: smallest values, then largest; of an 8-bit cache those of
+ *               the codes (without k_scale), exact like the others.  A coordinate that is NaN in a key is NaN in both
+ * Requests whose rows or length are invalid and blocks that the table does not name are passed over.  Where requests share a block, the last writer's
+ * view of its length counts: share full blocks.
+ */
+ms_status memstore_summarize_blocks(memstore_t* store, int32_t layer, const int32_t* q_start, int32_t n_tokens, const int32_t* seq_lens, int32_t nreq,
+                                    const int32_t* block_tables, int32_t max_blocks, const ms_paged_cache* cache, void* summaries, ms_stream stream);
+
+/*
+ * Choose the blocks that each new token reads, per K/V head.  The token at position p may read blocks 0 .. p / block_size of its request; block b has the score
+ *   sum over the group's query heads and the coordinates of max(q lo_b, q hi_b)  =  sum_d (P_d hi_bd + N_d lo_bd)
+ * (P, N: sums over the group of the positive and of the negative parts of q), an upper bound of the group's summed scores of any key in it, formed
+ * in 64 bits and rounded to fp32.  The first n_first and the last n_last blocks are always chosen, then the others by score, equal scores the
+ * lower block first; NaN counts as plus infinity.  Blocks that the table does not name are never chosen.
+ *   q, q_start, seq_lens  as for memstore_attend (rotated queries)
+ *   summaries    as memstore_summarize_blocks writes them
+ *   cache        geometry only: block_size and num_blocks are read
+ *   max_blocks   at most 49,152 here (MS_ERR_UNSUPPORTED)
+ *   n_select     1 or more, n_first + n_last at most n_select
+ *   out_blocks   device int32 [n_tokens][n_kv_heads][n_select]: block numbers of the request (its table's columns) in rising order, -1 behind the last
+ *   out_scores   device fp32 [n_tokens][n_kv_heads][max_blocks] or NULL: the scores of all blocks that the token may read (-infinity: not named
+ *                by the table); entries behind its last block are not written
+ * Rows outside every valid request are not written.
+ */
+ms_status memstore_select_blocks(memstore_t* store, const ms_heads* q, int32_t n_q_heads, int32_t n_tokens, const int32_t* q_start,
+                                 const int32_t* seq_lens, int32_t nreq, const void* summaries, const int32_t* block_tables, int32_t max_blocks,
+                                 const ms_paged_cache* cache, int32_t n_select, int32_t n_first, int32_t n_last, int32_t* out_blocks,
+                                 float* out_scores, ms_stream stream);
+
+/*
+ * memstore_attend over listed blocks: row i of request r, at position p, attends for query head h to the keys at positions 0 .. p that lie in the blocks
+ * listed for the row and K/V head h / g.  Everything else, the workspace among it, is as for memstore_attend; a token's keys are read for it alone, so this
+ * call is for few new tokens per request.
+ *   blocks     device int32 [n_tokens][n_kv_heads][n_select]: block numbers of the request in any order, each once (one that is listed twice counts twice).  The first
+ *              min(n_select, ceil(seq_len / block_size)) entries of a list are looked at; numbers outside [0, max_blocks) or behind the
+ *              row's position, and blocks that the table does not name, are left out
+ *   n_select   1 or more, n_select * block_size at most 2^30 (MS_ERR_UNSUPPORTED)
+ */
+ms_status memstore_attend_blocks(memstore_t* store, int32_t layer, const ms_heads* q, int32_t n_q_heads, int32_t n_tokens, const int32_t* q_start,
+                                 const int32_t* seq_lens, int32_t nreq, const int32_t* blocks, int32_t n_select, const int32_t* block_tables,
+                                 int32_t max_blocks, const ms_paged_cache* cache, float scale, const ms_heads* out, float* out_lse,
+                                 int32_t* out_status, void* workspace, size_t workspace_bytes, ms_stream stream);
 
 /* Counters since creation (host side; bytes are the algorithmic ones, not measured traffic).  Reading
  * kernel_timeouts synchronises the device. */

@@ -6,7 +6,7 @@ be imported on its own.
 """
 import importlib
 
-_BINDING_NAMES = ("MemStore", "PagedCache", "MemStoreError", "GrownBlocks")
+_BINDING_NAMES = ("MemStore", "PagedCache", "MemStoreError", "GrownBlocks", "Accepted")
 
 
 def __getattr__(name):

@@ -31,6 +31,15 @@ constexpr int kAttnMaxGroup = 1024;
 constexpr int kAttnMaxCtasPerSm = 2;
 constexpr int32_t kAttnMaxLen = 1 << 30;  // (key numbers stay inside 32 bits)
 
+// Which keys a row sees:
+//   kSeeCausal  all at positions up to its own                                                              (memstore_attend)
+//   kSeeTree    all in front of the request's new tokens, and of those the ones that the row's bits name    (memstore_attend_tree)
+//   kSeeBlocks  those at positions up to its own in the blocks that the token's list for the K/V head names (memstore_attend_blocks).
+//               The keys of a unit are then numbered along its list: key v is place v % block_size of listed block v / block_size, and a
+//               unit has rows of one token alone, so that all its rows see the same keys and what they do not see is not loaded.
+enum { kSeeCausal = 0, kSeeTree = 1, kSeeBlocks = 2 };
+constexpr int kTreeMaxWords = 128;  // 32-bit words of a row's bits
+
 // What the border in front of a CTA's share cuts, written by that CTA: the unit to join when the border is the unit's first one.
 struct __align__(16) AttnCut {
   int32_t c_last;          // last CTA with a part of the unit, -1: nothing to join
@@ -68,31 +77,57 @@ struct AttendParams {
   float* part_o;     // [CTAs][2][kAttnRows][head_dim]
   float2* part_ml;   // [CTAs][2][kAttnRows]
   AttnCut* cuts;     // [CTAs]
+  const uint32_t* tree;  // kSeeTree: [n_tokens][tree_words], bit j of row i: new token i of a request sees the request's new token j
+  int32_t tree_words;    // (0 otherwise)
+  const int32_t* lists;  // kSeeBlocks: [n_tokens][n_kv][list_len] blocks of the token's request, counted from its first
+  int32_t list_len;
+  int32_t token_tiles;   // kSeeBlocks: row tiles of a token
 };
 
 // One request as the kernels see it.
 struct AttnReq {
   int32_t q0, n;    // rows of q; n = 0: left out
   int32_t len;      // tokens in the cache
-  int32_t keys;     // keys the table can name
+  int32_t keys;     // keys the table can name (kSeeBlocks: that a list can)
   int32_t rows;     // n * group
 };
+template <int SEE = kSeeCausal>
 __device__ __forceinline__ AttnReq attn_request(const AttendParams& p, int r) {
   AttnReq a;
   const int32_t q0 = __ldg(p.q_start + r), q1 = __ldg(p.q_start + r + 1);
   a.len = __ldg(p.seq_lens + r);
-  const bool ok = q0 >= 0 && q1 >= q0 && q1 <= p.n_tokens && a.len >= 0 && a.len <= kAttnMaxLen;
+  bool ok = q0 >= 0 && q1 >= q0 && q1 <= p.n_tokens && a.len >= 0 && a.len <= kAttnMaxLen;
+  if (SEE == kSeeTree) ok = ok && q1 - q0 <= 32 * p.tree_words;
   a.q0 = q0;
   a.n = ok ? q1 - q0 : 0;
-  a.keys = (int32_t)min((int64_t)a.len, (int64_t)p.max_blocks * p.block_size);
+  if (SEE == kSeeBlocks)  // (a list has no more entries than the request has blocks; list_len * block_size is at most 2^30)
+    a.keys = ok ? min(p.list_len, (int32_t)(((int64_t)a.len + p.block_size - 1) / p.block_size)) * p.block_size : 0;
+  else
+    a.keys = (int32_t)min((int64_t)a.len, (int64_t)p.max_blocks * p.block_size);
   a.rows = a.n * p.group;
   return a;
 }
 // Tiles of one unit of the request (one at least, so that rows without keys are written too), and of all its units.
 __device__ __forceinline__ int attn_tiles(const AttendParams& p, const AttnReq& a) { return max(1, (a.keys + (1 << p.tile_shift) - 1) >> p.tile_shift); }
+// row tiles of a K/V head
+template <int SEE = kSeeCausal>
+__device__ __forceinline__ int attn_row_tiles(const AttendParams& p, const AttnReq& a) {
+  return SEE == kSeeBlocks ? a.n * p.token_tiles : (a.rows + kAttnRows - 1) / kAttnRows;
+}
+template <int SEE = kSeeCausal>
 __device__ __forceinline__ int64_t attn_cost(const AttendParams& p, const AttnReq& a) {
   if (a.n == 0 || a.rows > p.max_rows) return 0;
-  return (int64_t)((a.rows + kAttnRows - 1) / kAttnRows) * p.n_kv * attn_tiles(p, a);
+  return (int64_t)attn_row_tiles<SEE>(p, a) * p.n_kv * attn_tiles(p, a);
+}
+
+// Which of the 32 keys from k0 on a row of a tree sees, out of those in `there`: the row's bits, with ones for everything in front of the
+// new tokens (the first of which is at position pos0).
+__device__ __forceinline__ uint32_t tree_see(uint32_t there, int k0, int pos0, const uint32_t* row, int words) {
+  const int rel = k0 - pos0;
+  if (rel <= -32) return there;
+  const int w = rel >> 5;
+  const uint32_t lo = w < 0 ? 0xffffffffu : w < words ? __ldg(row + w) : 0u, hi = w + 1 < words ? __ldg(row + w + 1) : 0u;
+  return there & __funnelshift_r(lo, hi, rel & 31);
 }
 
 // a / b and a % b; 64-bit division only where it is needed
@@ -293,7 +328,7 @@ __device__ __forceinline__ int attn_swz(int r, int c) {
   return (r * CHUNKS + (c ^ x)) * 16;
 }
 
-template <int D, bool FP8>
+template <int D, bool FP8, int SEE>
 __global__ void __launch_bounds__(kAttnThreads, AttnCfg<D, FP8>::kCtasPerSm) attend_rows_kernel(const AttendParams p) {
   using C = AttnCfg<D, FP8>;
   constexpr int kSteps = D / 16, kNT = D / 8;
@@ -308,7 +343,7 @@ __global__ void __launch_bounds__(kAttnThreads, AttnCfg<D, FP8>::kCtasPerSm) att
   grid_launch_dependents();
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t4 = lane & 3;
 
-  auto cost_of = [&](int i) { return attn_cost(p, attn_request(p, i)); };
+  auto cost_of = [&](int i) { return attn_cost<SEE>(p, attn_request<SEE>(p, i)); };
   AttnLine<kAttnThreads> line;
   line.init(p.nreq, cost_of, s_warp);
   const int64_t total = line.total;
@@ -319,7 +354,7 @@ __global__ void __launch_bounds__(kAttnThreads, AttnCfg<D, FP8>::kCtasPerSm) att
   int64_t req_start = 0;
   int r = off < off_end ? line.locate(p.nreq, cost_of, off, s_warp, s_found, &req_start) : -1;
   AttnReq rq{};
-  if (r >= 0) rq = attn_request(p, r);
+  if (r >= 0) rq = attn_request<SEE>(p, r);
   bool first = true;
 
   uint8_t* ring = smem + warp * (C::kStages * C::kStageBytes);
@@ -327,16 +362,24 @@ __global__ void __launch_bounds__(kAttnThreads, AttnCfg<D, FP8>::kCtasPerSm) att
 
   while (r >= 0 && off < off_end) {
     // ---- the unit that tile `off` belongs to
-    const int tiles = attn_tiles(p, rq), n_rt = (rq.rows + kAttnRows - 1) / kAttnRows;
+    const int tiles = attn_tiles(p, rq), n_rt = attn_row_tiles<SEE>(p, rq);
     int64_t rem;
     const int64_t u = attn_div(off - req_start, tiles, &rem);  // row tile fastest, so that the row tiles of a K/V head follow one another
     const int t0 = (int)rem;
     const int kvh = (int)attn_div(u, n_rt, &rem), rt = (int)rem;
     const int t1 = (int)min((int64_t)tiles, t0 + (off_end - off));
     const bool whole = t0 == 0 && t1 == tiles;
-    const int row0 = rt * kAttnRows;
-    const int rows = min(kAttnRows, rq.rows - row0);
-    const int tok0 = row0 / p.group, sub0 = row0 - tok0 * p.group;  // new token and query head of the group of row 0
+    int rows, tok0, sub0;  // rows, and new token and query head of the group of row 0
+    if constexpr (SEE == kSeeBlocks) {
+      tok0 = rt / p.token_tiles;
+      sub0 = (rt - tok0 * p.token_tiles) * kAttnRows;
+      rows = min(kAttnRows, p.group - sub0);
+    } else {
+      const int row0 = rt * kAttnRows;
+      rows = min(kAttnRows, rq.rows - row0);
+      tok0 = row0 / p.group;
+      sub0 = row0 - tok0 * p.group;
+    }
     if (first && tid == 0 && t0 != 0 && share >= t0) {
       AttnCut cut{};
       cut.c_last = (int)attn_div(off - t0 + tiles - 1, share, &rem);
@@ -349,19 +392,41 @@ __global__ void __launch_bounds__(kAttnThreads, AttnCfg<D, FP8>::kCtasPerSm) att
     first = false;
     const int pos0 = rq.len - rq.n;  // position of the request's first new token
     const int last_pos = pos0 + tok0 + group_div(p, sub0 + rows - 1);
-    const int key_end = min(rq.keys, last_pos + 1);  // keys that any row of the unit may see
+    // keys that any row of the unit may see
+    const int key_end = SEE == kSeeBlocks ? (last_pos < 0 ? 0 : rq.keys) : SEE == kSeeTree ? rq.keys : min(rq.keys, last_pos + 1);
     const int n_it = min(t1, (key_end + C::kTileKeys - 1) / C::kTileKeys) - t0;  // <= 0: nothing to read
     // last key of this thread's two rows (rows behind the unit's last follow the last one)
-    const int lim0 = pos0 + tok0 + group_div(p, sub0 + min(g, rows - 1)), lim1 = pos0 + tok0 + group_div(p, sub0 + min(g + 8, rows - 1));
-    const int lim_min = pos0 + tok0;
+    const int dt0 = group_div(p, sub0 + min(g, rows - 1)), dt1 = group_div(p, sub0 + min(g + 8, rows - 1));
+    const int lim0 = pos0 + tok0 + dt0, lim1 = pos0 + tok0 + dt1;
+    // last key that every row sees (of those that are loaded)
+    const int lim_min = SEE == kSeeBlocks ? 0x7fffffff - C::kTileKeys : SEE == kSeeTree ? pos0 - 1 : pos0 + tok0;
+    const uint32_t *tree0 = nullptr, *tree1 = nullptr;  // this thread's rows' bits
+    if constexpr (SEE == kSeeTree) {
+      tree0 = p.tree + (int64_t)(rq.q0 + tok0 + dt0) * p.tree_words;
+      tree1 = p.tree + (int64_t)(rq.q0 + tok0 + dt1) * p.tree_words;
+    }
 
     const int32_t* table = p.tables + (int64_t)r * p.max_blocks;
     const uint8_t* kh = p.k_cache + kvh * p.head_stride;
     const uint8_t* vh = p.v_cache + kvh * p.head_stride;
     // lane's key of iteration i, and its table entry (fetched one iteration before it is needed)
     auto key_of = [&](int i) { return (t0 + i) * C::kTileKeys + warp * C::kKeys + (lane & (C::kKeys - 1)); };
-    auto entry_of = [&](int i) {
+    const int32_t* list = nullptr;
+    int last_block = -1;  // kSeeBlocks: of those that hold keys the token may see and that the table has
+    if constexpr (SEE == kSeeBlocks) {
+      list = p.lists + ((int64_t)(rq.q0 + tok0) * p.n_kv + kvh) * p.list_len;
+      if (last_pos >= 0) last_block = min(attn_page(p, last_pos), p.max_blocks - 1);
+    }
+    auto listed = [&](int i) {  // kSeeBlocks: the entry of the list
       const int key = key_of(i);
+      return i < n_it && key < key_end ? __ldg(list + attn_page(p, key)) : -1;
+    };
+    auto entry_of = [&](int i, int32_t block) {
+      const int key = key_of(i);
+      if constexpr (SEE == kSeeBlocks) {
+        const bool there = block >= 0 && block <= last_block && block * p.block_size + attn_in_page(p, key) <= last_pos;
+        return there ? __ldg(table + block) : -1;
+      }
       return i < n_it && key < key_end ? __ldg(table + attn_page(p, key)) : -1;
     };
     auto issue = [&](int i, int32_t blk) {
@@ -388,11 +453,16 @@ __global__ void __launch_bounds__(kAttnThreads, AttnCfg<D, FP8>::kCtasPerSm) att
       cp_async_commit();
     };
 
-    int32_t nxt = entry_of(0);
+    // kSeeBlocks looks up twice, list and table: each look-up has the time of a tile
+    int32_t nxt_block = -1;
+    if constexpr (SEE == kSeeBlocks) nxt_block = listed(0);
+    int32_t nxt = entry_of(0, nxt_block);
+    if constexpr (SEE == kSeeBlocks) nxt_block = listed(1);
 #pragma unroll 1
     for (int i = 0; i < C::kStages - 1; ++i) {
       const int32_t blk = nxt;
-      nxt = entry_of(i + 1);
+      nxt = entry_of(i + 1, nxt_block);
+      if constexpr (SEE == kSeeBlocks) nxt_block = listed(i + 2);
       issue(i, blk);
     }
     // ---- queries: A fragments of the 16 rows, zero behind the last
@@ -452,7 +522,8 @@ __global__ void __launch_bounds__(kAttnThreads, AttnCfg<D, FP8>::kCtasPerSm) att
       __syncwarp();
       {
         const int32_t blk = nxt;
-        nxt = entry_of(i + C::kStages);
+        nxt = entry_of(i + C::kStages, nxt_block);
+        if constexpr (SEE == kSeeBlocks) nxt_block = listed(i + C::kStages + 1);
         issue(i + C::kStages - 1, blk);
       }
       const int st = i % C::kStages;
@@ -503,16 +574,26 @@ __global__ void __launch_bounds__(kAttnThreads, AttnCfg<D, FP8>::kCtasPerSm) att
           }
       }
       // ---- mask, running maximum and sum
-      const bool causal = k0 + C::kKeys - 1 > lim_min;  // some row ends inside or before these keys
+      const bool causal = k0 + C::kKeys - 1 > lim_min;  // some row ends inside or before these keys, or may leave some of them out
+      uint32_t tsee0 = mask, tsee1 = mask;
+      if (SEE == kSeeTree && causal) {
+        tsee0 = tree_see(mask, k0, pos0, tree0, p.tree_words);
+        tsee1 = tree_see(mask, k0, pos0, tree1, p.tree_words);
+      }
       if (causal || mask != kAllKeys) {
 #pragma unroll
         for (int nt = 0; nt < C::kST; ++nt)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
             const int c = nt * 8 + 2 * t4 + e;
-            const bool there = (mask >> c) & 1u;
-            if (!there || k0 + c > lim0) s[nt][e] = -INFINITY;
-            if (!there || k0 + c > lim1) s[nt][2 + e] = -INFINITY;
+            if constexpr (SEE == kSeeTree) {
+              if (!((tsee0 >> c) & 1u)) s[nt][e] = -INFINITY;
+              if (!((tsee1 >> c) & 1u)) s[nt][2 + e] = -INFINITY;
+            } else {
+              const bool there = (mask >> c) & 1u;
+              if (!there || (SEE == kSeeCausal && k0 + c > lim0)) s[nt][e] = -INFINITY;
+              if (!there || (SEE == kSeeCausal && k0 + c > lim1)) s[nt][2 + e] = -INFINITY;
+            }
           }
       }
       float x0 = -INFINITY, x1 = -INFINITY;
@@ -556,7 +637,7 @@ __global__ void __launch_bounds__(kAttnThreads, AttnCfg<D, FP8>::kCtasPerSm) att
       // ---- a value that is not finite at a key that some row must not see would reach that row as 0 * inf: such keys (only a chunk's
       // last ones can be) are summed one by one
       bool by_key = false;
-      if (causal) {
+      if (SEE != kSeeBlocks && causal) {
         const uint4* vp = reinterpret_cast<const uint4*>(ring + st * C::kStageBytes + C::kTileBytes);
         bool bad = false;
         for (int j = lane; j < C::kTileBytes / 16; j += 32) {
@@ -582,7 +663,8 @@ __global__ void __launch_bounds__(kAttnThreads, AttnCfg<D, FP8>::kCtasPerSm) att
             const float e0 = __shfl_sync(0xffffffffu, s[nt][0], from), e1 = __shfl_sync(0xffffffffu, s[nt][1], from);
             const float e2 = __shfl_sync(0xffffffffu, s[nt][2], from), e3 = __shfl_sync(0xffffffffu, s[nt][3], from);
             const float w0 = c & 1 ? e1 : e0, w1 = c & 1 ? e3 : e2;
-            const bool there = (mask >> c) & 1u, see0 = there && k0 + c <= lim0, see1 = there && k0 + c <= lim1;
+            const bool there = (mask >> c) & 1u;
+            const bool see0 = SEE == kSeeTree ? (tsee0 >> c) & 1u : there && k0 + c <= lim0, see1 = SEE == kSeeTree ? (tsee1 >> c) & 1u : there && k0 + c <= lim1;
 #pragma unroll
             for (int n = 0; n < kNT; ++n) {
               float v0, v1;
@@ -717,12 +799,12 @@ __global__ void __launch_bounds__(kAttnThreads, AttnCfg<D, FP8>::kCtasPerSm) att
 
     // ---- next
     off += t1 - t0;
-    if (off < off_end && off - req_start >= attn_cost(p, rq)) {
+    if (off < off_end && off - req_start >= attn_cost<SEE>(p, rq)) {
       req_start = off;
       do {
         if (++r >= p.nreq) r = -1;  // (cannot be: off lies before the end of the line)
-        else rq = attn_request(p, r);
-      } while (r >= 0 && attn_cost(p, rq) == 0);
+        else rq = attn_request<SEE>(p, r);
+      } while (r >= 0 && attn_cost<SEE>(p, rq) == 0);
     }
   }
   if (p.gate) grid_dependency_wait();
@@ -816,7 +898,7 @@ __device__ __forceinline__ void attend_report(const AttendParams& p, int block, 
   if (!p.status || r >= p.nreq) return;
   const int32_t q0 = p.q_start[r], q1 = p.q_start[r + 1], len = p.seq_lens[r];
   int st = 0;
-  if (q0 < 0 || q1 < q0 || q1 > p.n_tokens || len < 0 || len > kAttnMaxLen) {
+  if (q0 < 0 || q1 < q0 || q1 > p.n_tokens || len < 0 || len > kAttnMaxLen || (p.tree_words > 0 && q1 - q0 > 32 * p.tree_words)) {
     st = kReqBadLength;
   } else {
     const int64_t blocks = ((int64_t)len + p.block_size - 1) / p.block_size;

@@ -92,21 +92,26 @@ struct ChunkWalk {
   }
 };
 // Tiles of a unit: up to the last key that its last row sees (one at least: rows without keys are written too).
+// (A tree's rows may see any of the new tokens.)
+template <int SEE>
 __device__ __forceinline__ int chunk_tiles(const AttendParams& p, const AttnReq& q, const ChunkWalk& w) {
+  if (SEE == kSeeTree) return max(1, (q.keys + kChunkKeys - 1) / kChunkKeys);
   const int last = min(q.n - 1, w.tok + group_div(p, w.sub + kChunkRows - 1));
   return max(1, (min(q.keys, q.len - q.n + last + 1) + kChunkKeys - 1) / kChunkKeys);
 }
 __device__ __forceinline__ int chunk_row_tiles(const AttnReq& q) { return (q.rows + kChunkRows - 1) / kChunkRows; }
+template <int SEE>
 __device__ __forceinline__ int64_t chunk_head_cost(const ChunkParams& c, const AttnReq& q) {
   int64_t s = 0;
   ChunkWalk w;
   const int n = chunk_row_tiles(q);
-  for (int rt = 0; rt < n; ++rt, w.step(c)) s += chunk_tiles(c.a, q, w) + kChunkUnitCost;
+  for (int rt = 0; rt < n; ++rt, w.step(c)) s += chunk_tiles<SEE>(c.a, q, w) + kChunkUnitCost;
   return s;
 }
+template <int SEE>
 __device__ __forceinline__ int64_t chunk_cost(const ChunkParams& c, const AttnReq& q) {
   if (q.n == 0 || q.rows <= c.min_rows) return 0;
-  return chunk_head_cost(c, q) * c.a.n_kv;
+  return chunk_head_cost<SEE>(c, q) * c.a.n_kv;
 }
 
 // What the roles need to know of a unit, in a small ring of shared memory: worked out once, ahead of its use.
@@ -117,7 +122,7 @@ struct __align__(16) ChunkUnit {
   int32_t rows;             // rows of the unit
   int32_t req, kvh;         // request and K/V head
   int32_t tok0, sub0;       // token (row of q) and query head of the group of the unit's row 0
-  int32_t lim_min;          // position of that token: last key that every row sees
+  int32_t lim_min;          // last key that every row sees: position of that token, or (tree) the one in front of the request's first new token
   int32_t key_end;          // one behind the last key that any row sees
   int32_t keys;             // keys of the request that the table can name
   int32_t whole;            // all tiles of the unit are here
@@ -131,18 +136,18 @@ struct ChunkSeg {
 };
 
 // The unit that place `off` of the line lies in; false when off lies behind the line.
-template <int THREADS>
+template <int SEE, int THREADS>
 __device__ __forceinline__ bool chunk_locate(const ChunkParams& c, const AttnLine<THREADS>& line, int64_t off, int64_t* s_warp, int64_t* s_found,
                                              ChunkSeg* seg) {
   int64_t start, rem;
-  seg->r = line.locate(c.a.nreq, [&](int i) { return chunk_cost(c, attn_request(c.a, i)); }, off, s_warp, s_found, &start);
+  seg->r = line.locate(c.a.nreq, [&](int i) { return chunk_cost<SEE>(c, attn_request<SEE>(c.a, i)); }, off, s_warp, s_found, &start);
   if (seg->r < 0) return false;
-  seg->q = attn_request(c.a, seg->r);
-  seg->kvh = (int)attn_div(off - start, chunk_head_cost(c, seg->q), &rem);
+  seg->q = attn_request<SEE>(c.a, seg->r);
+  seg->kvh = (int)attn_div(off - start, chunk_head_cost<SEE>(c, seg->q), &rem);
   seg->rt = 0;
   seg->w = ChunkWalk();
   for (;;) {
-    seg->tiles = chunk_tiles(c.a, seg->q, seg->w);
+    seg->tiles = chunk_tiles<SEE>(c.a, seg->q, seg->w);
     if (rem < seg->tiles + kChunkUnitCost) break;
     rem -= seg->tiles + kChunkUnitCost;
     ++seg->rt;
@@ -153,6 +158,7 @@ __device__ __forceinline__ bool chunk_locate(const ChunkParams& c, const AttnLin
 }
 // The unit after seg; false behind the last request.  By a whole warp: the other roles of the CTA wait while requests of the other kernel
 // are passed over, 32 at a time (a million of them between two chunks: 4 ms).
+template <int SEE>
 __device__ __forceinline__ bool chunk_next(const ChunkParams& c, ChunkSeg* seg) {
   seg->pos = 0;
   seg->w.step(c);
@@ -166,7 +172,7 @@ __device__ __forceinline__ bool chunk_next(const ChunkParams& c, ChunkSeg* seg) 
         const int r = seg->r + (int)(threadIdx.x & 31);
         bool chunk = false;
         if (r < c.a.nreq) {
-          const AttnReq q = attn_request(c.a, r);
+          const AttnReq q = attn_request<SEE>(c.a, r);
           chunk = q.n != 0 && q.rows > c.min_rows;
         }
         here = __ballot_sync(0xffffffffu, chunk);
@@ -174,10 +180,10 @@ __device__ __forceinline__ bool chunk_next(const ChunkParams& c, ChunkSeg* seg) 
       }
       if (!here) return false;
       seg->r += __ffs(here) - 1;
-      seg->q = attn_request(c.a, seg->r);
+      seg->q = attn_request<SEE>(c.a, seg->r);
     }
   }
-  seg->tiles = chunk_tiles(c.a, seg->q, seg->w);
+  seg->tiles = chunk_tiles<SEE>(c.a, seg->q, seg->w);
   return true;
 }
 
@@ -315,7 +321,7 @@ struct ChunkNo {
   static constexpr bool value = false;
 };
 
-template <int D, bool FP8>
+template <int D, bool FP8, int SEE>
 __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const ChunkParams c) {
   using C = ChunkCfg<D, FP8>;
   const AttendParams& p = c.a;
@@ -381,7 +387,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
   const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_slot, 0);
   const uint32_t limit = c.spin_limit ? c.spin_limit : kChunkSpinLimit;
 
-  auto cost_of = [&](int i) { return chunk_cost(c, attn_request(p, i)); };
+  auto cost_of = [&](int i) { return chunk_cost<SEE>(c, attn_request<SEE>(p, i)); };
   int64_t off = 0, off_end = 0, share = 1;
   ChunkSeg seg;
   bool more = false;
@@ -391,7 +397,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
     share = attn_share(line.total, gridDim.x, c.min_share);
     off = blockIdx.x * share;
     off_end = min(line.total, off + share);
-    more = off < off_end && chunk_locate<kChunkThreads>(c, line, off, s_warp, s_found, &seg);
+    more = off < off_end && chunk_locate<SEE>(c, line, off, s_warp, s_found, &seg);
   };
   if (p.nreq > 32 * kLinePerLane) {
     find();           // (by the whole block; few requests are looked through by the describing warp alone)
@@ -597,14 +603,14 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
             u.kvh = seg.kvh;
             u.tok0 = seg.q.q0 + seg.w.tok;
             u.sub0 = seg.w.sub;
-            u.lim_min = seg.q.len - seg.q.n + seg.w.tok;
-            u.key_end = min(seg.q.keys, u.lim_min + group_div(p, u.sub0 + u.rows - 1) + 1);
+            u.lim_min = SEE == kSeeTree ? seg.q.len - seg.q.n - 1 : seg.q.len - seg.q.n + seg.w.tok;
+            u.key_end = SEE == kSeeTree ? seg.q.keys : min(seg.q.keys, u.lim_min + group_div(p, u.sub0 + u.rows - 1) + 1);
             u.keys = seg.q.keys;
             u.nt = u.key_end <= 0 ? 0 : u.t1 - u.t0;
             u.whole = u.t0 == 0 && u.t1 == tiles;
           }
           off += here;
-          more = off < off_end && chunk_next(c, &seg);
+          more = off < off_end && chunk_next<SEE>(c, &seg);
         }
         if (n == 0 && lane == 0) {
           AttnCut cut{};
@@ -789,7 +795,14 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
       }
       if (!loaded && nt > 0) load_queries(un);
       loaded = false;
-      const int lim_min = un.lim_min, lim = lim_min + group_div(p, un.sub0 + min(row, rows - 1)), t0 = un.t0;
+      const int lim_min = un.lim_min, lim = SEE == kSeeTree ? 0 : lim_min + group_div(p, un.sub0 + min(row, rows - 1)), t0 = un.t0;
+      const uint32_t* tree = nullptr;  // the row's bits
+      if constexpr (SEE == kSeeTree) tree = p.tree + (int64_t)(un.tok0 + group_div(p, un.sub0 + min(row, rows - 1))) * p.tree_words;
+      // which of the 32 keys from k on the row sees
+      auto row_sees = [&](uint32_t there, int k) {
+        if constexpr (SEE == kSeeTree) return tree_see(there, k, lim_min + 1, tree, p.tree_words);
+        return chunk_see(there, k, lim);
+      };
       float m = -INFINITY, l = 0.f, sc = p.scale_log2;
       bool any_bad = false;
       int v_at = 0;
@@ -823,7 +836,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
             float s[16];
             tmem_ld16(ts + part * 64 + b * 16, s);
             tmem_ld_wait();
-            if (with_mask.value) chunk_mask(s, chunk_see(b >= 2 ? there.y : there.x, k0 + (b >> 1) * 32, lim) >> ((b & 1) * 16));
+            if (with_mask.value) chunk_mask(s, row_sees(b >= 2 ? there.y : there.x, k0 + (b >> 1) * 32) >> ((b & 1) * 16));
 #pragma unroll
             for (int e = 0; e < 16; e += 2) {
               float w0, w1;
@@ -858,7 +871,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
               tmem_ld32(ts + part * 64 + b * 32, s);
               tmem_ld_wait();
               if (masked) {
-                const uint32_t see = chunk_see(b ? there.y : there.x, k0 + b * 32, lim);
+                const uint32_t see = row_sees(b ? there.y : there.x, k0 + b * 32);
                 chunk_mask(s, see);
                 chunk_mask(s + 16, see >> 16);
               }
@@ -955,8 +968,9 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
           // they decide the sum
           const int32_t* table = p.tables + (int64_t)un.req * p.max_blocks;
           const int from = max(t0, (lim_min + 1) / kChunkKeys) * kChunkKeys;
-          const int to_key = min(min(lim, un.keys - 1), un.t1 * kChunkKeys - 1);
+          const int to_key = min(SEE == kSeeTree ? un.keys - 1 : min(lim, un.keys - 1), un.t1 * kChunkKeys - 1);
           for (int key = from; key <= to_key; ++key) {
+            if (SEE == kSeeTree && !row_sees(1u, key)) continue;
             const int32_t blk = __ldg(table + key / p.block_size);
             if (blk < 0 || blk >= p.num_blocks) continue;
             const uint8_t* v = p.v_cache + blk * p.block_stride + (key % p.block_size) * p.token_stride + un.kvh * p.head_stride;

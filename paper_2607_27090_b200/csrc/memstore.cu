@@ -28,6 +28,8 @@
 #include "attend.cuh"
 #include "attend_chunk.cuh"
 #include "blocks.cuh"
+#include "select.cuh"
+#include "tree.cuh"
 
 using namespace ms;
 

@@ -1,10 +1,10 @@
-// Host side of the serving calls (memstore_grow_blocks, memstore_release_blocks, memstore_append, memstore_attend); included by
-// memstore.cu inside extern "C".  None of them uses scratch of the store
-// (memstore_attend sets one word of it when a wait ran out).
+// Host side of the serving calls (memstore_grow_blocks, memstore_release_blocks, memstore_append, memstore_attend, drafted trees, selected
+// blocks); included by memstore.cu inside extern "C".  None of them uses scratch of the store
+// (memstore_attend and memstore_attend_tree set one word of it when a wait ran out).
 
 static_assert(kReqTableShort == MS_REQ_BLOCK_TABLE_SHORT && kReqBadBlock == MS_REQ_BAD_BLOCK_ID && kReqPosOverflow == MS_REQ_POSITION_OVERFLOW &&
                   kReqTimeout == MS_REQ_KERNEL_TIMEOUT && kReqBadStart == MS_REQ_BAD_START && kReqNoBlocks == MS_REQ_NO_BLOCKS &&
-                  kReqBadLength == MS_REQ_BAD_LENGTH,
+                  kReqBadLength == MS_REQ_BAD_LENGTH && kReqBadTree == MS_REQ_BAD_TREE,
               "status bits of the kernels and the header");
 
 // Counts are at most 2^30, so that the kernels' 32-bit loops end before they wrap.
@@ -37,7 +37,7 @@ static ms_status check_cache(memstore* s, const ms_paged_cache* c, int32_t layer
     if (!(c->k_scale > 0.f && c->v_scale > 0.f && std::isfinite(c->k_scale) && std::isfinite(c->v_scale)))
       return fail(s, MS_ERR_INVALID_ARG, "an 8-bit cache needs finite positive k_scale and v_scale");
     if (reads && ((c->layer_stride | c->block_stride | c->token_stride | c->head_stride) % 16))
-      return fail(s, MS_ERR_UNSUPPORTED, "memstore_attend reads an 8-bit cache whose strides are multiples of 16");
+      return fail(s, MS_ERR_UNSUPPORTED, "this call reads an 8-bit cache whose strides are multiples of 16");
   }
   return MS_OK;
 }
@@ -235,28 +235,30 @@ static AttendLayout attend_layout(const memstore* s) {
 
 extern "C++" {
 // Shared-memory limits of the attention kernels, raised once per device.
-template <int D, bool FP8>
+template <int D, bool FP8, int SEE>
 static cudaError_t attend_prepare(int device) {
   static std::mutex mu;
   static bool done[64] = {false};
   std::lock_guard<std::mutex> lock(mu);
   if (done[device & 63]) return cudaSuccess;
-  cudaError_t e = cudaFuncSetAttribute(attend_rows_kernel<D, FP8>, cudaFuncAttributeMaxDynamicSharedMemorySize, AttnCfg<D, FP8>::kSmemBytes);
-  if constexpr (D == 64 || D == 128)
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(attend_chunk_kernel<D, FP8>, cudaFuncAttributeMaxDynamicSharedMemorySize, (ChunkCfg<D, FP8>::kSmemBytes));
+  cudaError_t e = cudaFuncSetAttribute(attend_rows_kernel<D, FP8, SEE>, cudaFuncAttributeMaxDynamicSharedMemorySize, AttnCfg<D, FP8>::kSmemBytes);
+  if constexpr (SEE != kSeeBlocks && (D == 64 || D == 128))
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(attend_chunk_kernel<D, FP8, SEE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (ChunkCfg<D, FP8>::kSmemBytes));
   if (e == cudaSuccess) done[device & 63] = true;
   return e;
 }
 
-template <int D, bool FP8>
+template <int D, bool FP8, int SEE>
 static ms_status attend_launch(memstore* s, ChunkParams& c, int64_t max_rows, cudaStream_t st) {
-  MS_CUDA(s, (attend_prepare<D, FP8>(s->cfg.device)));
+  MS_CUDA(s, (attend_prepare<D, FP8, SEE>(s->cfg.device)));
   AttendParams& p = c.a;
   // Which kernels: the chunk kernel when a request may have more rows than the rows kernel serves well, the rows kernel when a
   // request may have fewer.  A single request whose rows are probably many goes to the chunk kernel whatever it turns out to be,
   // and one kernel is saved.
   const int min_rows = chunk_min_rows((int64_t)p.n_kv * p.nreq, s->sm_count);
-  bool chunks = (D == 64 || D == 128) && max_rows > min_rows;
+  // (tokens that read lists of blocks of their own have no keys in common: nothing for the chunk kernel)
+  constexpr bool kChunks = SEE != kSeeBlocks && (D == 64 || D == 128);
+  const bool chunks = kChunks && max_rows > min_rows;
   const bool rows = !chunks || p.nreq > 1;
   c.min_rows = rows ? min_rows : 0;
   p.max_rows = chunks ? c.min_rows : 0x7fffffff;
@@ -266,24 +268,25 @@ static ms_status attend_launch(memstore* s, ChunkParams& c, int64_t max_rows, cu
   const int64_t all_rows = (int64_t)p.n_tokens * p.group;
   p.tile_shift = __builtin_ctz((unsigned)AttnCfg<D, FP8>::kTileKeys);
   int chunk_ctas = 0, rows_ctas = 0;
-  if constexpr (D == 64 || D == 128) {
+  if constexpr (kChunks) {
     if (chunks) {
       chunk_ctas = s->sm_count;
-      MS_CUDA(s, launch_dependent(attend_chunk_kernel<D, FP8>, dim3((unsigned)chunk_ctas), dim3(kChunkThreads), (ChunkCfg<D, FP8>::kSmemBytes), st, c));
+      MS_CUDA(s, launch_dependent(attend_chunk_kernel<D, FP8, SEE>, dim3((unsigned)chunk_ctas), dim3(kChunkThreads), (ChunkCfg<D, FP8>::kSmemBytes), st, c));
       s->kernels_launched++;
       s->attn_chunks = true;
     }
   }
   if (rows) {
     rows_ctas = s->sm_count * AttnCfg<D, FP8>::kCtasPerSm;
-    MS_CUDA(s, launch_dependent(attend_rows_kernel<D, FP8>, dim3((unsigned)rows_ctas), dim3(kAttnThreads), AttnCfg<D, FP8>::kSmemBytes, st, p));
+    MS_CUDA(s, launch_dependent(attend_rows_kernel<D, FP8, SEE>, dim3((unsigned)rows_ctas), dim3(kAttnThreads), AttnCfg<D, FP8>::kSmemBytes, st, p));
     s->kernels_launched++;
   }
   const int checks = p.status ? (p.nreq + kCombineThreads / 32 - 1) / (kCombineThreads / 32) : 0;
   // units that the call can have at most, whatever the lengths on the device say, and so cuts to join (each unit has one first border)
   const int64_t units = (int64_t)p.n_kv * p.nreq;
+  const int64_t row_units = SEE == kSeeBlocks ? (int64_t)p.n_kv * p.n_tokens * p.token_tiles : units * (all_rows / kAttnRows + 1);
   const int chunk_joins = (int)std::max<int64_t>(0, std::min<int64_t>(chunk_ctas - 1, units * (all_rows / kChunkRows + 1)));
-  const int rows_joins = (int)std::max<int64_t>(0, std::min<int64_t>(rows_ctas - 1, units * (all_rows / kAttnRows + 1)));
+  const int rows_joins = (int)std::max<int64_t>(0, std::min<int64_t>(rows_ctas - 1, row_units));
   // Few cuts are spread over more blocks: 61 tokens of one request (8 cuts) 25 us with 16 pieces a cut, 39 with 4; a batch with 147 cuts
   // 57 us with 4, 60 with 16.
   const int pieces = chunk_joins <= 32 ? kChunkRows / kChunkJoinRows : 4;
@@ -296,14 +299,34 @@ static ms_status attend_launch(memstore* s, ChunkParams& c, int64_t max_rows, cu
 }
 }  // extern "C++"
 
+extern "C++" {
+template <int SEE>
+static ms_status attend_dispatch(memstore* s, ChunkParams& cp, bool fp8, int64_t max_rows, cudaStream_t st) {
+  switch (s->cfg.head_dim) {
+    case 16: return fp8 ? attend_launch<16, true, SEE>(s, cp, max_rows, st) : attend_launch<16, false, SEE>(s, cp, max_rows, st);
+    case 32: return fp8 ? attend_launch<32, true, SEE>(s, cp, max_rows, st) : attend_launch<32, false, SEE>(s, cp, max_rows, st);
+    case 64: return fp8 ? attend_launch<64, true, SEE>(s, cp, max_rows, st) : attend_launch<64, false, SEE>(s, cp, max_rows, st);
+    case 128: return fp8 ? attend_launch<128, true, SEE>(s, cp, max_rows, st) : attend_launch<128, false, SEE>(s, cp, max_rows, st);
+    default: return fp8 ? attend_launch<256, true, SEE>(s, cp, max_rows, st) : attend_launch<256, false, SEE>(s, cp, max_rows, st);
+  }
+}
+}  // extern "C++"
+
 size_t memstore_attend_workspace(memstore_t* s) { return s ? attend_layout(s).bytes : 0; }
 
-ms_status memstore_attend(memstore_t* s, int32_t layer, const ms_heads* q, int32_t n_q_heads, int32_t n_tokens, const int32_t* q_start,
-                          const int32_t* seq_lens, int32_t nreq, const int32_t* block_tables, int32_t max_blocks, const ms_paged_cache* cache,
-                          float scale, int32_t max_q_len, const ms_heads* out, float* out_lse, int32_t* out_status, void* workspace,
-                          size_t workspace_bytes, ms_stream stream) {
-  Range range("memstore_attend");
-  if (!s) return MS_ERR_INVALID_ARG;
+// What a row sees besides the arguments that all attention calls have: a tree's bits, or lists of blocks.
+struct AttendSees {
+  int see = kSeeCausal;
+  const uint32_t* tree = nullptr;
+  int32_t words = 0;
+  const int32_t* lists = nullptr;
+  int32_t list_len = 0;
+};
+
+static ms_status attend_any(memstore* s, int32_t layer, const ms_heads* q, int32_t n_q_heads, int32_t n_tokens, const int32_t* q_start,
+                            const int32_t* seq_lens, int32_t nreq, const int32_t* block_tables, int32_t max_blocks, const ms_paged_cache* cache,
+                            float scale, int32_t max_q_len, const ms_heads* out, float* out_lse, int32_t* out_status, void* workspace,
+                            size_t workspace_bytes, ms_stream stream, const AttendSees& sees) {
   std::lock_guard<std::recursive_mutex> lock(s->mu);
   const memstore_config& c = s->cfg;
   if (n_tokens < 0 || nreq < 0 || max_blocks < 0 || max_q_len < 0)
@@ -319,6 +342,15 @@ ms_status memstore_attend(memstore_t* s, int32_t layer, const ms_heads* q, int32
   if (rc == MS_OK && nreq > kMaxAttendReqs) rc = fail(s, MS_ERR_UNSUPPORTED, "%d requests in one attention call (at most 2^26)", nreq);
   if (rc == MS_OK) rc = check_heads(s, q, n_tokens, n_q_heads, false, "q");
   if (rc == MS_OK) rc = check_heads(s, out, n_tokens, n_q_heads, true, "out");
+  if (rc == MS_OK && sees.see == kSeeTree) {
+    if (sees.words < 1 || sees.words > kTreeMaxWords) rc = fail(s, MS_ERR_INVALID_ARG, "mask_words=%d (1 to %d)", sees.words, kTreeMaxWords);
+    else if (!sees.tree && n_tokens > 0) rc = fail(s, MS_ERR_INVALID_ARG, "tree_mask is NULL");
+  }
+  if (rc == MS_OK && sees.see == kSeeBlocks) {
+    if (sees.list_len < 1) rc = fail(s, MS_ERR_INVALID_ARG, "n_select=%d", sees.list_len);
+    else if ((int64_t)sees.list_len * cache->block_size > kAttnMaxLen) rc = fail(s, MS_ERR_UNSUPPORTED, "%d blocks of %d keys", sees.list_len, cache->block_size);
+    else if (!sees.lists && n_tokens > 0) rc = fail(s, MS_ERR_INVALID_ARG, "blocks is NULL");
+  }
   if (rc != MS_OK) return rc;
   if (nreq == 0) return MS_OK;
   if (!q_start || !seq_lens || (max_blocks > 0 && !block_tables)) return fail(s, MS_ERR_INVALID_ARG, "null request arrays");
@@ -376,11 +408,270 @@ ms_status memstore_attend(memstore_t* s, int32_t layer, const ms_heads* q, int32
   cp.mute_producer = s->test_mute_producers;
   const int64_t max_rows = (int64_t)(max_q_len > 0 && max_q_len < n_tokens ? max_q_len : n_tokens) * group;
   cudaStream_t st = (cudaStream_t)stream;
-  switch (c.head_dim) {
-    case 16: return fp8 ? attend_launch<16, true>(s, cp, max_rows, st) : attend_launch<16, false>(s, cp, max_rows, st);
-    case 32: return fp8 ? attend_launch<32, true>(s, cp, max_rows, st) : attend_launch<32, false>(s, cp, max_rows, st);
-    case 64: return fp8 ? attend_launch<64, true>(s, cp, max_rows, st) : attend_launch<64, false>(s, cp, max_rows, st);
-    case 128: return fp8 ? attend_launch<128, true>(s, cp, max_rows, st) : attend_launch<128, false>(s, cp, max_rows, st);
-    default: return fp8 ? attend_launch<256, true>(s, cp, max_rows, st) : attend_launch<256, false>(s, cp, max_rows, st);
+  p.tree = sees.tree;
+  p.tree_words = sees.words;
+  p.lists = sees.lists;
+  p.list_len = sees.list_len;
+  p.token_tiles = (group + kAttnRows - 1) / kAttnRows;
+  if (sees.see == kSeeTree) return attend_dispatch<kSeeTree>(s, cp, fp8, max_rows, st);
+  if (sees.see == kSeeBlocks) return attend_dispatch<kSeeBlocks>(s, cp, fp8, max_rows, st);
+  return attend_dispatch<kSeeCausal>(s, cp, fp8, max_rows, st);
+}
+
+ms_status memstore_attend(memstore_t* s, int32_t layer, const ms_heads* q, int32_t n_q_heads, int32_t n_tokens, const int32_t* q_start,
+                          const int32_t* seq_lens, int32_t nreq, const int32_t* block_tables, int32_t max_blocks, const ms_paged_cache* cache,
+                          float scale, int32_t max_q_len, const ms_heads* out, float* out_lse, int32_t* out_status, void* workspace,
+                          size_t workspace_bytes, ms_stream stream) {
+  Range range("memstore_attend");
+  if (!s) return MS_ERR_INVALID_ARG;
+  return attend_any(s, layer, q, n_q_heads, n_tokens, q_start, seq_lens, nreq, block_tables, max_blocks, cache, scale, max_q_len, out, out_lse, out_status,
+                    workspace, workspace_bytes, stream, AttendSees());
+}
+
+// ---- drafted trees ----------------------------------------------------------------------------------------------------
+ms_status memstore_plan_tree(memstore_t* s, const int32_t* parents, int32_t n_tokens, const int32_t* q_start, int32_t nreq, const int32_t* positions,
+                             int32_t mask_words, int32_t* out_positions, uint32_t* out_mask, int32_t* out_status, ms_stream stream) {
+  Range range("memstore_plan_tree");
+  if (!s) return MS_ERR_INVALID_ARG;
+  std::lock_guard<std::recursive_mutex> lock(s->mu);
+  if (n_tokens < 0 || nreq < 0) return fail(s, MS_ERR_INVALID_ARG, "n_tokens=%d nreq=%d", n_tokens, nreq);
+  if (mask_words < 1 || mask_words > kTreeMaxWords) return fail(s, MS_ERR_INVALID_ARG, "mask_words=%d (1 to %d)", mask_words, kTreeMaxWords);
+  const ms_status rc = check_counts(s, n_tokens, nreq, 0);
+  if (rc != MS_OK) return rc;
+  if (nreq == 0) return MS_OK;
+  if (!q_start || (n_tokens > 0 && (!parents || !positions))) return fail(s, MS_ERR_INVALID_ARG, "null request arrays");
+  DeviceGuard g(s->cfg.device);
+  const TreePlanParams p{parents, q_start, positions, n_tokens, nreq, mask_words, out_positions, out_mask, out_status};
+  MS_CUDA(s, launch_dependent(plan_tree_kernel, dim3((unsigned)nreq), dim3(kTreeThreads), (size_t)mask_words * 32 * 4, (cudaStream_t)stream, p));
+  s->kernels_launched++;
+  return MS_OK;
+}
+
+ms_status memstore_attend_tree(memstore_t* s, int32_t layer, const ms_heads* q, int32_t n_q_heads, int32_t n_tokens, const int32_t* q_start,
+                               const int32_t* seq_lens, int32_t nreq, const uint32_t* tree_mask, int32_t mask_words, const int32_t* block_tables,
+                               int32_t max_blocks, const ms_paged_cache* cache, float scale, int32_t max_q_len, const ms_heads* out, float* out_lse,
+                               int32_t* out_status, void* workspace, size_t workspace_bytes, ms_stream stream) {
+  Range range("memstore_attend_tree");
+  if (!s) return MS_ERR_INVALID_ARG;
+  AttendSees sees;
+  sees.see = kSeeTree;
+  sees.tree = tree_mask;
+  sees.words = mask_words;
+  return attend_any(s, layer, q, n_q_heads, n_tokens, q_start, seq_lens, nreq, block_tables, max_blocks, cache, scale, max_q_len, out, out_lse, out_status,
+                    workspace, workspace_bytes, stream, sees);
+}
+
+ms_status memstore_accept(memstore_t* s, const int32_t* parents, const int32_t* tokens, const int32_t* choices, const int32_t* positions,
+                          int32_t n_tokens, const int32_t* q_start, const int32_t* seq_lens, int32_t nreq, const int32_t* block_tables,
+                          int32_t max_blocks, const ms_paged_cache* cache, int32_t* free_blocks, int32_t n_free, const int32_t* n_taken,
+                          int32_t* out_path, int32_t* out_n_accepted, int32_t* out_next, int32_t* out_seq_lens, int32_t* out_n_taken,
+                          int32_t* out_status, ms_stream stream) {
+  Range range("memstore_accept");
+  if (!s) return MS_ERR_INVALID_ARG;
+  std::lock_guard<std::recursive_mutex> lock(s->mu);
+  const memstore_config& c = s->cfg;
+  if (n_tokens < 0 || nreq < 0 || max_blocks < 0 || n_free < 0)
+    return fail(s, MS_ERR_INVALID_ARG, "n_tokens=%d nreq=%d max_blocks=%d n_free=%d", n_tokens, nreq, max_blocks, n_free);
+  ms_status rc = check_cache(s, cache, 0, true);
+  if (rc == MS_OK) rc = check_counts(s, n_tokens, nreq, max_blocks);
+  if (rc != MS_OK) return rc;
+  if ((nreq > 0 && (!q_start || !seq_lens || !out_n_accepted || !out_next || !out_seq_lens || !out_status || (max_blocks > 0 && !block_tables))) ||
+      (n_tokens > 0 && (!parents || !tokens || !choices || !positions || !out_path)) || (free_blocks && (!n_taken || !out_n_taken)))
+    return fail(s, MS_ERR_INVALID_ARG, "null request arrays");
+  DeviceGuard g(c.device);
+  const bool fp8 = cache->dtype == MS_CACHE_FP8_E4M3;
+  const int64_t esz = fp8 ? 1 : 2;
+  AcceptParams p{};
+  p.parents = parents;
+  p.tokens = tokens;
+  p.choices = choices;
+  p.positions = positions;
+  p.n_tokens = n_tokens;
+  p.q_start = q_start;
+  p.seq_lens = seq_lens;
+  p.nreq = nreq;
+  p.tables = block_tables;
+  p.max_blocks = max_blocks;
+  p.block_size = cache->block_size;
+  p.num_blocks = cache->num_blocks;
+  p.free_blocks = free_blocks;
+  p.n_free = n_free;
+  p.n_taken = n_taken;
+  p.out_lens = out_seq_lens;
+  p.path = out_path;
+  p.n_accepted = out_n_accepted;
+  p.next = out_next;
+  p.out_n_taken = out_n_taken;
+  p.status = out_status;
+  p.k_cache = (uint8_t*)cache->k_base;
+  p.v_cache = (uint8_t*)cache->v_base;
+  p.layer_stride = cache->layer_stride * esz;
+  p.block_stride = cache->block_stride * esz;
+  p.token_stride = cache->token_stride * esz;
+  p.head_stride = cache->head_stride * esz;
+  p.n_layers = c.n_layers;
+  p.n_kv = c.n_kv_heads;
+  p.row_chunks = (int32_t)(c.head_dim * esz / 16);
+  cudaStream_t st = (cudaStream_t)stream;
+  if (nreq > 0) {
+    MS_CUDA(s, launch_dependent(accept_walk_kernel, dim3((unsigned)((nreq + kWalkWarps - 1) / kWalkWarps)), dim3(kWalkWarps * 32), 0, st, p));
+    s->kernels_launched++;
   }
+  const int64_t columns = (int64_t)c.n_layers * 2 * c.n_kv_heads * p.row_chunks;
+  const int64_t items = (columns + kMoveThreads - 1) / kMoveThreads * nreq;
+  MS_CUDA(s, launch_dependent(accept_move_kernel, dim3(1u + (unsigned)std::min<int64_t>(items, (int64_t)s->sm_count * kMoveCtasPerSm)), dim3(kMoveThreads), 0, st, p));
+  s->kernels_launched++;
+  return MS_OK;
+}
+
+// ---- selected blocks --------------------------------------------------------------------------------------------------
+ms_status memstore_summarize_blocks(memstore_t* s, int32_t layer, const int32_t* q_start, int32_t n_tokens, const int32_t* seq_lens, int32_t nreq,
+                                    const int32_t* block_tables, int32_t max_blocks, const ms_paged_cache* cache, void* summaries, ms_stream stream) {
+  Range range("memstore_summarize_blocks");
+  if (!s) return MS_ERR_INVALID_ARG;
+  std::lock_guard<std::recursive_mutex> lock(s->mu);
+  const memstore_config& c = s->cfg;
+  if (n_tokens < 0 || nreq < 0 || max_blocks < 0) return fail(s, MS_ERR_INVALID_ARG, "n_tokens=%d nreq=%d max_blocks=%d", n_tokens, nreq, max_blocks);
+  ms_status rc = check_cache(s, cache, layer, true);
+  if (rc == MS_OK) rc = check_counts(s, n_tokens, nreq, max_blocks);
+  if (rc == MS_OK && nreq > kMaxAttendReqs) rc = fail(s, MS_ERR_UNSUPPORTED, "%d requests in one call (at most 2^26)", nreq);
+  if (rc != MS_OK) return rc;
+  if (!summaries || ((uintptr_t)summaries & 15)) return fail(s, MS_ERR_INVALID_ARG, "summaries must be 16-byte aligned");
+  if (nreq == 0 || max_blocks == 0) return MS_OK;
+  if (!seq_lens || !block_tables) return fail(s, MS_ERR_INVALID_ARG, "null request arrays");
+  DeviceGuard g(c.device);
+  const bool fp8 = cache->dtype == MS_CACHE_FP8_E4M3;
+  const int64_t esz = fp8 ? 1 : 2;
+  SummaryParams p{};
+  p.q_start = q_start;
+  p.n_tokens = n_tokens;
+  p.seq_lens = seq_lens;
+  p.nreq = nreq;
+  p.tables = block_tables;
+  p.max_blocks = max_blocks;
+  p.block_size = cache->block_size;
+  p.num_blocks = cache->num_blocks;
+  p.k_cache = (const uint8_t*)cache->k_base + layer * cache->layer_stride * esz;
+  p.block_stride = cache->block_stride * esz;
+  p.token_stride = cache->token_stride * esz;
+  p.head_stride = cache->head_stride * esz;
+  p.n_kv = c.n_kv_heads;
+  p.summaries = (uint4*)summaries;
+  // blocks that the call can touch at most: a request's new tokens begin and end inside a block
+  const int64_t blocks = q_start ? n_tokens / cache->block_size + 2 * (int64_t)nreq : (int64_t)nreq * max_blocks;
+  const int64_t ctas = (blocks * c.n_kv_heads + kSummaryThreads / 32 - 1) / (kSummaryThreads / 32);
+  const dim3 grid((unsigned)std::min<int64_t>(ctas, (int64_t)s->sm_count * kSummaryCtasPerSm));
+  void (*kernel)(SummaryParams) = nullptr;
+  switch (c.head_dim) {
+    case 16: kernel = fp8 ? summarize_kernel<16, true> : summarize_kernel<16, false>; break;
+    case 32: kernel = fp8 ? summarize_kernel<32, true> : summarize_kernel<32, false>; break;
+    case 64: kernel = fp8 ? summarize_kernel<64, true> : summarize_kernel<64, false>; break;
+    case 128: kernel = fp8 ? summarize_kernel<128, true> : summarize_kernel<128, false>; break;
+    default: kernel = fp8 ? summarize_kernel<256, true> : summarize_kernel<256, false>; break;
+  }
+  MS_CUDA(s, launch_dependent(kernel, grid, dim3(kSummaryThreads), 0, (cudaStream_t)stream, p));
+  s->kernels_launched++;
+  return MS_OK;
+}
+
+// Shared-memory limit and cluster size of the selection kernels, raised once per device.
+static cudaError_t select_prepare(int device, const void* kernel) {
+  static std::mutex mu;
+  static const void* done[64][5] = {};
+  std::lock_guard<std::mutex> lock(mu);
+  for (const void*& d : done[device & 63]) {
+    if (d == kernel) return cudaSuccess;
+    if (d) continue;
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSelectMaxBlocks * 4);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e == cudaSuccess) d = kernel;
+    return e;
+  }
+  return cudaSuccess;
+}
+
+ms_status memstore_select_blocks(memstore_t* s, const ms_heads* q, int32_t n_q_heads, int32_t n_tokens, const int32_t* q_start, const int32_t* seq_lens,
+                                 int32_t nreq, const void* summaries, const int32_t* block_tables, int32_t max_blocks, const ms_paged_cache* cache,
+                                 int32_t n_select, int32_t n_first, int32_t n_last, int32_t* out_blocks, float* out_scores, ms_stream stream) {
+  Range range("memstore_select_blocks");
+  if (!s) return MS_ERR_INVALID_ARG;
+  std::lock_guard<std::recursive_mutex> lock(s->mu);
+  const memstore_config& c = s->cfg;
+  if (n_tokens < 0 || nreq < 0 || max_blocks < 0) return fail(s, MS_ERR_INVALID_ARG, "n_tokens=%d nreq=%d max_blocks=%d", n_tokens, nreq, max_blocks);
+  if (n_q_heads <= 0 || n_q_heads % c.n_kv_heads) return fail(s, MS_ERR_INVALID_ARG, "%d query heads for %d K/V heads", n_q_heads, c.n_kv_heads);
+  if (n_select < 1 || n_first < 0 || n_last < 0 || (int64_t)n_first + n_last > n_select)
+    return fail(s, MS_ERR_INVALID_ARG, "n_select=%d n_first=%d n_last=%d", n_select, n_first, n_last);
+  ms_status rc = check_geometry(s, cache);
+  if (rc == MS_OK) rc = check_counts(s, n_tokens, nreq, n_select);
+  if (rc == MS_OK && max_blocks > kSelectMaxBlocks) rc = fail(s, MS_ERR_UNSUPPORTED, "%d blocks per table (at most %d)", max_blocks, kSelectMaxBlocks);
+  if (rc == MS_OK && (int64_t)n_tokens * c.n_kv_heads > kMaxCount) rc = fail(s, MS_ERR_UNSUPPORTED, "%d tokens of %d K/V heads", n_tokens, c.n_kv_heads);
+  if (rc == MS_OK) rc = check_heads(s, q, n_tokens, n_q_heads, false, "q");
+  if (rc != MS_OK) return rc;
+  if (!summaries || ((uintptr_t)summaries & 15)) return fail(s, MS_ERR_INVALID_ARG, "summaries must be 16-byte aligned");
+  if (nreq == 0 || n_tokens == 0) return MS_OK;
+  if (!q_start || !seq_lens || !out_blocks || (max_blocks > 0 && !block_tables)) return fail(s, MS_ERR_INVALID_ARG, "null request arrays");
+  DeviceGuard g(c.device);
+  SelectParams p{};
+  p.q = (const __nv_bfloat16*)q->base;
+  p.q_ts = q->token_stride;
+  p.q_hs = q->head_stride;
+  p.n_q = n_q_heads;
+  p.n_kv = c.n_kv_heads;
+  p.group = n_q_heads / c.n_kv_heads;
+  p.n_tokens = n_tokens;
+  p.q_start = q_start;
+  p.seq_lens = seq_lens;
+  p.nreq = nreq;
+  p.summaries = (const uint4*)summaries;
+  p.tables = block_tables;
+  p.max_blocks = max_blocks;
+  p.block_size = cache->block_size;
+  p.num_blocks = cache->num_blocks;
+  p.n_select = n_select;
+  p.n_first = n_first;
+  p.n_last = n_last;
+  p.blocks = out_blocks;
+  p.scores = out_scores;
+  void (*kernel)(SelectParams) = c.head_dim == 16 ? select_kernel<16> : c.head_dim == 32 ? select_kernel<32> : c.head_dim == 64 ? select_kernel<64>
+                               : c.head_dim == 128 ? select_kernel<128> : select_kernel<256>;
+  MS_CUDA(s, select_prepare(c.device, (const void*)kernel));
+  // CTAs of a cluster: as many as find an SM of their own, each with some hundred blocks to score
+  const int64_t units = (int64_t)n_tokens * c.n_kv_heads;
+  unsigned parts = 1;
+  while (parts < 16 && units * parts * 2 <= s->sm_count && max_blocks >= (int)parts * 2 * 128) parts *= 2;
+  cudaLaunchConfig_t lc{};
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  lc.blockDim = dim3(kSelectThreads);
+  lc.dynamicSmemBytes = (size_t)max_blocks * 4;
+  lc.stream = (cudaStream_t)stream;
+  lc.attrs = attr;
+  lc.numAttrs = 2;
+  for (;; parts /= 2) {  // a cluster that the device cannot hold at once with this much shared memory: halve it
+    attr[1].val.clusterDim.x = parts;
+    lc.gridDim = dim3((unsigned)(units * parts));
+    int n_clusters = 0;
+    if (parts == 1 || (cudaOccupancyMaxActiveClusters(&n_clusters, kernel, &lc) == cudaSuccess && n_clusters > 0)) break;
+    (void)cudaGetLastError();
+  }
+  MS_CUDA(s, cudaLaunchKernelEx(&lc, kernel, p));
+  s->kernels_launched++;
+  return MS_OK;
+}
+
+ms_status memstore_attend_blocks(memstore_t* s, int32_t layer, const ms_heads* q, int32_t n_q_heads, int32_t n_tokens, const int32_t* q_start,
+                                 const int32_t* seq_lens, int32_t nreq, const int32_t* blocks, int32_t n_select, const int32_t* block_tables,
+                                 int32_t max_blocks, const ms_paged_cache* cache, float scale, const ms_heads* out, float* out_lse,
+                                 int32_t* out_status, void* workspace, size_t workspace_bytes, ms_stream stream) {
+  Range range("memstore_attend_blocks");
+  if (!s) return MS_ERR_INVALID_ARG;
+  AttendSees sees;
+  sees.see = kSeeBlocks;
+  sees.lists = blocks;
+  sees.list_len = n_select;
+  return attend_any(s, layer, q, n_q_heads, n_tokens, q_start, seq_lens, nreq, block_tables, max_blocks, cache, scale, 0, out, out_lse, out_status,
+                    workspace, workspace_bytes, stream, sees);
 }

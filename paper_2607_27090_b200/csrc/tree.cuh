@@ -1,0 +1,273 @@
+// Drafted trees of tokens: positions and visibility masks from parents (memstore_plan_tree), and what is left of a tree once the model has
+// said what follows each node (memstore_accept).
+//
+// A request's new tokens are the nodes of a tree: node 0 is the certain token, node i hangs on a node before it.  Their keys and values lie in
+// the cache one after another, in node order, whatever their positions.
+#pragma once
+#include "blocks.cuh"
+
+namespace ms {
+
+constexpr int32_t kReqBadTree = 512;
+constexpr int kTreeThreads = 128;
+
+struct TreePlanParams {
+  const int32_t* parents;
+  const int32_t* q_start;
+  const int32_t* positions;
+  int32_t n_tokens, nreq, words;
+  int32_t* out_positions;  // may be positions
+  uint32_t* mask;          // [n_tokens][words]
+  int32_t* status;
+};
+
+// A CTA per request, a thread per node: the walk from a node to its root counts the node's depth and meets its ancestors in falling order,
+// so that the words of the mask are finished one after another and written once.  Latency-bound: a request's parents are read once into
+// shared memory, a step of the walk is one access to it.
+__global__ void __launch_bounds__(kTreeThreads) plan_tree_kernel(const TreePlanParams p) {
+  extern __shared__ int32_t s_parent[];  // [32 * words]
+  grid_dependency_wait();
+  grid_launch_dependents();
+  const int r = blockIdx.x;
+  const int32_t q0 = p.q_start[r], q1 = p.q_start[r + 1];
+  const bool fits = q0 >= 0 && q1 >= q0 && q1 <= p.n_tokens && q1 - q0 <= 32 * p.words;
+  if (!fits) {
+    if (p.status && threadIdx.x == 0) p.status[r] = kReqBadLength;
+    return;
+  }
+  const int n = q1 - q0;
+  const int32_t base = n > 0 ? p.positions[q0] : 0;
+  bool bad = false;
+  for (int i = threadIdx.x; i < n; i += kTreeThreads) {
+    const int32_t up = p.parents[q0 + i];
+    bad = bad || up < -1 || up >= i;
+    s_parent[i] = up;
+  }
+  bad = __syncthreads_or(bad);
+  if (p.status && threadIdx.x == 0) p.status[r] = bad ? kReqBadTree : 0;
+  for (int i = threadIdx.x; i < n; i += kTreeThreads) {
+    uint32_t* row = p.mask ? p.mask + (int64_t)(q0 + i) * p.words : nullptr;
+    int depth = -1, w = p.words - 1;
+    uint32_t acc = 0u;
+    if (!bad)
+      for (int c = i; c >= 0; c = s_parent[c]) {
+        for (; w > (c >> 5); --w) {
+          if (row) row[w] = acc;
+          acc = 0u;
+        }
+        acc |= 1u << (c & 31);
+        ++depth;
+      }
+    if (row)
+      for (; w >= 0; --w) {
+        row[w] = acc;
+        acc = 0u;
+      }
+    if (p.out_positions) p.out_positions[q0 + i] = bad || base < 0 ? -1 : base + depth;
+  }
+}
+
+struct AcceptParams {
+  const int32_t *parents, *tokens, *choices, *positions;  // [n_tokens]
+  int32_t n_tokens;
+  const int32_t* q_start;
+  const int32_t* seq_lens;
+  int32_t nreq;
+  const int32_t* tables;
+  int32_t max_blocks, block_size;
+  int64_t num_blocks;
+  int32_t* free_blocks;  // nullptr: the blocks behind the new end stay with the request
+  int32_t n_free;
+  const int32_t* n_taken;
+  int32_t *out_lens, *path, *n_accepted, *next, *out_n_taken, *status;
+  uint8_t *k_cache, *v_cache;
+  int64_t layer_stride, block_stride, token_stride, head_stride;  // bytes
+  int32_t n_layers, n_kv, row_chunks;                             // row_chunks: 16-byte pieces of a head's row
+};
+
+constexpr int kWalkWarps = 4;
+constexpr int kWalkRegs = 4;  // 32-node pieces of a tree that a warp keeps in registers
+
+// The walk down the trees, a warp per request.  At a node with the model's choice t it goes on to the node's lowest child with token t.
+// Children come behind their parents, so the walk looks at every node once at most.
+__global__ void __launch_bounds__(kWalkWarps * 32) accept_walk_kernel(const AcceptParams p) {
+  grid_dependency_wait();
+  grid_launch_dependents();
+  const int lane = threadIdx.x & 31;
+  const int64_t r = (int64_t)blockIdx.x * kWalkWarps + (threadIdx.x >> 5);
+  if (r >= p.nreq) return;
+  const int32_t q0 = p.q_start[r], q1 = p.q_start[r + 1], len = p.seq_lens[r];
+  const bool range = q0 >= 0 && q1 >= q0 && q1 <= p.n_tokens;
+  const int n = range ? q1 - q0 : 0;
+  int32_t st = range && len >= 0 ? 0 : kReqBadLength;
+  const int32_t start = n > 0 ? p.positions[q0] : 0;
+  if (st == 0 && n > 0) st = start < 0 ? kReqBadStart : (int64_t)start + n != len ? kReqBadLength : 0;
+  int a = 0;
+  int32_t said = -1;
+  if (st == 0 && n > 0) {
+    int32_t up[kWalkRegs], tok[kWalkRegs], choice[kWalkRegs];
+    const bool small = n <= 32 * kWalkRegs;
+    if (small) {
+#pragma unroll
+      for (int j = 0; j < kWalkRegs; ++j) {
+        const int i = 32 * j + lane;
+        up[j] = -2;
+        tok[j] = choice[j] = 0;
+        if (i < n) {
+          up[j] = p.parents[q0 + i];
+          tok[j] = p.tokens[q0 + i];
+          choice[j] = p.choices[q0 + i];
+        }
+      }
+    }
+    int cur = 0;
+    for (;;) {
+      if (lane == 0) p.path[q0 + a] = cur;
+      ++a;
+      int found = -1;
+      if (small) {
+        int32_t mine = choice[0];
+#pragma unroll
+        for (int j = 1; j < kWalkRegs; ++j)
+          if ((cur >> 5) == j) mine = choice[j];
+        said = __shfl_sync(0xffffffffu, mine, cur & 31);
+#pragma unroll
+        for (int j = kWalkRegs - 1; j >= 0; --j) {
+          const unsigned m = __ballot_sync(0xffffffffu, up[j] == cur && tok[j] == said && 32 * j + lane > cur);
+          if (m) found = 32 * j + __ffs(m) - 1;
+        }
+      } else {
+        said = p.choices[q0 + cur];
+        for (int i0 = cur & ~31; i0 < n && found < 0; i0 += 32) {
+          const int i = i0 + lane;
+          const unsigned m = __ballot_sync(0xffffffffu, i > cur && i < n && p.parents[q0 + i] == cur && p.tokens[q0 + i] == said);
+          if (m) found = i0 + __ffs(m) - 1;
+        }
+      }
+      if (found < 0) break;
+      cur = found;
+    }
+    __syncwarp();  // the path's entries are there for the other lanes
+    bool no_table = false, no_block = false;
+    auto look = [&](int32_t pos) {
+      const int b = pos / p.block_size;
+      if (b >= p.max_blocks) {
+        no_table = true;
+      } else {
+        const int32_t x = p.tables[r * p.max_blocks + b];
+        no_block = no_block || x < 0 || x >= p.num_blocks;
+      }
+    };
+    for (int i = lane; i < a; i += 32) {
+      const int from = __ldcg(p.path + q0 + i);
+      if (from != i) {
+        look(start + from);
+        look(start + i);
+      }
+    }
+    if (__any_sync(0xffffffffu, no_table)) st |= kReqTableShort;
+    if (__any_sync(0xffffffffu, no_block)) st |= kReqBadBlock;
+  }
+  for (int i = a + lane; i < n; i += 32) p.path[q0 + i] = -1;
+  __syncwarp();  // (out_lens may be seq_lens)
+  if (lane == 0) {
+    p.out_lens[r] = a > 0 ? start + a : len;
+    p.n_accepted[r] = a;
+    p.next[r] = said;
+    p.status[r] = st;
+  }
+}
+
+// Blocks behind the new ends go back to the free list: those of the first request that has some directly in front of entry *n_taken, those
+// of the next in front of them.  By one CTA.
+constexpr int kMoveThreads = 256;
+__device__ __forceinline__ void accept_trim(const AcceptParams& p, int64_t* s_warp) {
+  const int64_t taken = *p.n_taken;
+  const bool list_ok = taken >= 0 && taken <= p.n_free;
+  int64_t asked = 0, returned = 0;
+  for (int r0 = 0; r0 < p.nreq; r0 += kMoveThreads) {
+    const int r = r0 + threadIdx.x;
+    int first = 0, last = 0;  // table entries that go
+    const int32_t* t = p.tables;
+    if (r < p.nreq) {
+      const int a = p.n_accepted[r];
+      if (a > 0) {
+        const int64_t end = p.out_lens[r], was = end - a + (p.q_start[r + 1] - p.q_start[r]);
+        first = (int)min((end + p.block_size - 1) / p.block_size, (int64_t)p.max_blocks);
+        last = (int)min((was + p.block_size - 1) / p.block_size, (int64_t)p.max_blocks);
+        t = p.tables + (int64_t)r * p.max_blocks;
+      }
+    }
+    int count = 0;
+    for (int b = first; b < last; ++b) count += t[b] >= 0 && t[b] < p.num_blocks;
+    int64_t total, given;
+    const int64_t upto = asked + block_scan<kMoveThreads>(count, s_warp, &total);
+    asked += total;
+    const bool fits = count == 0 || (list_ok && upto <= taken);
+    block_scan<kMoveThreads>(fits ? count : 0, s_warp, &given);
+    returned += given;
+    if (last > first) {
+      int64_t at = taken - upto;
+      for (int b = first; b < last && fits; ++b)
+        if (t[b] >= 0 && t[b] < p.num_blocks) p.free_blocks[at++] = t[b];
+      const int32_t more = (fits ? 0 : kReqNoBlocks) | (count < last - first ? kReqBadBlock : 0);
+      if (more) p.status[r] |= more;
+    }
+  }
+  if (threadIdx.x == 0) *p.out_n_taken = (int32_t)(taken - returned);
+}
+
+// Moves the accepted nodes' rows to their places behind the context, and returns blocks (block 0).  A thread has one 16-byte column
+// (layer, K or V, head, piece) of a request and takes the accepted nodes in order, kMoveBatch loads before their stores: path[j] >= j,
+// so no row is written before it has been read.  Bound: HBM for many requests, the chain of look-ups for one.
+constexpr int kMoveBatch = 4;
+constexpr int kMoveCtasPerSm = 8;
+__global__ void __launch_bounds__(kMoveThreads) accept_move_kernel(const AcceptParams p) {
+  __shared__ int64_t s_warp[32];
+  grid_dependency_wait();
+  grid_launch_dependents();
+  if (blockIdx.x == 0) {
+    if (p.free_blocks) accept_trim(p, s_warp);
+    return;
+  }
+  const int per_layer = 2 * p.n_kv * p.row_chunks;
+  const int64_t columns = (int64_t)p.n_layers * per_layer, pieces = (columns + kMoveThreads - 1) / kMoveThreads;
+  for (int64_t item = blockIdx.x - 1; item < pieces * p.nreq; item += gridDim.x - 1) {
+    const int64_t r = item / pieces, column = (item - r * pieces) * kMoveThreads + threadIdx.x;
+    const int a = p.n_accepted[r];
+    if (a <= 1 || column >= columns) continue;
+    const int32_t q0 = p.q_start[r], start = p.out_lens[r] - a;
+    const int layer = (int)(column / per_layer), c = (int)(column - (int64_t)layer * per_layer);
+    const int head = (c / p.row_chunks) % p.n_kv;
+    uint8_t* base = (c >= p.n_kv * p.row_chunks ? p.v_cache : p.k_cache) + layer * p.layer_stride + head * p.head_stride + (c % p.row_chunks) * 16;
+    const int32_t* table = p.tables + r * p.max_blocks;
+    auto place = [&](int32_t pos) -> uint8_t* {
+      const int b = pos / p.block_size;
+      const int32_t blk = b < p.max_blocks ? table[b] : -1;
+      return blk >= 0 && blk < p.num_blocks ? base + blk * p.block_stride + (pos - b * p.block_size) * p.token_stride : nullptr;
+    };
+    for (int i0 = 1; i0 < a; i0 += kMoveBatch) {
+      uint4 x[kMoveBatch];
+      uint8_t* to[kMoveBatch];
+#pragma unroll
+      for (int j = 0; j < kMoveBatch; ++j) {
+        const int i = i0 + j;
+        const int from = i < a ? p.path[q0 + i] : i;
+        to[j] = nullptr;
+        if (from != i) {
+          const uint8_t* src = place(start + from);
+          to[j] = place(start + i);
+          if (src && to[j])
+            x[j] = *reinterpret_cast<const uint4*>(src);
+          else
+            to[j] = nullptr;
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < kMoveBatch; ++j)
+        if (to[j]) *reinterpret_cast<uint4*>(to[j]) = x[j];
+    }
+  }
+}
+
+}  // namespace ms

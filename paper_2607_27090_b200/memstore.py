@@ -32,7 +32,7 @@ CACHE_BF16, CACHE_FP8_E4M3 = 0, 1
 STORE_TMA_COPY_PATH = 1
 REQ_KERNEL_TIMEOUT = 32
 REQ_BAD_START = 64
-REQ_NO_BLOCKS, REQ_BAD_LENGTH = 128, 256
+REQ_NO_BLOCKS, REQ_BAD_LENGTH, REQ_BAD_TREE = 128, 256, 512
 
 
 class MemStoreError(RuntimeError):
@@ -83,7 +83,8 @@ EXPORTS = (
     "memstore_build_graph", "memstore_set_graph", "memstore_get_graph", "memstore_retrieve_ann", "memstore_graph_append",
     "memstore_test_hooks", "memstore_reserve", "memstore_compose_cache", "memstore_remove_fact", "memstore_set_graph_user",
     "memstore_get_graph_user", "memstore_retrieve_ann_users", "memstore_grow_blocks", "memstore_release_blocks",
-    "memstore_append", "memstore_attend", "memstore_attend_workspace",
+    "memstore_append", "memstore_attend", "memstore_attend_workspace", "memstore_plan_tree", "memstore_attend_tree", "memstore_accept",
+    "memstore_summarize_blocks", "memstore_select_blocks", "memstore_attend_blocks",
 )  # fmt: skip
 
 _lib = None
@@ -164,6 +165,18 @@ def load_library() -> C.CDLL:
     L.memstore_attend.argtypes = [vp, i32, hp, i32, i32, vp, vp, i32, vp, i32, C.POINTER(_PagedCache), C.c_float, i32, hp, vp, vp, vp, C.c_size_t, vp]
     L.memstore_attend_workspace.restype = C.c_size_t
     L.memstore_attend_workspace.argtypes = [vp]
+    L.memstore_plan_tree.restype = i32
+    L.memstore_plan_tree.argtypes = [vp, vp, i32, vp, i32, vp, i32, vp, vp, vp, vp]
+    L.memstore_attend_tree.restype = i32
+    L.memstore_attend_tree.argtypes = [vp, i32, hp, i32, i32, vp, vp, i32, vp, i32, vp, i32, C.POINTER(_PagedCache), C.c_float, i32, hp, vp, vp, vp, C.c_size_t, vp]
+    L.memstore_accept.restype = i32
+    L.memstore_accept.argtypes = [vp, vp, vp, vp, vp, i32, vp, vp, i32, vp, i32, C.POINTER(_PagedCache), vp, i32, vp, vp, vp, vp, vp, vp, vp, vp]
+    L.memstore_summarize_blocks.restype = i32
+    L.memstore_summarize_blocks.argtypes = [vp, i32, vp, i32, vp, i32, vp, i32, C.POINTER(_PagedCache), vp, vp]
+    L.memstore_select_blocks.restype = i32
+    L.memstore_select_blocks.argtypes = [vp, hp, i32, i32, vp, vp, i32, vp, vp, i32, C.POINTER(_PagedCache), i32, i32, i32, vp, vp, vp]
+    L.memstore_attend_blocks.restype = i32
+    L.memstore_attend_blocks.argtypes = [vp, i32, hp, i32, i32, vp, vp, i32, vp, i32, vp, i32, C.POINTER(_PagedCache), C.c_float, hp, vp, vp, vp, C.c_size_t, vp]
     L.memstore_stats.restype = i32
     L.memstore_stats.argtypes = [vp, C.POINTER(_Stats)]
     L.memstore_set_profile_events.restype = i32
@@ -202,6 +215,17 @@ class GrownBlocks(NamedTuple):
     positions: torch.Tensor
     slots: torch.Tensor
     n_taken: torch.Tensor
+    status: torch.Tensor
+
+
+class Accepted(NamedTuple):
+    """What ``MemStore.accept`` returns (see ``memstore_accept``)."""
+
+    path: torch.Tensor
+    n_accepted: torch.Tensor
+    next_tokens: torch.Tensor
+    seq_lens: torch.Tensor
+    n_taken: torch.Tensor | None
     status: torch.Tensor
 
 
@@ -690,6 +714,11 @@ class MemStore:
         goes on with them gives buffers of its own.  A kernel's time-out shows in ``out_status`` and in ``stats()["kernel_timeouts"]``.
         ``workspace``: a uint8 tensor of ``attend_workspace_bytes()``; by default the store keeps one for
         each of torch's streams that is current in a call; captures, calls with ``stream`` and external streams get one of their own."""
+        return self._attend(self._lib.memstore_attend, (), (max_q_len,), layer, q, cache, q_start, seq_lens, block_tables, scale, out, want_lse, out_lse,
+                            out_status, workspace, stream)  # fmt: skip
+
+    def _attend(self, call, sees, bound, layer, q, cache, q_start, seq_lens, block_tables, scale, out, want_lse, out_lse, out_status, workspace, stream):
+        """What the attention calls share; ``sees``: the arguments that say what a row sees, ``bound``: (max_q_len,) of calls that take it."""
         (T, n_q, _), nreq, i32, ptr = q.shape, seq_lens.shape[0], torch.int32, self._ptr
         if block_tables.dim() != 2 or block_tables.shape[0] != nreq:
             raise ValueError(f"block_tables must have shape ({nreq}, max_blocks), got {tuple(block_tables.shape)}")
@@ -709,13 +738,133 @@ class MemStore:
         raw = self._raw_stream(stream)
         if workspace is None:
             workspace = self._workspace(raw, stream)
-        self._check(self._lib.memstore_attend(
-            self._h, layer, hq, n_q, T, ptr(q_start, i32, "q_start", (nreq + 1,)), ptr(seq_lens, i32, "seq_lens", (nreq,)), nreq,
-            ptr(block_tables, i32, "block_tables"), block_tables.shape[1], self._paged(cache), scale, max_q_len,
+        self._check(call(
+            self._h, layer, hq, n_q, T, ptr(q_start, i32, "q_start", (nreq + 1,)), ptr(seq_lens, i32, "seq_lens", (nreq,)), nreq, *sees,
+            ptr(block_tables, i32, "block_tables"), block_tables.shape[1], self._paged(cache), scale, *bound,
             ho, None if out_lse is None else ptr(out_lse, torch.float32, "out_lse", (T, n_q)),
             None if out_status is None else ptr(out_status, i32, "out_status", (nreq,)), ptr(workspace, torch.uint8, "workspace"),
             workspace.numel(), raw))  # fmt: skip
         return out, out_lse, out_status
+
+    # -- drafted trees -------------------------------------------------------------------------------
+    def plan_tree(self, parents, q_start, positions, mask_words: int = 0, out_positions=None, out_mask=None, out_status=None, stream=None):
+        """Positions and visibility masks of drafted trees: ``parents`` [T] int32 (node numbers inside the request, -1: no parent), ``positions`` [T] as
+        ``grow_blocks`` lists them (``out_positions`` may be ``positions`` itself).  Returns (positions, mask [T, mask_words] int32,
+        ``out_status`` as given); ``mask_words`` is that of ``out_mask`` where it is given, else needed: words of 32 nodes of the largest tree.  Rows outside
+        every request (padding) are not written: in a new ``out_positions`` they are -1, in a new mask 0."""
+        T, nreq, i32, ptr = parents.shape[0], q_start.shape[0] - 1, torch.int32, self._ptr
+        if out_mask is None:
+            if mask_words < 1:
+                raise ValueError("plan_tree needs mask_words or out_mask")
+            (out_mask,) = self._empty(stream, ((T, mask_words), i32))
+            self._fill(out_mask, 0, stream)
+        elif out_mask.dim() != 2 or mask_words not in (0, out_mask.shape[1]):
+            raise ValueError(f"out_mask must have shape ({T}, mask_words), got {tuple(out_mask.shape)}")
+        mask_words = out_mask.shape[1]
+        if out_positions is None:
+            (out_positions,) = self._empty(stream, ((T,), i32))
+            self._fill(out_positions, -1, stream)
+        self._check(self._lib.memstore_plan_tree(
+            self._h, ptr(parents, i32, "parents", (T,)), T, ptr(q_start, i32, "q_start"), nreq, ptr(positions, i32, "positions", (T,)), mask_words,
+            ptr(out_positions, i32, "out_positions", (T,)), ptr(out_mask, i32, "out_mask", (T, mask_words)),
+            None if out_status is None else ptr(out_status, i32, "out_status", (nreq,)), self._raw_stream(stream)))  # fmt: skip
+        return out_positions, out_mask, out_status
+
+    def _fill(self, t: torch.Tensor, value: int, stream) -> None:
+        if stream is None:
+            t.fill_(value)
+        else:
+            with torch.cuda.stream(stream):
+                t.fill_(value)
+
+    def attend_tree(self, layer: int, q, tree_mask, cache: PagedCache, q_start, seq_lens, block_tables, scale: float = 0.0, max_q_len: int = 0, out=None,
+                    want_lse: bool = False, out_lse=None, out_status=None, workspace=None, stream=None):  # fmt: skip
+        """``attend`` with a mask among a request's new tokens: bit j of row i of ``tree_mask`` [T, mask_words] int32 lets new token i see new token j.
+        Arguments and results otherwise as for ``attend``, padding and workspaces included."""
+        if tree_mask.dim() != 2:
+            raise ValueError(f"tree_mask must have shape ({q.shape[0]}, mask_words), got {tuple(tree_mask.shape)}")
+        words = tree_mask.shape[1]
+        sees = (self._ptr(tree_mask, torch.int32, "tree_mask", (q.shape[0], words)), words)
+        return self._attend(self._lib.memstore_attend_tree, sees, (max_q_len,), layer, q, cache, q_start, seq_lens, block_tables, scale, out, want_lse, out_lse,
+                            out_status, workspace, stream)  # fmt: skip
+
+    def accept(self, parents, tokens, choices, positions, q_start, seq_lens, block_tables, cache: PagedCache, free_blocks=None, n_taken=None,
+               out: Accepted | None = None, stream=None) -> Accepted:  # fmt: skip
+        """Accept the part of each tree that the model confirms (``choices`` [T]: the token that it puts behind each node): moves the accepted rows of all
+        layers of the cache into place, shortens the lengths and returns blocks to ``free_blocks`` (in place).  ``out`` takes buffers, in which
+        ``seq_lens`` and ``n_taken`` may be the arguments themselves.  Rows of ``path`` outside every request (padding) are not written."""
+        T, nreq, i32, ptr = parents.shape[0], seq_lens.shape[0], torch.int32, self._ptr
+        if block_tables.dim() != 2 or block_tables.shape[0] != nreq:
+            raise ValueError(f"block_tables must have shape ({nreq}, max_blocks), got {tuple(block_tables.shape)}")
+        if (free_blocks is None) != (n_taken is None):
+            raise ValueError("free_blocks and n_taken go together")
+        if cache.k.shape[0] < self.n_layers:
+            raise ValueError(f"the cache has {cache.k.shape[0]} layers, the store {self.n_layers}")
+        if out is None:
+            (ints,) = self._empty(stream, ((T + 4 * nreq + 1,), i32))
+            path, a, said, lens, status, taken = ints.split_with_sizes((T, nreq, nreq, nreq, nreq, 1))
+            out = Accepted(path, a, said, lens, None if n_taken is None else taken, status)
+        self._check(self._lib.memstore_accept(
+            self._h, ptr(parents, i32, "parents", (T,)), ptr(tokens, i32, "tokens", (T,)), ptr(choices, i32, "choices", (T,)),
+            ptr(positions, i32, "positions", (T,)), T, ptr(q_start, i32, "q_start", (nreq + 1,)), ptr(seq_lens, i32, "seq_lens", (nreq,)), nreq,
+            ptr(block_tables, i32, "block_tables"), block_tables.shape[1], self._paged(cache),
+            None if free_blocks is None else ptr(free_blocks, i32, "free_blocks"), 0 if free_blocks is None else free_blocks.numel(),
+            None if n_taken is None else ptr(n_taken, i32, "n_taken", (1,)), ptr(out.path, i32, "out.path", (T,)),
+            ptr(out.n_accepted, i32, "out.n_accepted", (nreq,)), ptr(out.next_tokens, i32, "out.next_tokens", (nreq,)),
+            ptr(out.seq_lens, i32, "out.seq_lens", (nreq,)), None if n_taken is None else ptr(out.n_taken, i32, "out.n_taken", (1,)),
+            ptr(out.status, i32, "out.status", (nreq,)), self._raw_stream(stream)))  # fmt: skip
+        return out
+
+    # -- selected blocks -----------------------------------------------------------------------------
+    def allocate_summaries(self, cache: PagedCache) -> torch.Tensor:
+        """Summaries of the blocks of a cache, all zeros: [n_layers, num_blocks, n_kv_heads, 2, head_dim] bf16; the calls take one layer's."""
+        shape = (self.n_layers, cache.num_blocks, self.n_kv_heads, 2, self.head_dim)
+        return torch.zeros(shape, dtype=torch.bfloat16, device=self.device)
+
+    def _summaries(self, cache: PagedCache, summaries) -> int:
+        return self._ptr(summaries, torch.bfloat16, "summaries", (cache.num_blocks, self.n_kv_heads, 2, self.head_dim))
+
+    def summarize_blocks(self, layer: int, cache: PagedCache, summaries, seq_lens, block_tables, q_start=None, n_tokens: int = 1 << 30, stream=None) -> None:
+        """Form the summaries (of ``layer``: [num_blocks, n_kv_heads, 2, head_dim] bf16, in place) of the blocks that hold the new tokens of ``q_start``
+        (``n_tokens``: how many there are at most, which sizes the launch); without ``q_start`` of all blocks of the requests."""
+        nreq, i32, ptr = seq_lens.shape[0], torch.int32, self._ptr
+        if block_tables.dim() != 2 or block_tables.shape[0] != nreq:
+            raise ValueError(f"block_tables must have shape ({nreq}, max_blocks), got {tuple(block_tables.shape)}")
+        self._check(self._lib.memstore_summarize_blocks(
+            self._h, layer, None if q_start is None else ptr(q_start, i32, "q_start", (nreq + 1,)), n_tokens, ptr(seq_lens, i32, "seq_lens", (nreq,)), nreq,
+            ptr(block_tables, i32, "block_tables"), block_tables.shape[1], self._paged(cache), self._summaries(cache, summaries),
+            self._raw_stream(stream)))  # fmt: skip
+
+    def select_blocks(self, q, cache: PagedCache, summaries, q_start, seq_lens, block_tables, n_select: int, n_first: int = 1, n_last: int = 1, out_blocks=None,
+                      out_scores=None, stream=None):  # fmt: skip
+        """The ``n_select`` blocks that each new token reads, per K/V head: the first ``n_first``, the last ``n_last`` and the best others by
+        their summaries (one layer's).  Returns (blocks [T, n_kv_heads, n_select] int32, ``out_scores`` as given: [T, n_kv_heads, max_blocks] fp32).  Rows outside
+        every request (padding) are not written."""
+        (T, n_q, _), nreq, i32, ptr = q.shape, seq_lens.shape[0], torch.int32, self._ptr
+        if block_tables.dim() != 2 or block_tables.shape[0] != nreq:
+            raise ValueError(f"block_tables must have shape ({nreq}, max_blocks), got {tuple(block_tables.shape)}")
+        hq = self._heads(q, T, n_q, "q")
+        lists = (T, self.n_kv_heads, n_select)
+        if out_blocks is None:
+            (out_blocks,) = self._empty(stream, (lists if n_select > 0 else (0,), i32))
+        self._check(self._lib.memstore_select_blocks(
+            self._h, hq, n_q, T, ptr(q_start, i32, "q_start", (nreq + 1,)), ptr(seq_lens, i32, "seq_lens", (nreq,)), nreq,
+            self._summaries(cache, summaries), ptr(block_tables, i32, "block_tables"), block_tables.shape[1], self._paged(cache), n_select, n_first, n_last,
+            ptr(out_blocks, i32, "out_blocks", lists if n_select > 0 else None),
+            None if out_scores is None else ptr(out_scores, torch.float32, "out_scores", (T, self.n_kv_heads, block_tables.shape[1])),
+            self._raw_stream(stream)))  # fmt: skip
+        return out_blocks, out_scores
+
+    def attend_blocks(self, layer: int, q, blocks, cache: PagedCache, q_start, seq_lens, block_tables, scale: float = 0.0, out=None, want_lse: bool = False,
+                      out_lse=None, out_status=None, workspace=None, stream=None):  # fmt: skip
+        """``attend`` over the blocks that ``blocks`` [T, n_kv_heads, n_select] int32 lists for each new token and K/V head (-1: none).  Arguments and results
+        otherwise as for ``attend``, padding and workspaces included."""
+        if blocks.dim() != 3:
+            raise ValueError(f"blocks must have shape ({q.shape[0]}, {self.n_kv_heads}, n_select), got {tuple(blocks.shape)}")
+        k = blocks.shape[2]
+        sees = (self._ptr(blocks, torch.int32, "blocks", (q.shape[0], self.n_kv_heads, k)), k)
+        return self._attend(self._lib.memstore_attend_blocks, sees, (), layer, q, cache, q_start, seq_lens, block_tables, scale, out, want_lse, out_lse,
+                            out_status, workspace, stream)  # fmt: skip
 
     def stats(self) -> dict:
         st = _Stats()
