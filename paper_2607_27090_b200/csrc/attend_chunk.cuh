@@ -16,10 +16,12 @@
 // columns and are the A operand of the second product, whose accumulator stays in TMEM for the whole unit.
 //   warps 0-7, 8-15  queries (scaled to fp16 for an 8-bit cache), weights and epilogue of rows 0-127, 128-255: two threads share a row,
 //                    64 of the tile's keys each (16 warps: a single warp per scheduler cannot keep the exponentials' unit busy)
-//   warps 16-19      loads: K and V tiles of 128 keys through a ring of 5 buffers, gathered through the block table with cp.async
-//                    (8-bit: the codes go to a place of the loading thread's own, a tile ahead, and are converted to fp16, exactly, from there)
+//   warp 22          loads: K and V tiles of 128 keys through a ring of 5 buffers, gathered through the block table by tensor copies of a block
+//                    each (block sizes that divide 128, from 8 on, and multiples of 128)
+//   warps 16-19      work on tiles between their copy and the tensor cores: codes of an 8-bit cache become fp16, exactly; V tiles at the causal border
+//                    lose what is not finite.  For other block sizes they do the loads too, with cp.async
 //   warp 20          TMEM allocation, tcgen05.mma issue by one elected lane
-//   warp 21          walks the CTA's share of the line and describes its units to the other roles (warps 22, 23 complete the warpgroup)
+//   warp 21          walks the CTA's share of the line and describes its units to the other roles (warp 23 completes the warpgroup)
 // Work split: as in attend.cuh, the tiles of all units (causal: only as many as a unit's last row sees) form one line of which every
 // CTA takes an equal share, so 64 units on 148 SMs balance as well as 6400.  Starting and ending a unit costs as much as a few of its
 // tiles, so each unit takes kChunkUnitCost places more on the line.  Places for that, and the time of a call (32/8 heads of 128,
@@ -37,7 +39,7 @@ namespace ms {
 
 constexpr int kChunkRows = 256;
 constexpr int kChunkKeys = 128;
-constexpr int kChunkStages = 5;
+constexpr int kChunkStages = 5;       // tiles of the ring (see ChunkCfg::kStages)
 constexpr int kChunkThreads = 24 * 32;
 constexpr int kChunkRegsWeights = 88, kChunkRegsLoads = 72, kChunkRegsIssue = 56;
 static_assert(4 * kChunkRegsWeights + kChunkRegsLoads + kChunkRegsIssue <= 6 * 80, "six warpgroups share the 80 registers a thread of the launch");
@@ -47,12 +49,15 @@ constexpr uint32_t kChunkSpinLimit = 1u << 26;  // polls (a second or more)
 
 template <int D, bool FP8>
 struct ChunkCfg {
-  static constexpr int kStages = FP8 ? 4 : kChunkStages;             // an 8-bit cache gives one tile's place to codes on their way
+  // Tiles of the ring.  With an 8-bit cache and copies by threads (blocks that no tensor copy takes) the last tile's place is for codes on their way.
+  static constexpr int kStages = kChunkStages;
+  static constexpr int kStagesByThreads = FP8 ? kStages - 1 : kStages;
   static constexpr int kHalves = D / 64;                             // 128-byte column blocks of a 16-bit row
   static constexpr int kTileBytes = kChunkKeys * D * 2;              // K or V tile, 16 bits per element
   static constexpr int kQBytes = kChunkRows * D * 2;
-  static constexpr int kRawBytes = FP8 ? kTileBytes : 0;             // two tiles of codes
-  static constexpr int kRingBytes = kStages * kTileBytes + kRawBytes;
+  static constexpr int kRingBytes = kStages * kTileBytes;
+  static constexpr int kRawAt = FP8 ? kTileBytes / 2 : 0;            // codes land in the second half of the tile that they become
+  static constexpr int kCopyBytes = FP8 ? kTileBytes / 2 : kTileBytes;
   static constexpr int kSmemBytes = 1024 + kQBytes + kRingBytes + 2048;  // alignment, tiles, barriers and small arrays
   static_assert(kSmemBytes <= 232448, "shared memory of a CTA");
   static constexpr int kColO = 2 * kChunkKeys;                       // TMEM: S0, S1 (128 columns each), O0, O1 (D columns each)
@@ -64,6 +69,11 @@ struct ChunkCfg {
   static constexpr float kMaxSum = FP8 ? 61440.f : 16384.f;
   static constexpr float kLift = FP8 ? 4.f : 0.f;
 };
+
+// Where tiles may come by tensor copies: trees, and causal chunks over an 8-bit cache with head_dim 128 (2,048 tokens of 8,192 in it 334 us with
+// copies by threads, 267 with tensor copies; a bf16 cache 246 and 248, head_dim 64 226 and 228, 8-bit 234 and 235).
+template <int D, bool FP8, int SEE>
+constexpr bool kChunkTensorCopies = SEE == kSeeTree || (FP8 && D == 128);
 
 struct ChunkParams {
   AttendParams a;
@@ -77,6 +87,8 @@ struct ChunkParams {
   int32_t* timed_out; // of the store: set to 1 when one did, for whoever asks for no status
   uint32_t spin_limit;
   int mute_producer;
+  int tensor_copies;  // tiles come by tensor copies, a block (or 128 keys of it) each
+  int page_shift;     // log2 of the keys of such a copy
 };
 
 // The row tiles of a request one after another: token and query head of the group of the tile's first row.
@@ -267,6 +279,21 @@ __device__ __forceinline__ bool chunk_wait(uint64_t* bar, uint32_t parity, volat
   *abort_flag = 1;
   return false;
 }
+__device__ __forceinline__ void tma_load_4d(void* smem_dst, const CUtensorMap* map, int x, int y, int z, int w, uint64_t* bar) {
+  asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(smem_u32(smem_dst)),
+               "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(w), "r"(smem_u32(bar))
+               : "memory");
+}
+template <int N>
+__device__ __forceinline__ void mbar_arrive_n(uint64_t* bar) {
+  asm volatile("{ .reg .b64 st; mbarrier.arrive.shared::cta.b64 st, [%0], %1; }" ::"r"(smem_u32(bar)), "n"(N) : "memory");
+}
+// Disjunction over the four loading warps, which meet there.
+__device__ __forceinline__ bool loaders_any(bool v) {
+  uint32_t r;
+  asm volatile("{ .reg .pred p, q; setp.ne.u32 p, %1, 0; barrier.cta.red.or.pred q, 13, 128, p; selp.u32 %0, 1, 0, q; }" : "=r"(r) : "r"((uint32_t)v) : "memory");
+  return r != 0u;
+}
 __device__ __forceinline__ bool elect_one() {
   uint32_t p;
   asm volatile("{ .reg .pred q; elect.sync _|q, 0xffffffff; selp.u32 %0, 1, 0, q; }" : "=r"(p));
@@ -277,6 +304,14 @@ __device__ __forceinline__ void pair_sync(int id) { asm volatile("barrier.cta.sy
 __device__ __forceinline__ bool pair_any(int id, bool v) {
   uint32_t r;
   asm volatile("{ .reg .pred p, q; setp.ne.u32 p, %2, 0; barrier.cta.red.or.pred q, %1, 64, p; selp.u32 %0, 1, 0, q; }" : "=r"(r) : "r"(id), "r"((uint32_t)v) : "memory");
+  return r != 0u;
+}
+
+// The same for the four warps that have the same 32 rows' place in both halves.
+__device__ __forceinline__ void quad_sync(int id) { asm volatile("barrier.cta.sync %0, 128;" ::"r"(id) : "memory"); }
+__device__ __forceinline__ bool quad_any(int id, bool v) {
+  uint32_t r;
+  asm volatile("{ .reg .pred p, q; setp.ne.u32 p, %2, 0; barrier.cta.red.or.pred q, %1, 128, p; selp.u32 %0, 1, 0, q; }" : "=r"(r) : "r"(id), "r"((uint32_t)v) : "memory");
   return r != 0u;
 }
 
@@ -320,9 +355,14 @@ struct ChunkYes {
 struct ChunkNo {
   static constexpr bool value = false;
 };
+template <int N>
+struct ChunkInt {
+  static constexpr int value = N;
+};
 
 template <int D, bool FP8, int SEE>
-__global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const ChunkParams c) {
+__global__ void __launch_bounds__(kChunkThreads, 1)
+    attend_chunk_kernel(const __grid_constant__ ChunkParams c, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
   using C = ChunkCfg<D, FP8>;
   const AttendParams& p = c.a;
   extern __shared__ uint8_t smem_raw[];
@@ -338,24 +378,30 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
   uint64_t* o_full = p_full + 2;               // [2]
   uint64_t* u_full = o_full + 2;               // [kChunkUnits]
   uint64_t* u_empty = u_full + kChunkUnits;    // [kChunkUnits]
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(u_empty + kChunkUnits);
+  uint64_t* raw_full = u_empty + kChunkUnits;  // [kChunkStages]: a tile that the loading warps work on before it goes to the tensor cores
+  constexpr int kBars = 2 + 3 * kChunkStages + 6 + 2 * kChunkUnits;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + (kBars + 1) / 2 * 2);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   uint32_t* s_masks = tmem_slot + 4;           // [kChunkMaskRing][4]: keys of the tile that the table names
   // [kChunkMaskRing][4]: a loading warp's part of the V tile holds values that are not finite.  Looked for in causal tiles alone (0 for
   // the others); may be read once the next tile's scores, or the unit's last accumulator, are there.
-  uint32_t* s_bad = s_masks + 4 * kChunkMaskRing;
+  uint8_t* s_bad = reinterpret_cast<uint8_t*>(s_masks + 4 * kChunkMaskRing);
   float* s_pair = reinterpret_cast<float*>(s_bad + 4 * kChunkMaskRing);  // [256]: exchange between the two threads of a row
   uint8_t* s_qexp = reinterpret_cast<uint8_t*>(s_pair + kChunkRows);  // [256], 8-bit cache: exponent fields of the rows' inverse powers of two
   int64_t* s_warp = reinterpret_cast<int64_t*>(s_qexp + kChunkRows);  // [32]
   int64_t* s_found = s_warp + 32;                                      // [2]
   ChunkUnit* units = reinterpret_cast<ChunkUnit*>(s_warp);             // [kChunkUnits], once the first unit has been found
   static_assert(sizeof(ChunkUnit) * kChunkUnits <= 32 * sizeof(int64_t), "the units' ring takes the place of the scan's");
+  static_assert((kBars + 1) / 2 * 16 + 16 + 20 * kChunkMaskRing + 5 * kChunkRows + 34 * 8 <= 2048 && (20 * kChunkMaskRing) % 16 == 0, "small arrays");
+  const bool tensor_copies = kChunkTensorCopies<D, FP8, SEE> && c.tensor_copies;
+  const int n_stages = tensor_copies ? C::kStages : C::kStagesByThreads;
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
     for (int s = 0; s < C::kStages; ++s) {
       mbar_init(&kv_full[s], 4);
       mbar_init(&kv_empty[s], 1);
+      mbar_init(&raw_full[s], 1);
     }
     for (int h = 0; h < 2; ++h) {
       mbar_init(&q_full[h], 8);
@@ -365,7 +411,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
     }
     for (int i = 0; i < kChunkUnits; ++i) {
       mbar_init(&u_full[i], 1);
-      mbar_init(&u_empty[i], 21);  // every warp of the other roles
+      mbar_init(&u_empty[i], tensor_copies ? 22 : 21);  // every warp of the other roles
     }
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -409,8 +455,102 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
     if (lane == 0) mbar_arrive(&u_empty[n % kChunkUnits]);
   };
 
-  if (warp >= 16 && warp < 20) {
-    // ------------------------------------------------------------------ loads
+  if (warp >= 16 && warp < 20 && tensor_copies) {
+    // ------------------------------------------------------------------ tiles that need work before the tensor cores take them
+    // (8-bit cache: all of them, codes become fp16; else the causal V tiles, whose values that are not finite become zeros)
+    regs_down<kChunkRegsLoads>();
+    const int w = warp - 16, lt = tid - 16 * 32;
+    constexpr int kRowPieces = D * (FP8 ? 1 : 2) / 16;  // 16-byte pieces of a cache row; as many as a thread takes of a tile
+    // the four warps meet once per tile of an 8-bit cache, so they leave together
+    auto together = [&](bool fine) {
+      fine = __all_sync(0xffffffffu, fine);
+      return FP8 ? !loaders_any(!fine) : fine;
+    };
+    bool ok = true;
+    int stage = 0, mask_at = 0;
+    uint32_t raw_ph = 0;
+    for (int n = 0; ok; ++n) {
+      ok = together(unit_ready(n));
+      if (!ok) break;
+      const ChunkUnit u = units[n % kChunkUnits];
+      __syncwarp();
+      if (u.nt < 0) break;
+      unit_done(n);
+      for (int t = u.t0; ok && t < u.t0 + u.nt; ++t) {
+        const bool causal = t * kChunkKeys + kChunkKeys - 1 > u.lim_min;
+        for (int kv = 0; kv < 2; ++kv) {
+          if (FP8 || (kv && causal)) {
+            ok = __all_sync(0xffffffffu, chunk_wait(&raw_full[stage], (raw_ph >> stage) & 1u, abort_flag, limit));
+            raw_ph ^= 1u << stage;
+            uint8_t* tile = ring + stage * C::kTileBytes;
+            bool bad = false;
+            if constexpr (FP8) {
+              uint4 x[kRowPieces];
+              if (ok) {
+#pragma unroll
+                for (int i = 0; i < kRowPieces; ++i) x[i] = *reinterpret_cast<const uint4*>(tile + C::kRawAt + (i * 128 + lt) * 16);
+              }
+              ok = together(ok);  // (everybody's codes have been read: they lie where the numbers go)
+              if (!ok) break;
+#pragma unroll
+              for (int i = 0; i < kRowPieces; ++i) {
+                const int idx = i * 128 + lt, row = idx / kRowPieces, ch = idx % kRowPieces;
+                uint32_t y[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+                if (kv && causal) {  // NaN codes become zeros here; the epilogue adds them to the rows that see them
+#pragma unroll
+                  for (int e = 0; e < 4; ++e) {
+                    const uint32_t m = __vcmpeq4(y[e] & 0x7f7f7f7fu, 0x7f7f7f7fu);
+                    bad = bad || m;
+                    y[e] &= ~m;
+                  }
+                }
+                uint4 lo, hi;
+                e4m3x4_half2(y[0], lo.x, lo.y);
+                e4m3x4_half2(y[1], lo.z, lo.w);
+                e4m3x4_half2(y[2], hi.x, hi.y);
+                e4m3x4_half2(y[3], hi.z, hi.w);
+                uint8_t* d = tile + (ch >> 2) * 16384;
+                *reinterpret_cast<uint4*>(d + chunk_swz(row, 2 * (ch & 3))) = lo;
+                *reinterpret_cast<uint4*>(d + chunk_swz(row, 2 * (ch & 3) + 1)) = hi;
+              }
+            } else {
+              if (!ok) break;
+              // a value that is not finite would reach rows that must not see it as 0 * inf.  It becomes zero here, and the epilogue adds it
+              // to the rows that see it.  (Values behind a request's last key are among them.)
+#pragma unroll 4
+              for (int i = 0; i < kRowPieces; ++i) {
+                const int idx = i * 128 + lt, row = idx / kRowPieces, ch = idx % kRowPieces;
+                uint4* at16 = reinterpret_cast<uint4*>(tile + (ch >> 3) * 16384 + chunk_swz(row, ch & 7));
+                const uint4 z = *at16;
+                const uint32_t y[4] = {z.x, z.y, z.z, z.w};
+                uint32_t keep[4];
+                bool some = false;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                  keep[e] = ((y[e] & 0x7f80u) == 0x7f80u ? 0u : 0xffffu) | ((y[e] & 0x7f800000u) == 0x7f800000u ? 0u : 0xffff0000u);
+                  some = some || keep[e] != 0xffffffffu;
+                }
+                if (some) {
+                  *at16 = make_uint4(y[0] & keep[0], y[1] & keep[1], y[2] & keep[2], y[3] & keep[3]);
+                  bad = true;
+                }
+              }
+            }
+            if (kv && causal) {
+              bad = __any_sync(0xffffffffu, bad);
+              if (lane == 0) s_bad[mask_at * 4 + w] = bad;
+            }
+            fence_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&kv_full[stage]);
+          }
+          if (++stage == C::kStages) stage = 0;
+        }
+        if (++mask_at == kChunkMaskRing) mask_at = 0;
+      }
+    }
+  } else if (warp >= 16 && warp < 20) {
+    // ------------------------------------------------------------------ loads, copied by threads
     regs_down<kChunkRegsLoads>();
     const int w = warp - 16, lt = tid - 16 * 32;
     bool ok = !c.mute_producer;
@@ -421,12 +561,12 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
       fence_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(&kv_full[pub]);
-      if (++pub == C::kStages) pub = 0;
+      if (++pub == C::kStagesByThreads) pub = 0;
       --unpublished;
     };
     // 8-bit cache: this thread's 16-byte pieces of its warp's 32 rows, into a place that only it reads
     constexpr int kLoads = 32 * D / 512;
-    uint8_t* raw = ring + C::kStages * C::kTileBytes + lt * 16;
+    uint8_t* raw = ring + C::kStagesByThreads * C::kTileBytes + lt * 16;
     int raw_in = 0, raw_out = 0;
     auto raw_issue = [&](const uint8_t* base, int64_t at, uint32_t mask) {
 #pragma unroll
@@ -566,7 +706,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
             cp_async_wait<1>();
             publish();
           }
-          if (++stage == C::kStages) {
+          if (++stage == C::kStagesByThreads) {
             stage = 0;
             ph ^= 1u;
           }
@@ -633,6 +773,65 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
         }
         if (u.nt < 0) break;
       }
+    } else if (warp == 22 && tensor_copies) {
+      // ---------------------------------------------------------------- tensor copies: K, V, K, V ..., as far ahead as there are stages
+      // A lane copies a block (or 128 keys of one): rows of 128 bytes, swizzled as the tensor cores take them, or the codes of an 8-bit cache.  Keys
+      // whose block the table does not name are copied from outside the cache, which gives zeros.
+      bool ok = !c.mute_producer;
+      if (lane < 2) asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(lane ? &v_map : &k_map)) : "memory");
+      int stage = 0, mask_at = 0;
+      uint32_t ph = 1;
+      const int pages = kChunkKeys >> c.page_shift;
+      for (int n = 0; ok; ++n) {
+        ok = __all_sync(0xffffffffu, unit_ready(n));
+        if (!ok) break;
+        const ChunkUnit u = units[n % kChunkUnits];
+        __syncwarp();
+        if (u.nt < 0) break;
+        unit_done(n);
+        const int t_end = u.t0 + u.nt;
+        const int32_t* table = p.tables + (int64_t)u.req * p.max_blocks;
+        auto key_of = [&](int t) { return t * kChunkKeys + (lane << c.page_shift); };
+        auto entry_of = [&](int t) { return t < t_end && lane < pages && key_of(t) < u.key_end ? __ldg(table + attn_page(p, key_of(t))) : -1; };
+        int32_t nxt = entry_of(u.t0);
+        for (int t = u.t0; ok && t < t_end; ++t) {
+          const int32_t blk = nxt >= 0 && nxt < p.num_blocks ? nxt : -1;
+          nxt = entry_of(t + 1);
+          const uint32_t named = __ballot_sync(0xffffffffu, blk >= 0);
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            const int key = w * 32 + lane;
+            const uint32_t there = __ballot_sync(0xffffffffu, ((named >> (key >> c.page_shift)) & 1u) && t * kChunkKeys + key < u.key_end);
+            if (lane == w) s_masks[mask_at * 4 + w] = there;
+          }
+          __syncwarp();
+          const int in_page = attn_in_page(p, key_of(t));
+          const bool causal = t * kChunkKeys + kChunkKeys - 1 > u.lim_min;
+          for (int kv = 0; kv < 2; ++kv) {
+            ok = __all_sync(0xffffffffu, chunk_wait(&kv_empty[stage], ph, abort_flag, limit));
+            if (!ok) break;
+            const bool raw = FP8 || (kv && causal);
+            uint64_t* bar = raw ? &raw_full[stage] : &kv_full[stage];
+            if (lane == 0) {
+              mbar_arrive_expect_tx(bar, C::kCopyBytes);
+              if (!raw) mbar_arrive_n<3>(bar);  // (in the loading warps' place)
+            }
+            __syncwarp();
+            if (lane < pages) {
+              const CUtensorMap* map = kv ? &v_map : &k_map;
+              uint8_t* dst = ring + stage * C::kTileBytes + C::kRawAt + ((lane << c.page_shift) * (FP8 ? D : 128));
+#pragma unroll
+              for (int b = 0; b < (FP8 ? 1 : C::kHalves); ++b) tma_load_4d(dst + b * 16384, map, b * 64, in_page, u.kvh, blk, bar);
+            }
+            if (++stage == C::kStages) {
+              stage = 0;
+              ph ^= 1u;
+            }
+          }
+          if (++mask_at == kChunkMaskRing) mask_at = 0;
+        }
+      }
+      __syncwarp();
     } else if (warp == 20) {
       const bool lead = elect_one();
       constexpr uint32_t kTypes = FP8 ? 0u : (1u << 7) | (1u << 10);  // fp16 or bf16 operands
@@ -651,6 +850,57 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
         if (nt < 0) break;
         unit_done(n);
         if (nt == 0) continue;
+        if (SEE == kSeeTree && halves == 1) {
+          // the halves share the rows and take the tiles in turn: tile i goes to half i % 2
+          int v_stage[2] = {0, 0};
+          uint32_t v_ph[2] = {0, 0};
+          auto advance = [&] {
+            if (++stage == n_stages) {
+              stage = 0;
+              ph ^= 1u;
+            }
+          };
+          auto turn = [&](int i, auto half) {
+            constexpr int h = decltype(half)::value ? 1 : 0;
+            if (i >= 2) {  // O += P V of the half's tile before
+              ok = chunk_wait(&kv_full[v_stage[h]], v_ph[h], abort_flag, limit);
+              if (ok) ok = chunk_wait(&p_full[h], p_ph[h], abort_flag, limit);
+              if (!ok) return;
+              p_ph[h] ^= 1u;
+              tc_fence_after();
+              const uint32_t vd = desc_lo_mn(ring_u + v_stage[h] * C::kTileBytes);
+#pragma unroll
+              for (int k = 0; k < kChunkKeys / 16; ++k)
+                umma_ts(lead, tmem + C::kColO + h * D, tmem + h * kChunkKeys + k * 8, vd + k * 128, kIdescO, (i > 3 || k > 0) ? 1u : 0u);
+              umma_commit_if(lead, &kv_empty[v_stage[h]]);
+              if (i >= nt) umma_commit_if(lead, &o_full[h]);
+            }
+            if (i < nt) {  // S = Q K^T
+              ok = chunk_wait(&kv_full[stage], ph, abort_flag, limit);
+              if (ok && i < 2) {
+                ok = chunk_wait(&q_full[h], (q_ph >> h) & 1u, abort_flag, limit);
+                q_ph ^= 1u << h;
+              }
+              if (!ok) return;
+              tc_fence_after();
+              const uint32_t qd = desc_lo_k(q_u + h * (C::kQBytes / 2)), kd = desc_lo_k(ring_u + stage * C::kTileBytes);
+#pragma unroll
+              for (int k = 0; k < D / 16; ++k)
+                umma_ss(lead, tmem + h * kChunkKeys, qd + (k >> 2) * 1024 + 2 * (k & 3), kd + (k >> 2) * 1024 + 2 * (k & 3), kIdescS, k > 0 ? 1u : 0u);
+              umma_commit_if(lead, &s_full[h]);
+              umma_commit_if(lead, &kv_empty[stage]);
+              advance();
+              v_stage[h] = stage;
+              v_ph[h] = ph;
+              advance();
+            }
+          };
+          for (int i = 0; ok && i < nt + 2; i += 2) {
+            turn(i, ChunkNo{});
+            if (ok && i + 1 < nt + 2 && (i > 0 || nt > 1)) turn(i + 1, ChunkYes{});
+          }
+          continue;
+        }
         int v_stage = 0;
         uint32_t v_ph = 0;
         for (int j = 0; ok && j <= nt; ++j) {
@@ -690,13 +940,13 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
           if (!ok) break;
           if (j < nt) {
             umma_commit_if(lead, &kv_empty[k_stage]);
-            if (++stage == C::kStages) {
+            if (++stage == n_stages) {
               stage = 0;
               ph ^= 1u;
             }
             v_stage = stage;
             v_ph = ph;
-            if (++stage == C::kStages) {
+            if (++stage == n_stages) {
               stage = 0;
               ph ^= 1u;
             }
@@ -711,6 +961,9 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
     const int h = warp >> 3, part = (warp >> 2) & 1;     // half of the rows; half of a tile's keys and of the accumulator's columns
     const int row = h * 128 + (warp & 3) * 32 + lane;    // of the unit
     const int pair = 1 + h * 4 + (warp & 3);             // barrier of the two warps that share these rows
+    const int quad = 9 + (warp & 3);                     // and of those with the same place in the other half
+    // Whether any of the warps that leave a unit together says so: those that share rows, or (tree) share barriers across the halves.
+    auto leave_any = [&](bool v) { return SEE == kSeeTree ? quad_any(quad, v) : pair_any(pair, v); };
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t ts = tmem + lanes + h * kChunkKeys, to = tmem + lanes + C::kColO + h * D + part * (D / 2);
     // both threads of a row get what `join` makes of their values
@@ -726,40 +979,38 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
       return v;
     };
     bool ok = true;
-    uint32_t s_ph = 0, o_ph = 0;
+    uint32_t s_ph = 0, o_ph = 0, o_ph_other = 0;  // (the other half's accumulator: units that the halves share)
     int mask_at = 0;
+    // Tree: a unit of at most 128 rows belongs to both halves, which take its tiles in turn, since a lone half leaves the tensor cores idle while
+    // its weights are formed.  40 requests of 4,850 tokens, 60 rows for each of 8 K/V heads of 128: 204 us with a lone half, 194 with both, 179
+    // with both and tensor copies; 8-bit cache 253, 260 and 212.
+    auto shared = [](int rows) { return SEE == kSeeTree && rows <= 128; };
+    // first tile of this half
+    auto tile0 = [&](int rows) { return shared(rows) ? h : 0; };
     // queries of this warp's 16 rows of a unit, 16 bytes a lane; the products of the unit before have read theirs
-    auto load_queries = [&](const ChunkUnit& g) {
-      constexpr int kLanes = D / 8, kPerWarp = 32 / kLanes, kLoads = 16 / kPerWarp;  // lanes of a row, rows of a load
-      const int ql = lane % kLanes, first = h * 128 + (warp & 3) * 32 + part * 16 + lane / kLanes;
-      const int rows = g.rows, sub0 = g.sub0, head0 = g.kvh * p.group;
-      const __nv_bfloat16* q0 = p.q + g.tok0 * p.q_ts + ql * 8;
-      auto place = [&](int r) { return q_smem + h * (C::kQBytes / 2) + (ql >> 3) * 16384 + chunk_swz(r & 127, ql & 7); };
-      auto source = [&](int r) {
-        const int dt = group_div(p, sub0 + r);
-        return q0 + dt * p.q_ts + (int64_t)(head0 + sub0 + r - dt * p.group) * p.q_hs;
-      };
-      if constexpr (!FP8) {
+    constexpr int kLanes = D / 8, kPerWarp = 32 / kLanes, kLoads = 16 / kPerWarp;  // lanes of a row, rows of a load
+    auto query_place = [&](int r) { return q_smem + h * (C::kQBytes / 2) + ((lane % kLanes) >> 3) * 16384 + chunk_swz(r & 127, (lane % kLanes) & 7); };
+    auto first_query = [&](int rows) { return (shared(rows) ? 0 : h * 128) + (warp & 3) * 32 + part * 16 + lane / kLanes; };
+    auto request_queries = [&](const ChunkUnit& g) {
+      const int rows = g.rows, sub0 = g.sub0, head0 = g.kvh * p.group, first = first_query(rows);
+      const __nv_bfloat16* q0 = p.q + g.tok0 * p.q_ts + (lane % kLanes) * 8;
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-          const int r = first + i * kPerWarp;
-          cp_async16(smem_u32(place(r)), r < rows ? source(r) : p.q, r < rows);
-        }
-        cp_async_commit();
-        cp_async_wait<0>();
-      } else {
-        uint4 x[kLoads];
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-          const int r = first + i * kPerWarp;
-          x[i] = make_uint4(0u, 0u, 0u, 0u);
-          if (r < rows) x[i] = *reinterpret_cast<const uint4*>(source(r));
-        }
-#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        const int r = first + i * kPerWarp, dt = group_div(p, sub0 + r);
+        cp_async16(smem_u32(query_place(r)), r < rows ? q0 + dt * p.q_ts + (int64_t)(head0 + sub0 + r - dt * p.group) * p.q_hs : p.q, r < rows);
+      }
+      cp_async_commit();
+    };
+    auto give_queries = [&](int rows) {
+      cp_async_wait<0>();
+      if constexpr (FP8) {
+        const int first = first_query(rows), ql = lane % kLanes;
+#pragma unroll 1
         for (int i = 0; i < kLoads; ++i) {
           // to fp16 by a power of two per row (see attend.cuh)
           const int r = first + i * kPerWarp;
-          uint32_t y[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+          const uint4 x = *reinterpret_cast<const uint4*>(query_place(r));
+          uint32_t y[4] = {x.x, x.y, x.z, x.w};
           float top = 0.f;
 #pragma unroll
           for (int e = 0; e < 4; ++e) top = fmaxf(top, fmaxf(fabsf(bf16lo(y[e])), fabsf(bf16hi(y[e]))));
@@ -767,10 +1018,10 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
           for (int o = kLanes / 2; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
           const int ex = min(max(268 - (int)(__float_as_uint(top) >> 23), 13), 227);
           const float f = __uint_as_float((uint32_t)ex << 23);
-          if (ql == 0) s_qexp[r] = (uint8_t)(254 - ex);
+          if (ql == 0) s_qexp[h * 128 + (r & 127)] = (uint8_t)(254 - ex);
 #pragma unroll
           for (int e = 0; e < 4; ++e) y[e] = pack_half(bf16lo(y[e]) * f, bf16hi(y[e]) * f);
-          *reinterpret_cast<uint4*>(place(r)) = make_uint4(y[0], y[1], y[2], y[3]);
+          *reinterpret_cast<uint4*>(query_place(r)) = make_uint4(y[0], y[1], y[2], y[3]);
         }
       }
       fence_async_smem();
@@ -778,26 +1029,31 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
       if (lane == 0) mbar_arrive(&q_full[h]);
     };
     // (the two warps of a pair always learn the same of a wait: neither is left at a barrier)
-    bool ready = false, loaded = false;  // the unit has been waited for already, and its queries loaded
+    bool ready = false, loaded = false;  // the unit has been waited for already, and its queries given
     for (int n = 0; ok; ++n) {
-      if (!ready) ok = !pair_any(pair, !unit_ready(n));
+      if (!ready) ok = !leave_any(!unit_ready(n));
       if (!ok) break;
       ready = false;
       const ChunkUnit& un = units[n % kChunkUnits];
       const int nt = un.nt;
       if (nt < 0) break;
       const int rows = un.rows;
-      if (h == 1 && rows <= 128) {
+      if (SEE != kSeeTree && h == 1 && rows <= 128) {
         mask_at = (mask_at + nt) % kChunkMaskRing;
         __syncwarp();
         unit_done(n);
         continue;
       }
-      if (!loaded && nt > 0) load_queries(un);
+      const int j0 = tile0(rows), j_step = shared(rows) ? 2 : 1, mask_end = (mask_at + nt) % kChunkMaskRing;
+      const int urow = shared(rows) ? row & 127 : row;  // of the unit
+      if (!loaded && nt > j0) {
+        request_queries(un);
+        give_queries(rows);
+      }
       loaded = false;
-      const int lim_min = un.lim_min, lim = SEE == kSeeTree ? 0 : lim_min + group_div(p, un.sub0 + min(row, rows - 1)), t0 = un.t0;
+      const int lim_min = un.lim_min, lim = SEE == kSeeTree ? 0 : lim_min + group_div(p, un.sub0 + min(urow, rows - 1)), t0 = un.t0;
       const uint32_t* tree = nullptr;  // the row's bits
-      if constexpr (SEE == kSeeTree) tree = p.tree + (int64_t)(un.tok0 + group_div(p, un.sub0 + min(row, rows - 1))) * p.tree_words;
+      if constexpr (SEE == kSeeTree) tree = p.tree + (int64_t)(un.tok0 + group_div(p, un.sub0 + min(urow, rows - 1))) * p.tree_words;
       // which of the 32 keys from k on the row sees
       auto row_sees = [&](uint32_t there, int k) {
         if constexpr (SEE == kSeeTree) return tree_see(there, k, lim_min + 1, tree, p.tree_words);
@@ -808,20 +1064,21 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
       int v_at = 0;
       bool v_causal = false;  // the tile before was a causal one
       auto look_at_v = [&] {
-        const uint4 b = *reinterpret_cast<const uint4*>(s_bad + v_at * 4);
-        any_bad = any_bad || (b.x | b.y | b.z | b.w) != 0u;
+        any_bad = any_bad || *reinterpret_cast<const uint32_t*>(s_bad + v_at * 4) != 0u;
       };
-      for (int j = 0; j < nt; ++j) {
+      if (SEE == kSeeTree) mask_at = (mask_at + j0) % kChunkMaskRing;
+      for (int j = j0; j < nt; j += j_step) {
         ok = chunk_wait(&s_full[h], s_ph, abort_flag, limit);
         s_ph ^= 1u;
         tc_fence_after();
-        if (FP8 && j == 0) sc = attn_scale(p.scale_log2, s_qexp[row]);
+        if (FP8 && j == j0) sc = attn_scale(p.scale_log2, s_qexp[row]);
         const int k0 = (t0 + j) * kChunkKeys + part * 64;
         const uint2 there = *reinterpret_cast<const uint2*>(s_masks + mask_at * 4 + part * 2);
         if (v_causal) look_at_v();  // (of the tile before: its product with V was issued before these scores)
         v_at = mask_at;
         v_causal = (t0 + j) * kChunkKeys + kChunkKeys - 1 > lim_min;
-        if (++mask_at == kChunkMaskRing) mask_at = 0;
+        if (SEE == kSeeTree) mask_at = (mask_at + j_step) % kChunkMaskRing;
+        else if (++mask_at == kChunkMaskRing) mask_at = 0;
         const bool masked = k0 + 63 > lim_min || (there.x & there.y) != 0xffffffffu;
         uint32_t pk[32];
         float sum = 0.f;
@@ -859,7 +1116,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
         };
         // A new maximum is taken first in a segment's first tile, and later when the sum asks for one.  (The vote is also the point
         // from which both warps have read their scores, over which the weights are stored.)
-        bool renew = j == 0, again = renew, stop = false;  // stop: a wait ran out, and both warps leave together
+        bool renew = j == j0, again = renew, stop = false;  // stop: a wait ran out, and both warps leave together
         if (again) stop = pair_any(pair, !ok);
 #pragma unroll 1
         while (!stop) {
@@ -880,10 +1137,10 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
             }
             // (a row's maximum changes by its own scores alone, so that a row does not depend on its neighbours)
             mx = pair_join(mx, [](float a, float b) { return fmaxf(a, b); });
-            const bool own = j == 0 || pair_join(renew ? 1.f : 0.f, [](float a, float b) { return fmaxf(a, b); }) != 0.f;
+            const bool own = j == j0 || pair_join(renew ? 1.f : 0.f, [](float a, float b) { return fmaxf(a, b); }) != 0.f;
             const float n = own ? fmaxf(m, fmaf(mx, sc, -C::kLift)) : m;
             const float f = n == -INFINITY || m == n ? 1.f : ex2(m - n);
-            if (j > 0) {
+            if (j > j0) {
               // the accumulator holds the tiles before this one (the commit that signalled these scores follows their product)
 #pragma unroll 1
               for (int b = 0; b < D / 2; b += 16) {
@@ -920,17 +1177,34 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
         __syncwarp();
         if (lane == 0) mbar_arrive(&p_full[h]);
       }
-      // all scores of this half have been taken, so its queries' place is free: the next unit's come while the last product runs
-      if (ok) {
-        ok = !pair_any(pair, !unit_ready(n + 1));
+      // all scores of this half have been taken, so its queries' place is free: the next unit's come while the last product and the epilogue run
+      // (tree: all four warps come here whatever became of their tiles, and leave together)
+      if (SEE == kSeeTree) mask_at = mask_end;
+      if (SEE == kSeeTree || ok) {
+        ok = !leave_any(!ok || !unit_ready(n + 1));
         const ChunkUnit& next = units[(n + 1) % kChunkUnits];
         ready = ok;
-        if (ok && next.nt > 0 && (h == 0 || next.rows > 128)) {
-          load_queries(next);
+        if (ok && (SEE == kSeeTree ? next.nt > tile0(next.rows) : next.nt > 0 && (h == 0 || next.rows > 128))) {
+          request_queries(next);
+          if (SEE != kSeeTree) give_queries(next.rows);  // (trees, 40 requests as above: 178 us with the queries given here, 176 after the epilogue)
           loaded = true;
         }
       }
-      if (ok && nt > 0) {
+      if (SEE == kSeeTree) {
+        // this half's accumulator, and of a shared unit the other half's
+        if (ok && nt > j0) {
+          ok = chunk_wait(&o_full[h], o_ph, abort_flag, limit);
+          o_ph ^= 1u;
+        }
+        const bool other = nt > (shared(rows) ? 1 - h : 0);
+        if (ok && other) {
+          if (shared(rows)) ok = chunk_wait(&o_full[h ^ 1], o_ph_other, abort_flag, limit);
+          o_ph_other ^= 1u;
+        }
+        tc_fence_after();
+        if (ok && v_causal) look_at_v();
+        if (nt > 0) ok = !leave_any(!ok);
+      } else if (ok && nt > 0) {
         ok = chunk_wait(&o_full[h], o_ph, abort_flag, limit);
         o_ph ^= 1u;
         tc_fence_after();
@@ -940,29 +1214,36 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
       if (!ok) break;
       // ---- epilogue: this thread's half of its row
       if (nt > 0) l = pair_join(l, [](float a, float b) { return a + b; });
+      float f_own = 1.f, f_other = 0.f;  // tree: factors of the halves' accumulators in a shared unit
+      if (SEE == kSeeTree && shared(rows)) {
+        any_bad = quad_any(quad, any_bad);
+        if (part == 0) s_pair[row] = m;
+        quad_sync(quad);
+        const float m_other = s_pair[row ^ 128];
+        quad_sync(quad);
+        if (part == 0) s_pair[row] = l;
+        quad_sync(quad);
+        const float l_other = s_pair[row ^ 128], top = fmaxf(m, m_other);
+        f_own = m == -INFINITY ? 1.f : ex2(m - top);  // (sums without a maximum: zeros, or NaN that has to stay)
+        f_other = m_other == -INFINITY ? 1.f : ex2(m_other - top);
+        l = fmaf(l_other, f_other, l * f_own);
+        m = top;
+      }
       const bool whole = un.whole != 0;
-      const bool mine = row < rows;
-      const int sr = un.sub0 + min(row, rows - 1), dt = group_div(p, sr), tok = un.tok0 + dt, head = un.kvh * p.group + sr - dt * p.group;
+      const bool mine = urow < rows;
+      const int sr = un.sub0 + min(urow, rows - 1), dt = group_div(p, sr), tok = un.tok0 + dt, head = un.kvh * p.group + sr - dt * p.group;
       const float inv = l == 0.f ? 0.f : p.v_scale / l;
       const int64_t slot = (int64_t)blockIdx.x * 2 + (t0 == 0 ? 1 : 0);
-      if (mine && part == 0) {
+      if (mine && part == 0 && (!shared(rows) || h == 0)) {
         if (whole) {
           if (p.lse) p.lse[(int64_t)tok * p.n_q + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
         } else {
-          c.part_ml[slot * kChunkRows + row] = make_float2(m, l);
+          c.part_ml[slot * kChunkRows + urow] = make_float2(m, l);
         }
       }
-#pragma unroll 1
-      for (int b = 0; b < D / 2; b += 32) {
-        const int col = part * (D / 2) + b;
-        float o[32];
-        if (nt > 0) {
-          tmem_ld32(to + b, o);
-          tmem_ld_wait();
-        } else {
-#pragma unroll
-          for (int e = 0; e < 32; ++e) o[e] = 0.f;
-        }
+      // WIDTH columns from `col` on of this thread's row
+      auto finish = [&](auto* o, int col, auto width) {
+        constexpr int kWidth = decltype(width)::value;
         if (any_bad) {
           // values that are not finite, at the keys of this segment's causal tiles that the row sees: their weight is positive, so
           // they decide the sum
@@ -975,7 +1256,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
             if (blk < 0 || blk >= p.num_blocks) continue;
             const uint8_t* v = p.v_cache + blk * p.block_stride + (key % p.block_size) * p.token_stride + un.kvh * p.head_stride;
 #pragma unroll
-            for (int e = 0; e < 32; ++e) {
+            for (int e = 0; e < kWidth; ++e) {
               if (FP8) {
                 if ((v[col + e] & 0x7f) == 0x7f) o[e] = NAN;
               } else {
@@ -989,16 +1270,56 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
           if (whole) {
             __nv_bfloat16* dst = p.out + tok * p.o_ts + head * p.o_hs + col;
 #pragma unroll
-            for (int e = 0; e < 32; e += 8)
+            for (int e = 0; e < kWidth; e += 8)
               *reinterpret_cast<uint4*>(dst + e) = make_uint4(pack_bf16(o[e] * inv, o[e + 1] * inv), pack_bf16(o[e + 2] * inv, o[e + 3] * inv),
                                                               pack_bf16(o[e + 4] * inv, o[e + 5] * inv), pack_bf16(o[e + 6] * inv, o[e + 7] * inv));
           } else {
 #pragma unroll
-            for (int e = 0; e < 32; e += 4)
-              *reinterpret_cast<float4*>(c.part_o + ((slot * (D / 4) + (col + e) / 4) * kChunkRows + row) * 4) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+            for (int e = 0; e < kWidth; e += 4)
+              *reinterpret_cast<float4*>(c.part_o + ((slot * (D / 4) + (col + e) / 4) * kChunkRows + urow) * 4) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
           }
         }
+      };
+      if (SEE == kSeeTree && shared(rows)) {
+        // a quarter of the row: both halves' accumulators, each with its own factor
+        const uint32_t own = tmem + lanes + C::kColO + h * D, theirs = tmem + lanes + C::kColO + (h ^ 1) * D;
+#pragma unroll 1
+        for (int b = 0; b < D / 4; b += 16) {
+          const int col = part * (D / 2) + h * (D / 4) + b;
+          float o[16], x[16];
+#pragma unroll
+          for (int e = 0; e < 16; ++e) o[e] = 0.f;
+          if (nt > h) {
+            tmem_ld16(own + col, x);
+            tmem_ld_wait();
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[e] = x[e] * f_own;
+          }
+          if (nt > (h ^ 1)) {
+            tmem_ld16(theirs + col, x);
+            tmem_ld_wait();
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[e] = fmaf(x[e], f_other, o[e]);
+          }
+          finish(o, col, ChunkInt<16>{});
+        }
+        tc_fence_before();
+        quad_sync(quad);  // (a half's next product into its accumulator follows its own warps' arrivals alone)
+      } else {
+#pragma unroll 1
+        for (int b = 0; b < D / 2; b += 32) {
+          float o[32];
+          if (nt > 0) {
+            tmem_ld32(to + b, o);
+            tmem_ld_wait();
+          } else {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) o[e] = 0.f;
+          }
+          finish(o, part * (D / 2) + b, ChunkInt<32>{});
+        }
       }
+      if (SEE == kSeeTree && loaded) give_queries(units[(n + 1) % kChunkUnits].rows);
       __syncwarp();
       unit_done(n);
       tc_fence_before();  // (the accumulator is read; the next unit's first product follows this warp's next arrival)
@@ -1018,6 +1339,21 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attend_chunk_kernel(const Ch
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(C::kTmemCols) : "memory");
   }
+}
+
+// ---- host side: the cache of a layer for tensor copies of `box_keys` keys of one block and head; x: elements of a row (64 at a time, swizzled; an
+// 8-bit cache: the whole row), then key of the block, head, block.
+inline bool make_tmap_cache(CUtensorMap* out, const void* base, bool fp8, int head_dim, int block_size, int box_keys, int n_heads, int64_t num_blocks,
+                            int64_t token_bytes, int64_t head_bytes, int64_t block_bytes) {
+  const tmap_encode_fn encode = tmap_encoder();
+  if (!encode) return false;
+  const cuuint64_t dims[4] = {(cuuint64_t)head_dim, (cuuint64_t)block_size, (cuuint64_t)n_heads, (cuuint64_t)num_blocks};
+  const cuuint64_t strides[3] = {(cuuint64_t)token_bytes, (cuuint64_t)head_bytes, (cuuint64_t)block_bytes};
+  const cuuint32_t box[4] = {(cuuint32_t)(fp8 ? head_dim : 64), (cuuint32_t)box_keys, 1, 1};
+  const cuuint32_t steps[4] = {1, 1, 1, 1};
+  return encode(out, fp8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, steps,
+                CU_TENSOR_MAP_INTERLEAVE_NONE, fp8 ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 // Joins 16 rows of the chunk unit that the border in front of CTA b's share cuts, if it is the unit's first border.

@@ -43,6 +43,8 @@
 #pragma once
 #include <cuda.h>
 
+#include <atomic>
+
 #include "inject_tma.cuh"  // mbarrier helpers
 
 namespace ms {
@@ -686,19 +688,24 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
 
 // ---- host side: TMA tensor map of a row-major fp16 matrix [n_rows][row_elems], box = 64 elements x box_rows rows,
 // 128-byte swizzle, zero fill outside the matrix.  The encoder is a driver entry point looked up through the runtime.
-inline bool make_tmap_rows_f16(CUtensorMap* out, const void* base, uint64_t n_rows, uint64_t row_elems, uint32_t box_rows) {
-  typedef CUresult (*encode_fn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
-                                const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-  static encode_fn encode = nullptr;
-  if (!encode) {
+typedef CUresult (*tmap_encode_fn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                   const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                   CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+inline tmap_encode_fn tmap_encoder() {
+  static std::atomic<tmap_encode_fn> encode{nullptr};
+  if (!encode.load()) {
     void* fn = nullptr;
     cudaDriverEntryPointQueryResult qres;
     if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &qres) != cudaSuccess || !fn ||
         qres != cudaDriverEntryPointSuccess)
-      return false;
-    encode = reinterpret_cast<encode_fn>(fn);
+      return nullptr;
+    encode.store(reinterpret_cast<tmap_encode_fn>(fn));
   }
+  return encode.load();
+}
+inline bool make_tmap_rows_f16(CUtensorMap* out, const void* base, uint64_t n_rows, uint64_t row_elems, uint32_t box_rows) {
+  const tmap_encode_fn encode = tmap_encoder();
+  if (!encode) return false;
   const cuuint64_t dims[2] = {row_elems, n_rows};
   const cuuint64_t strides[1] = {row_elems * 2};  // bytes between rows
   const cuuint32_t box[2] = {(cuuint32_t)kGemmKChunk, box_rows};

@@ -204,6 +204,9 @@ ms_status memstore_append(memstore_t* s, int32_t layer, const ms_heads* q, int32
 // 22.8 us, 64 of 2,000 321 against 165.
 static int chunk_min_rows(int64_t units, int sm_count) { return units <= sm_count / 2 ? 2 * kAttnRows : kAttnRows; }
 
+// Block sizes whose tiles of 128 keys are whole copies of (parts of) blocks that begin on the 1 KiB of a swizzled group of 8 rows.
+static bool chunk_tensor_copies(int block_size) { return (block_size >= 8 && kChunkKeys % block_size == 0) || block_size % kChunkKeys == 0; }
+
 // The workspace: unfinished rows of the rows kernel (kAttnMaxCtasPerSm CTAs per SM at most) and their statistics, then those of the chunk kernel
 // (one CTA per SM), its error words and the gate between the two.  It depends on the GPU and head_dim alone.
 struct AttendLayout {
@@ -271,7 +274,16 @@ static ms_status attend_launch(memstore* s, ChunkParams& c, int64_t max_rows, cu
   if constexpr (kChunks) {
     if (chunks) {
       chunk_ctas = s->sm_count;
-      MS_CUDA(s, launch_dependent(attend_chunk_kernel<D, FP8, SEE>, dim3((unsigned)chunk_ctas), dim3(kChunkThreads), (ChunkCfg<D, FP8>::kSmemBytes), st, c));
+      CUtensorMap k_map{}, v_map{};
+      c.tensor_copies = 0;
+      if (kChunkTensorCopies<D, FP8, SEE> && chunk_tensor_copies(p.block_size)) {
+        const int keys = std::min(p.block_size, kChunkKeys);
+        c.page_shift = __builtin_ctz((unsigned)keys);
+        // (where a description is refused, as for a stride that a tensor copy does not take, threads copy)
+        c.tensor_copies = make_tmap_cache(&k_map, p.k_cache, FP8, D, p.block_size, keys, p.n_kv, p.num_blocks, p.token_stride, p.head_stride, p.block_stride) &&
+                          make_tmap_cache(&v_map, p.v_cache, FP8, D, p.block_size, keys, p.n_kv, p.num_blocks, p.token_stride, p.head_stride, p.block_stride);
+      }
+      MS_CUDA(s, launch_dependent(attend_chunk_kernel<D, FP8, SEE>, dim3((unsigned)chunk_ctas), dim3(kChunkThreads), (ChunkCfg<D, FP8>::kSmemBytes), st, c, k_map, v_map));
       s->kernels_launched++;
       s->attn_chunks = true;
     }

@@ -593,6 +593,39 @@ def test_a_step_with_drafts_leaves_the_cache_as_steps_without_them_would(graph):
     ms.close()
 
 
+@pytest.mark.parametrize("bs", [8, 16, 32, 64, 128, 256, 384, 4, 24])
+@pytest.mark.parametrize("fp8,d", [(False, 64), (True, 64), (False, 128), (True, 128)])
+def test_tree_attention_with_every_way_to_fetch_a_tile(bs, fp8, d):
+    """Block sizes that tensor copies take and others, strides with gaps between blocks, heads and tokens, tables with holes, units that the halves share (few
+    rows) and others, a cache whose unused places hold NaN."""
+    rng = random.Random(bs + d + fp8)
+    hk, hq, q, lens = 2, 10, [9, 40, 25, 60, 1], [700, 1300, 90, 2500, 333]
+    q_start = [0] + [int(x) for x in np.cumsum(q)]
+    tables, nb = paged(rng, lens, bs)
+    tables[1, 1], tables[3, 0] = nb + 3, -7
+    dt = torch.uint8 if fp8 else torch.bfloat16
+    gen = torch.Generator(device=DEV).manual_seed(bs)
+    planes = []
+    for scale in (0.02, 0.03):
+        wide = torch.full((1, nb, bs, hk + 1, d + 16), 0x7F if fp8 else math.nan, device=DEV, dtype=dt)
+        x = torch.randn((1, nb, bs, hk, d), generator=gen, device=DEV)
+        wide[:, :, :, :hk, :d] = (x / scale).clamp(-448, 448).to(ref.F8).view(torch.uint8) if fp8 else x.to(torch.bfloat16)
+        planes.append(wide[:, :, :, :hk, :d])
+    row = (hk + 1) * (d + 16)
+    cache = PagedCache(planes[0], planes[1], nb * bs * row, bs * row, row, d + 16, nb, bs, k_scale=0.02, v_scale=0.03)
+    for r, n in enumerate(lens):  # behind the last tokens
+        blk = int(tables[r, n // bs])
+        if n % bs and 0 <= blk < nb:
+            for t in planes:
+                t[0, blk, n % bs :] = 0x7F if fp8 else math.nan
+    ms = store(hk, d)
+    x = torch.randn((q_start[-1], hq, d), generator=gen, device=DEV).to(torch.bfloat16)
+    status = [8 if (r == 1 and lens[1] > bs) or r == 3 else 0 for r in range(5)]
+    check_tree(ms, cache, x, q_start, lens, tables, masks(rng, q, 2, "tree"), want_status=status)
+    check_attend(ms, cache, x, q_start, lens, tables, want_status=status)
+    ms.close()
+
+
 def test_drafts_on_another_stream_and_with_two_graphs_side_by_side():
     rng = random.Random(12)
     sizes, lens = [40, 7, 64], [900, 300, 1500]
