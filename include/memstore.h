@@ -609,8 +609,8 @@ ms_status memstore_summarize_blocks(memstore_t* store, int32_t layer, const int3
 /*
  * Choose the blocks that each new token reads, per K/V head.  The token at position p may read blocks 0 .. p / block_size of its request; block b has the score
  *   sum over the group's query heads and the coordinates of max(q lo_b, q hi_b)  =  sum_d (P_d hi_bd + N_d lo_bd)
- * (P, N: sums over the group of the positive and of the negative parts of q), an upper bound of the group's summed scores of any key in it, formed
- * in 64 bits and rounded to fp32.  The first n_first and the last n_last blocks are always chosen, then the others by score, equal scores the
+ * (P, N: sums over the group of the positive and of the negative parts of q), an upper bound of the group's summed scores of any key in it.  The choice
+ * goes by 64-bit sums rounded to fp32: the first n_first and the last n_last blocks are always chosen, then the others by score, equal scores the
  * lower block first; NaN counts as plus infinity.  Blocks that the table does not name are never chosen.
  *   q, q_start, seq_lens  as for memstore_attend (rotated queries)
  *   summaries    as memstore_summarize_blocks writes them
@@ -618,8 +618,8 @@ ms_status memstore_summarize_blocks(memstore_t* store, int32_t layer, const int3
  *   max_blocks   at most 49,152 here (MS_ERR_UNSUPPORTED)
  *   n_select     1 or more, n_first + n_last at most n_select
  *   out_blocks   device int32 [n_tokens][n_kv_heads][n_select]: block numbers of the request (its table's columns) in rising order, -1 behind the last
- *   out_scores   device fp32 [n_tokens][n_kv_heads][max_blocks] or NULL: the scores of all blocks that the token may read (-infinity: not named
- *                by the table); entries behind its last block are not written
+ *   out_scores   device fp32 [n_tokens][n_kv_heads][max_blocks] or NULL: the scores of all blocks that the token may read as fp32 sums (off by at most
+ *                head_dim * 2^-21 of the sum of the terms' magnitudes; -infinity: not named by the table); entries behind its last block are not written
  * Rows outside every valid request are not written.
  */
 ms_status memstore_select_blocks(memstore_t* store, const ms_heads* q, int32_t n_q_heads, int32_t n_tokens, const int32_t* q_start,

@@ -183,15 +183,26 @@ struct SelectParams {
   float* scores;           // [n_tokens][n_kv][max_blocks] or nullptr
 };
 
-constexpr int kSelectThreads = 256;
 constexpr int kSelectMaxBlocks = 49152;  // keys of a token that fit the shared memory of a CTA
+// Tables up to this are served by CTAs of 128 threads where there are more of them than SMs (100 users with at most 4,000 tokens 11 us, 14 with 256 threads; 60 with
+// at most 16,300 40 and 40, 32,700 71 and 67).
+constexpr int kSelectShort = 1024;
 constexpr int kSelectBins = 2048;
+constexpr int kSelectFew = 256;               // keys at the border that are ranked one against another
 constexpr uint32_t kKeyForced = 0xffffffffu;  // above every score's, which end at plus infinity (NaN counts as that)
 // Order-preserving map of fp32 to integers; 0 is left for blocks that cannot be chosen.
 __device__ __forceinline__ uint32_t select_key(float s) {
   const uint32_t u = s != s ? 0x7f800000u : __float_as_uint(s + 0.f);  // (-0 and +0 are equal)
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
+
+// max(|a|, |b|) of two pairs of bf16, NaN where one is
+__device__ __forceinline__ uint32_t max_magnitudes(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("max.NaN.xorsign.abs.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+__device__ __forceinline__ float select_score(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key); }
 
 // The request of token t, -1: none; by a whole warp, 32 borders at a time.
 __device__ __forceinline__ int request_of_token(const int32_t* q_start, int nreq, int t) {
@@ -211,24 +222,37 @@ __device__ __forceinline__ int request_of_token(const int32_t* q_start, int nreq
   return lo < nreq && __ldg(q_start + lo) <= t && __ldg(q_start + lo + 1) > t ? lo : -1;
 }
 
-// A cluster per (token, K/V head): its CTAs score a part of the blocks each and put the scores' keys into the shared memory of the first one,
-// which finds the border of the n_select best by three passes of counting (11, 11 and 10 bits) and writes the chosen blocks in order.  The sums are
-// formed in 64 bits and rounded to fp32 once: near the border a list depends on the last bits of the scores, which must therefore not depend on the
-// order of summation.  Bound: HBM where many long contexts are scored (a summary is read once per token).
-template <int D>
-__global__ void __launch_bounds__(kSelectThreads) select_kernel(const SelectParams p) {
+// A cluster per (token, K/V head).  Its CTAs score a run of the token's blocks each and put the scores' keys into the shared memory of the first one,
+// which finds the n_select best and writes them in order.
+// Scores: sixteen summaries are the rows of matrix products (m16n8k16); P and N, split into three bf16 numbers each whose sum has their first 24 bits,
+// are three columns.  A lane's 16 bytes of a summary are operands as they come from memory (the order of the elements along the inner dimension is
+// free).
+// Choice: the keys' range is divided into 2,048 bins, of which one holds the border of the best.  With [s, s'] the scores of that bin and e a bound of an
+// fp32 score's error, a block above s' + 2 e is among the best whatever the errors, one below s - 2 e is not, and the few in between are summed again in 64
+// bits and ranked one against another: near the border a list depends on the last bits of the scores, which must not depend on an order of summation.
+// Bound: HBM where many long contexts are scored (a summary is read once per token); the chain of look-ups, scores, border and list for one.
+// 60 users and one long context, us: 64-bit sums for all blocks 109 and 31, fp32 sums in the lanes 80 and 29 (50 instructions per summary and
+// warp), with copies through shared memory 92 and 31, matrix products 67 and 19.
+template <int D, int THREADS>
+__global__ void __launch_bounds__(THREADS, 512 / THREADS) select_kernel(const SelectParams p) {
   namespace cg = cooperative_groups;
-  constexpr int kLanes = D / 4 < 16 ? D / 4 : 16;  // lanes of a summary
-  constexpr int kPieces = D / 4 / kLanes;          // 16-byte pieces that a lane takes of it
-  constexpr int kPerWarp = 32 / kLanes;
-  constexpr int kFlight = kPieces >= 4 ? 2 : 4;    // summaries of a lane that fly together
-  extern __shared__ uint32_t s_keys[];             // [max_blocks], of the cluster's first CTA
+  constexpr int kRecord = 4 * D;                   // bytes of a summary
+  constexpr int kGroups = kRecord / 64;            // 64 bytes of each of 16 summaries are the operands of two products
+  constexpr int kBatch = kGroups < 8 ? kGroups : 8;  // groups whose loads fly together
+  constexpr int kWarps = THREADS / 32;
+  extern __shared__ __align__(16) uint32_t s_keys[];  // of this CTA's run of blocks; in the cluster's first CTA [max_blocks] of all
+  __shared__ uint4 s_b[kGroups][32];               // the columns, as the lanes take them
   __shared__ double s_q[2][D];                     // N, P
   __shared__ uint32_t s_hist[kSelectBins];
-  __shared__ int64_t s_scan[32];
+  __shared__ uint32_t s_scan[32];
   __shared__ int32_t s_req;
-  __shared__ uint32_t s_border[3];
-  __shared__ uint32_t s_counts[2 * kSelectThreads / 32];
+  __shared__ float s_terms;                        // sum of |P| and |N|
+  // of all CTAs of the cluster, in the first one: largest magnitude of a summary, smallest and largest key by score, blocks that can be chosen, that must be
+  __shared__ uint32_t s_top, s_low, s_high, s_can, s_must;
+  __shared__ uint32_t s_border[3], s_few_n;
+  __shared__ uint32_t s_few[kSelectFew];
+  __shared__ int32_t s_few_at[kSelectFew];
+  __shared__ uint32_t s_counts[kWarps];            // chosen blocks of each warp's run
   grid_dependency_wait();
   grid_launch_dependents();
   cg::cluster_group cluster = cg::this_cluster();
@@ -236,19 +260,45 @@ __global__ void __launch_bounds__(kSelectThreads) select_kernel(const SelectPara
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int64_t unit = blockIdx.x / parts;
   const int t = (int)(unit / p.n_kv), head = (int)(unit - (int64_t)t * p.n_kv);
-  if (warp == 0) {
+  if (warp == kWarps - 1) {
     const int r = request_of_token(p.q_start, p.nreq, t);
     if (lane == 0) s_req = r;
   }
-  for (int d = tid; d < D; d += kSelectThreads) {
-    double lo = 0., hi = 0.;
+  // P and N, and their parts: lane (column, row t4) of group j takes the coordinates 32 j + 8 t4 .. + 7
+  if (tid == 0) s_terms = 0.f;
+  __syncthreads();
+  for (int d = tid; d < D; d += THREADS) {  // (whole warps or half of one)
+    const __nv_bfloat16* q = p.q + t * p.q_ts + (int64_t)head * p.group * p.q_hs + d;
+    double sum[2] = {0., 0.};
+#pragma unroll 4
     for (int g = 0; g < p.group; ++g) {
-      const float x = __bfloat162float(p.q[t * p.q_ts + (head * p.group + g) * p.q_hs + d]);
-      if (x >= 0.f) hi += x;
-      else lo += x;  // (NaN too)
+      const float x = __bfloat162float(q[g * p.q_hs]);
+      sum[0] += x >= 0.f ? 0.f : x;  // (NaN too)
+      sum[1] += x >= 0.f ? x : 0.f;
     }
-    s_q[0][d] = lo;
-    s_q[1][d] = hi;
+#pragma unroll
+    for (int side = 0; side < 2; ++side) {
+      s_q[side][d] = sum[side];
+      const int at = side * D + d, e = at & 7;
+      float rest = (float)sum[side];
+#pragma unroll
+      for (int col = 0; col < 3; ++col) {
+        const __nv_bfloat16 part = __float2bfloat16_rn(rest);
+        rest -= __bfloat162float(part);
+        reinterpret_cast<__nv_bfloat16*>(&s_b[at >> 5][col * 4 + ((at & 31) >> 3)])[e] = part;
+      }
+    }
+    float terms = (float)(sum[1] - sum[0]);
+#pragma unroll
+    for (int o = D < 32 ? D / 2 : 16; o; o >>= 1) terms += __shfl_xor_sync(D < 32 ? (1u << (D & 31)) - 1u : 0xffffffffu, terms, o);
+    if ((lane & (D - 1)) == 0) atomicAdd(&s_terms, terms);
+  }
+  for (int i = tid; i < kGroups * 20; i += THREADS) s_b[i / 20][12 + i % 20] = make_uint4(0u, 0u, 0u, 0u);
+  for (int i = tid; i < kSelectBins; i += THREADS) s_hist[i] = 0u;
+  if (tid < kWarps) s_counts[tid] = 0u;
+  if (tid == 0) {
+    s_top = s_high = s_can = s_must = s_few_n = 0u;
+    s_low = kKeyForced;
   }
   cluster.sync();  // (shared memory is there, and the first CTA's may be written)
   const int r = s_req;
@@ -261,131 +311,284 @@ __global__ void __launch_bounds__(kSelectThreads) select_kernel(const SelectPara
   const int32_t* table = p.tables + (int64_t)r * p.max_blocks;
   float* scores = p.scores ? p.scores + unit * p.max_blocks : nullptr;
 
-  // ---- scores
-  const int sub = lane % kLanes;
-  double q[kPieces][8];
-#pragma unroll
-  for (int i = 0; i < kPieces; ++i)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) q[i][e] = (&s_q[0][0])[(sub + i * kLanes) * 8 + e];
-  uint32_t* keys = cluster.map_shared_rank(s_keys, 0);
-  const int step = kPerWarp * kFlight, warps = (int)parts * (kSelectThreads / 32);
-  for (int b0 = ((int)rank * (kSelectThreads / 32) + warp) * step; b0 < nb; b0 += warps * step) {
-    uint4 x[kFlight][kPieces];
-    int32_t blk[kFlight];
-#pragma unroll
-    for (int f = 0; f < kFlight; ++f) {
-      const int b = b0 + f * kPerWarp + lane / kLanes;
-      blk[f] = b < nb ? __ldg(table + b) : -1;
-      if (blk[f] >= p.num_blocks) blk[f] = -1;
+  // ---- scores of this CTA's run (a multiple of four blocks, so that its keys are copied 16 bytes at a time)
+  const int run = ((nb + (int)parts - 1) / (int)parts + 3) & ~3, from = min(nb, (int)rank * run), to = min(nb, from + run);
+  const bool score = scores || nb > p.n_select;  // (else all are chosen)
+  const int g = lane >> 2, t4 = lane & 3;
+  auto entry_of = [&](int b) { return lane < 16 && b + lane < to ? __ldg(table + b + lane) : -1; };
+  // 64-bit sum of a block's score, by the warp
+  auto exact_score = [&](int b) {
+    const uint2* at8 = reinterpret_cast<const uint2*>(p.summaries) + ((int64_t)__ldg(table + b) * p.n_kv + head) * (kRecord / 8);
+    double sum = 0.;
+    for (int i = lane; i < kRecord / 8; i += 32) {
+      const uint2 x = at8[i];
+      const double* qd = &s_q[0][0] + i * 4;
+      sum = fma(qd[0], (double)bf16lo(x.x), sum);
+      sum = fma(qd[1], (double)bf16hi(x.x), sum);
+      sum = fma(qd[2], (double)bf16lo(x.y), sum);
+      sum = fma(qd[3], (double)bf16hi(x.y), sum);
     }
 #pragma unroll
-    for (int f = 0; f < kFlight; ++f)
+    for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    return (float)sum;
+  };
+  uint32_t top[2] = {0u, 0u};  // pairs of bf16: the largest magnitudes read (their signs mean nothing)
+  uint32_t low = kKeyForced, high = 0u;
+  int can = 0, must = 0;
+  int32_t nxt = entry_of(from + warp * 16);
+  for (int b0 = from + warp * 16; b0 < to; b0 += kWarps * 16) {
+    const int32_t blk = nxt >= 0 && nxt < p.num_blocks ? nxt : -1;
+    nxt = entry_of(b0 + kWarps * 16);
+    const unsigned named = __ballot_sync(0xffffffffu, blk >= 0);
+    const int32_t blk_a = __shfl_sync(0xffffffffu, blk, g), blk_b = __shfl_sync(0xffffffffu, blk, g + 8);
+    float c[4] = {0.f, 0.f, 0.f, 0.f}, c2[4] = {0.f, 0.f, 0.f, 0.f};
+    if (score) {
+      // (for a block that the table does not name block 0 is read, and its score left out: a load under a condition would wait for the one before)
+      const uint4* row_a = p.summaries + ((int64_t)max(blk_a, 0) * p.n_kv + head) * (kRecord / 16) + t4;
+      const uint4* row_b = p.summaries + ((int64_t)max(blk_b, 0) * p.n_kv + head) * (kRecord / 16) + t4;
 #pragma unroll
-      for (int i = 0; i < kPieces; ++i)
-        x[f][i] = blk[f] >= 0 ? ld_stream(p.summaries + ((int64_t)blk[f] * p.n_kv + head) * (D / 4) + sub + i * kLanes) : make_uint4(0u, 0u, 0u, 0u);
+      for (int j0 = 0; j0 < kGroups; j0 += kBatch) {
+        uint4 xa[kBatch], xb[kBatch];
 #pragma unroll
-    for (int f = 0; f < kFlight; ++f) {
-      double s = 0.;
+        for (int j = 0; j < kBatch; ++j) {
+          xa[j] = ld_stream(row_a + (j0 + j) * 4);
+          xb[j] = ld_stream(row_b + (j0 + j) * 4);
+        }
 #pragma unroll
-      for (int i = 0; i < kPieces; ++i) {
-        const uint32_t y[4] = {x[f][i].x, x[f][i].y, x[f][i].z, x[f][i].w};
+        for (int j = 0; j < kBatch; ++j) {
+          const uint4 w = s_b[j0 + j][lane];
+          const uint32_t lo[4] = {xa[j].x, xb[j].x, xa[j].y, xb[j].y}, hi[4] = {xa[j].z, xb[j].z, xa[j].w, xb[j].w};
+          mma16816<false>(c, lo, w.x, w.y);
+          mma16816<false>(c2, hi, w.z, w.w);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          s = fma(q[i][2 * e], (double)bf16lo(y[e]), s);
-          s = fma(q[i][2 * e + 1], (double)bf16hi(y[e]), s);
+          for (int e = 0; e < 4; ++e) top[e & 1] = max_magnitudes(top[e & 1], max_magnitudes(lo[e], hi[e]));
         }
       }
+    }
 #pragma unroll
-      for (int o = kLanes / 2; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-      const int b = b0 + f * kPerWarp + lane / kLanes;
-      if (sub == 0 && b < nb) {
-        const float v = blk[f] >= 0 ? (float)s : -INFINITY;
-        if (scores) scores[b] = v;
-        keys[b] = blk[f] < 0 ? 0u : b < p.n_first || b >= all - p.n_last ? kKeyForced : select_key(v);
+    for (int e = 0; e < 4; ++e) c[e] += c2[e];
+    // columns 0 and 1 are in lane t4 = 0, column 2 in lane t4 = 1; the first writes the score of summary g, the second that of g + 8
+    const float pa = t4 == 0 ? c[0] + c[1] : c[0], pb = t4 == 0 ? c[2] + c[3] : c[2];
+    const float va = pa + __shfl_xor_sync(0xffffffffu, pa, 1), vb = pb + __shfl_xor_sync(0xffffffffu, pb, 1);
+    const int rec = t4 == 0 ? g : g + 8, b = b0 + rec;
+    const bool there = (named >> rec) & 1u, writes = t4 < 2 && b < to;
+    float v = there ? (t4 == 0 ? va : vb) : -INFINITY;
+    // (an infinity in a summary meets the zeros among the columns: those scores are summed again)
+    unsigned odd = __ballot_sync(0xffffffffu, writes && there && score && !(fabsf(v) < INFINITY));
+    while (odd) {
+      const int l = __ffs(odd) - 1;
+      odd &= odd - 1u;
+      const float x = exact_score(__shfl_sync(0xffffffffu, b, l));
+      if (lane == l) v = x;
+    }
+    if (writes) {
+      if (scores) scores[b] = v;
+      uint32_t k = 0u;
+      if (there) {
+        ++can;
+        if (!score || b < p.n_first || b >= all - p.n_last) {
+          k = kKeyForced;
+          ++must;
+        } else {
+          k = select_key(v);
+          low = min(low, k);
+          high = max(high, k);
+        }
       }
+      s_keys[b - from] = k;
     }
   }
-  cluster.sync();
-  if (rank != 0) return;
+  top[0] = max_magnitudes(top[0], top[1]) & 0x7fff7fffu;
+  const uint32_t largest = __reduce_max_sync(0xffffffffu, max(top[0] & 0xffffu, top[0] >> 16));
+  low = __reduce_min_sync(0xffffffffu, low);
+  high = __reduce_max_sync(0xffffffffu, high);
+  can = __reduce_add_sync(0xffffffffu, can);
+  must = __reduce_add_sync(0xffffffffu, must);
+  if (lane == 0 && can > 0) {
+    atomicMax(cluster.map_shared_rank(&s_top, 0), largest);
+    atomicMin(cluster.map_shared_rank(&s_low, 0), low);
+    atomicMax(cluster.map_shared_rank(&s_high, 0), high);
+    atomicAdd(cluster.map_shared_rank(&s_can, 0), (uint32_t)can);
+    if (must) atomicAdd(cluster.map_shared_rank(&s_must, 0), (uint32_t)must);
+  }
+  if (parts > 1) {
+    __syncthreads();
+    if (rank != 0) {
+      uint4* keys = reinterpret_cast<uint4*>(cluster.map_shared_rank(s_keys, 0) + from);
+      for (int i = tid; i < (to - from + 3) / 4; i += THREADS) keys[i] = reinterpret_cast<const uint4*>(s_keys)[i];
+    }
+    cluster.sync();
+    if (rank != 0) return;
+  } else {
+    __syncthreads();
+  }
 
-  // ---- the border: the key of the n_select-th best, and how many blocks with that key are taken
-  int can = 0;
-  for (int b = tid; b < nb; b += kSelectThreads) can += s_keys[b] != 0u;
-  int64_t total;
-  block_scan<kSelectThreads>(can, s_scan, &total);
-  uint32_t border = 0u;
-  int ties = 0;
-  if (total > p.n_select) {
-    uint32_t prefix = 0u, prefix_mask = 0u;
-    int want = p.n_select;
-    for (int pass = 0; pass < 3; ++pass) {
-      const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bins = pass == 2 ? 1024 : 2048;
-      for (int i = tid; i < kSelectBins; i += kSelectThreads) s_hist[i] = 0u;
-      __syncthreads();
-      for (int b = tid; b < nb; b += kSelectThreads) {
-        const uint32_t k = s_keys[b];
-        if (k != 0u && (k & prefix_mask) == prefix) atomicAdd(&s_hist[(k >> shift) & (bins - 1)], 1u);
+  // ---- the choice.  A warp has a run of blocks; chosen blocks end with the key kKeyForced, the others with 0
+  const int w_run = ((nb + THREADS - 1) / THREADS) * 32, w_from = warp * w_run, w_to = min(nb, w_from + w_run);
+  // keeps the blocks for which keep(key) is above 0 as chosen, those for which it is 0 near the border, and takes the others out
+  auto divide = [&](auto keep) {
+    int chosen = 0;
+    for (int b = w_from + lane; b < w_to; b += 32) {
+      const uint32_t k = s_keys[b];
+      if (k == 0u) continue;
+      const int how = k == kKeyForced ? 1 : keep(k);
+      if (how > 0) ++chosen;
+      if (how == 0) {
+        const uint32_t i = atomicAdd(&s_few_n, 1u);
+        if (i < kSelectFew) s_few_at[i] = b;
+      } else {
+        s_keys[b] = how > 0 ? kKeyForced : 0u;
       }
+    }
+    chosen = __reduce_add_sync(0xffffffffu, chosen);
+    if (lane == 0) s_counts[warp] = (uint32_t)chosen;
+    __syncthreads();
+  };
+  // the bin of [low, high], cut into 2,048, that holds the want-th largest key: it becomes [low, high], want counts in it, its keys are returned
+  int want = 0;
+  auto find_bin = [&](bool clear) {
+    const int shift = max(0, 21 - __clz(high - low));  // (high - low) >> shift < 2048
+    if (clear) {
+      for (int i = tid; i < kSelectBins; i += THREADS) s_hist[i] = 0u;
       __syncthreads();
-      // thread i has the bins from the top: 8 i .. 8 i + 7
-      constexpr int kBins = kSelectBins / kSelectThreads;
-      uint32_t mine = 0u;
+    }
+    for (int b = tid; b < nb; b += THREADS) {
+      const uint32_t k = s_keys[b];
+      if (k >= low && k <= high && k != 0u) atomicAdd(&s_hist[(k - low) >> shift], 1u);
+    }
+    __syncthreads();
+    // thread i has bins from the top on
+    constexpr int kBins = kSelectBins / THREADS;
+    uint32_t here = 0u;
 #pragma unroll
-      for (int i = 0; i < kBins; ++i) mine += s_hist[kSelectBins - 1 - (tid * kBins + i)];
-      const int64_t upto = block_scan<kSelectThreads>((int64_t)mine, s_scan, &total);
-      if (upto >= want && upto - mine < want) {
-        int before = (int)(upto - mine);
-        for (int i = 0; i < kBins; ++i) {
-          const int bin = kSelectBins - 1 - (tid * kBins + i);
-          if (before + (int)s_hist[bin] >= want) {
-            s_border[0] = (uint32_t)bin;
-            s_border[1] = (uint32_t)(want - before);
-            break;
-          }
-          before += s_hist[bin];
+    for (int i = 0; i < kBins; ++i) here += s_hist[kSelectBins - 1 - (tid * kBins + i)];
+    uint32_t sum = here;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t u = __shfl_up_sync(0xffffffffu, sum, o);
+      if (lane >= o) sum += u;
+    }
+    if (lane == 31) s_scan[warp] = sum;
+    __syncthreads();
+    int upto = (int)sum;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w)
+      if (w < warp) upto += (int)s_scan[w];
+    if (upto >= want && upto - (int)here < want) {
+      int before = upto - (int)here;
+      for (int i = 0; i < kBins; ++i) {
+        const int bin = kSelectBins - 1 - (tid * kBins + i);
+        if (before + (int)s_hist[bin] >= want) {
+          s_border[0] = (uint32_t)bin;
+          s_border[1] = (uint32_t)(want - before);
+          break;
+        }
+        before += s_hist[bin];
+      }
+    }
+    __syncthreads();
+    low += s_border[0] << shift;
+    high = shift ? min(high, low + ((1u << shift) - 1u)) : low;
+    want = (int)s_border[1];
+  };
+  // the best `want` of the keys in [low, high] by key, equal ones the lower first; the rest of the range is out
+  auto settle = [&] {
+    while (low < high) find_bin(true);
+    // `want` of the equals, counted along the blocks
+    const uint32_t border = low;
+    int equal = 0;
+    for (int b = w_from + lane; b < w_to; b += 32) equal += s_keys[b] == border;
+    equal = __reduce_add_sync(0xffffffffu, equal);
+    __syncthreads();
+    if (lane == 0) s_scan[warp] = (uint32_t)equal;
+    __syncthreads();
+    int before = 0;
+    for (int w = 0; w < warp; ++w) before += (int)s_scan[w];
+    for (int b0 = w_from; b0 < w_to; b0 += 32) {
+      const int b = b0 + lane;
+      const bool is = b < w_to && s_keys[b] == border;
+      const unsigned m = __ballot_sync(0xffffffffu, is);
+      if (is) s_keys[b] = before + __popc(m & ((1u << lane) - 1u)) < want ? kKeyForced : 0u;
+      before += __popc(m);
+    }
+    __syncthreads();
+    divide([&](uint32_t k) { return k > border ? 1 : -1; });
+  };
+  const int can_all = (int)s_can, must_all = (int)s_must;
+  if (can_all <= p.n_select) {
+    divide([](uint32_t) { return 1; });
+  } else if (must_all >= p.n_select) {
+    divide([](uint32_t) { return -1; });
+  } else {
+    want = p.n_select - must_all;
+    low = s_low;
+    high = s_high;
+    find_bin(false);
+    // Error of an fp32 score, in terms of the sum t of the terms' magnitudes, at most (sum of |P| and |N|) x (largest magnitude of a summary): a
+    // product of 16 adds 17 numbers, each cut off at 2^-23 of the largest or better, and there are D / 8 one after another; the three parts of P
+    // and N leave out 2^-23, and the sums of the columns and of the 64-bit score's rounding are off by 2^-24 three times.  Parts below bf16's
+    // smallest normal number are off by 2^-133.  (Sums that may leave fp32's range have no such bound.)
+    const float largest_ever = __uint_as_float(s_top << 16), sum_q = 1.001f * s_terms, terms = sum_q * largest_ever;
+    const float err = terms < 1e38f && sum_q < 1e38f ? (D / 8 * 17 + 4) * 1.2e-07f * terms + 2 * D * 1e-40f * (largest_ever + 1.f) : INFINITY;
+    const float most = __fadd_ru(select_score(high), 2.f * err), least = __fadd_rd(select_score(low), -2.f * err);
+    // (all are near where the bound is infinite)
+    const uint32_t k_most = err < INFINITY ? select_key(most) : kKeyForced, k_least = err < INFINITY ? select_key(least) : 0u;
+    divide([&](uint32_t k) { return k > k_most ? 1 : k < k_least ? -1 : 0; });
+    const int near = (int)s_few_n;
+    want = p.n_select;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) want -= (int)s_counts[w];
+    // 64-bit sums of the blocks near the border
+    const int n = near <= kSelectFew ? near : nb;
+    if (near > want) {
+      for (int i = warp; i < n; i += kWarps) {
+        const int b = near <= kSelectFew ? s_few_at[i] : i;
+        if (s_keys[b] == 0u || s_keys[b] == kKeyForced) continue;
+        const uint32_t k = select_key(exact_score(b));
+        __syncwarp();
+        if (lane == 0) {
+          s_keys[b] = k;
+          if (near <= kSelectFew) s_few[i] = k;
         }
       }
       __syncthreads();
-      prefix |= s_border[0] << shift;
-      prefix_mask |= (uint32_t)(bins - 1) << shift;
-      want = (int)s_border[1];
     }
-    border = prefix;
-    ties = want;
+    if (near <= kSelectFew) {
+      for (int i = tid; i < near; i += THREADS) {
+        const int b = s_few_at[i];
+        int before = 0;
+        if (near > want) {
+          const uint32_t k = s_few[i];
+          for (int j = 0; j < near; ++j) before += s_few[j] > k || (s_few[j] == k && s_few_at[j] < b);
+        }
+        const bool chosen = before < want;
+        s_keys[b] = chosen ? kKeyForced : 0u;
+        if (chosen) atomicAdd(&s_counts[b / w_run], 1u);
+      }
+      __syncthreads();
+    } else {
+      low = 1u;
+      high = kKeyForced - 1u;
+      settle();
+    }
   }
-  // ---- the chosen blocks in rising order: a warp has a run of blocks
-  const int run = ((nb + kSelectThreads - 1) / kSelectThreads) * 32, from = warp * run, to = min(nb, from + run);
-  uint32_t above = 0u, equal = 0u;
-  for (int b0 = from; b0 < to; b0 += 32) {
-    const int b = b0 + lane;
-    const uint32_t k = b < to ? s_keys[b] : 0u;
-    above += __popc(__ballot_sync(0xffffffffu, k > border));
-    equal += __popc(__ballot_sync(0xffffffffu, k == border && k != 0u));
-  }
-  if (lane == 0) {
-    s_counts[warp] = above;
-    s_counts[kSelectThreads / 32 + warp] = equal;
-  }
-  __syncthreads();
-  uint32_t above_before = 0u, equal_before = 0u, above_all = 0u, equal_all = 0u;
-  for (int w = 0; w < kSelectThreads / 32; ++w) {
-    if (w < warp) above_before += s_counts[w], equal_before += s_counts[kSelectThreads / 32 + w];
-    above_all += s_counts[w], equal_all += s_counts[kSelectThreads / 32 + w];
+  // ---- the list, in rising order
+  uint32_t at = 0u, taken = 0u;
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) {
+    const uint32_t n = s_counts[w];
+    if (w < warp) at += n;
+    taken += n;
   }
   int32_t* out = p.blocks + unit * p.n_select;
-  const unsigned lower = (1u << lane) - 1u;
-  for (int b0 = from; b0 < to; b0 += 32) {
+  for (int b0 = w_from; b0 < w_to; b0 += 32) {
     const int b = b0 + lane;
-    const uint32_t k = b < to ? s_keys[b] : 0u;
-    const unsigned ma = __ballot_sync(0xffffffffu, k > border), me = __ballot_sync(0xffffffffu, k == border && k != 0u);
-    const uint32_t eq = equal_before + __popc(me & lower);  // blocks with the border's key before this one
-    if (k > border || (k != 0u && k == border && eq < (uint32_t)ties)) out[above_before + __popc(ma & lower) + min(eq, (uint32_t)ties)] = b;
-    above_before += __popc(ma);
-    equal_before += __popc(me);
+    const bool chosen = b < w_to && s_keys[b] == kKeyForced;
+    const unsigned m = __ballot_sync(0xffffffffu, chosen);
+    if (chosen) out[at + __popc(m & ((1u << lane) - 1u))] = b;
+    at += __popc(m);
   }
-  const int taken = (int)(above_all + min(equal_all, (uint32_t)ties));
-  for (int i = taken + tid; i < p.n_select; i += kSelectThreads) out[i] = -1;
+  for (int i = (int)taken + tid; i < p.n_select; i += THREADS) out[i] = -1;
 }
 
 }  // namespace ms

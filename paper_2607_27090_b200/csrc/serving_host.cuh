@@ -586,16 +586,15 @@ ms_status memstore_summarize_blocks(memstore_t* s, int32_t layer, const int32_t*
   return MS_OK;
 }
 
-// Shared-memory limit and cluster size of the selection kernels, raised once per device.
+// Shared-memory limit of the selection kernels, raised once per device.
 static cudaError_t select_prepare(int device, const void* kernel) {
   static std::mutex mu;
-  static const void* done[64][5] = {};
+  static const void* done[64][15] = {};
   std::lock_guard<std::mutex> lock(mu);
   for (const void*& d : done[device & 63]) {
     if (d == kernel) return cudaSuccess;
     if (d) continue;
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSelectMaxBlocks * 4);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     if (e == cudaSuccess) d = kernel;
     return e;
   }
@@ -644,21 +643,35 @@ ms_status memstore_select_blocks(memstore_t* s, const ms_heads* q, int32_t n_q_h
   p.n_last = n_last;
   p.blocks = out_blocks;
   p.scores = out_scores;
-  void (*kernel)(SelectParams) = c.head_dim == 16 ? select_kernel<16> : c.head_dim == 32 ? select_kernel<32> : c.head_dim == 64 ? select_kernel<64>
-                               : c.head_dim == 128 ? select_kernel<128> : select_kernel<256>;
-  MS_CUDA(s, select_prepare(c.device, (const void*)kernel));
-  // CTAs of a cluster: as many as find an SM of their own, each with some hundred blocks to score
+  // CTAs of a cluster: as many as find an SM of their own, each with some hundred blocks to score.  CTAs of 512 threads where there is one per SM, of
+  // 128 where tables are short.
   const int64_t units = (int64_t)n_tokens * c.n_kv_heads;
+  const size_t key_bytes = ((size_t)max_blocks + 3) / 4 * 16;
   unsigned parts = 1;
-  while (parts < 16 && units * parts * 2 <= s->sm_count && max_blocks >= (int)parts * 2 * 128) parts *= 2;
+  while (parts < 8 && units * parts * 2 <= s->sm_count && max_blocks >= (int)parts * 2 * 128) parts *= 2;
+  const bool wide = units * parts <= s->sm_count;
+  const int threads = wide ? 512 : max_blocks <= kSelectShort ? 128 : 256;
+  auto pick = [&](auto dim) -> void (*)(SelectParams) {
+    constexpr int kDim = decltype(dim)::value;
+    return threads == 512 ? select_kernel<kDim, 512> : threads == 256 ? select_kernel<kDim, 256> : select_kernel<kDim, 128>;
+  };
+  void (*kernel)(SelectParams) = nullptr;
+  switch (c.head_dim) {
+    case 16: kernel = pick(ChunkInt<16>{}); break;
+    case 32: kernel = pick(ChunkInt<32>{}); break;
+    case 64: kernel = pick(ChunkInt<64>{}); break;
+    case 128: kernel = pick(ChunkInt<128>{}); break;
+    default: kernel = pick(ChunkInt<256>{}); break;
+  }
+  MS_CUDA(s, select_prepare(c.device, (const void*)kernel));
   cudaLaunchConfig_t lc{};
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   attr[1].id = cudaLaunchAttributeClusterDimension;
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-  lc.blockDim = dim3(kSelectThreads);
-  lc.dynamicSmemBytes = (size_t)max_blocks * 4;
+  lc.blockDim = dim3((unsigned)threads);
+  lc.dynamicSmemBytes = key_bytes;
   lc.stream = (cudaStream_t)stream;
   lc.attrs = attr;
   lc.numAttrs = 2;

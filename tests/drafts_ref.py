@@ -100,6 +100,13 @@ def scores(q, box):
     return (p * box[:, 1].double() + n * box[:, 0].double()).sum(1)
 
 
+def magnitudes(q, box):
+    """Sums of the magnitudes of what `scores` sums."""
+    x = q.double()[:, None]
+    p, n = x.clamp(min=0).sum(0), x.clamp(max=0).sum(0)
+    return (p * box[:, 1].double().abs() - n * box[:, 0].double().abs()).sum(1)
+
+
 def choose(score, named, n_select, n_first, n_last, all_blocks):
     """Chosen blocks in rising order: score fp32 [blocks], named: which the table names."""
     s = np.where(np.isnan(score), np.inf, score)
