@@ -71,8 +71,12 @@ __device__ __forceinline__ uint32_t half2_to_bf16(uint32_t h) {
 }
 
 constexpr int kSummaryThreads = 256;
-constexpr int kSummaryCtasPerSm = 6;
-constexpr int kSummaryFlight = 4;  // loads of a thread that fly together
+// Loads of a thread that fly together, and CTAs per SM.  32 contexts, 250K tokens, 8 heads of 128: eight loads and four CTAs 84 us (6.2 TB/s), four and
+// six 98; an 8-bit cache, whose values take twice the registers once they are fp16, 75 with four and six, 105 with eight and four.
+template <bool FP8>
+constexpr int kSummaryFlight = FP8 ? 4 : 8;
+template <bool FP8>
+constexpr int kSummaryCtasPerSm = FP8 ? 6 : 4;
 
 // A warp per (block, K/V head); heads of a block follow one another, so that a CTA reads whole rows of a token-major cache.  The items of
 // all requests form a line of which every CTA takes an equal share.  Bound: HBM where there are many blocks (each key is read once), else latency.
@@ -120,13 +124,14 @@ __global__ void __launch_bounds__(kSummaryThreads) summarize_kernel(const Summar
     const int last = min(p.block_size, span.len - b * p.block_size) - 1;  // the block's last key
     const uint8_t* base = p.k_cache + blk * p.block_stride + head * p.head_stride + (lane % kLanes) * 16;
     uint32_t lo[kWords], hi[kWords];
-    for (int k0 = 0; k0 <= last; k0 += kRows * kSummaryFlight) {
-      uint4 x[kSummaryFlight];
+    constexpr int kFlight = kSummaryFlight<FP8>;
+    for (int k0 = 0; k0 <= last; k0 += kRows * kFlight) {
+      uint4 x[kFlight];
 #pragma unroll
-      for (int i = 0; i < kSummaryFlight; ++i)  // (behind the last key the last key again, which changes nothing)
+      for (int i = 0; i < kFlight; ++i)  // (behind the last key the last key again, which changes nothing)
         x[i] = ld_stream(reinterpret_cast<const uint4*>(base + (int64_t)min(last, k0 + i * kRows + lane / kLanes) * p.token_stride));
 #pragma unroll
-      for (int i = 0; i < kSummaryFlight; ++i) {
+      for (int i = 0; i < kFlight; ++i) {
         uint32_t y[kWords];
         if constexpr (FP8) {
           e4m3x4_half2(x[i].x, y[0], y[1]);

@@ -261,7 +261,13 @@ static ms_status attend_launch(memstore* s, ChunkParams& c, int64_t max_rows, cu
   const int min_rows = chunk_min_rows((int64_t)p.n_kv * p.nreq, s->sm_count);
   // (tokens that read lists of blocks of their own have no keys in common: nothing for the chunk kernel)
   constexpr bool kChunks = SEE != kSeeBlocks && (D == 64 || D == 128);
-  const bool chunks = kChunks && max_rows > min_rows;
+  // Trees whose tiles leave each CTA of the rows kernel at most ten, by the longest context that the tables can hold, stay there: one request of
+  // 500 tokens (32/8 heads of 128) with 9 nodes 12 us against 18 in the chunk kernel, with 64 20 and 22; of 2,033 with 26 nodes 22.7 and 23.4 (6 tiles), with 64 32 and 25 (14
+  // tiles); four of 1,000 with 16 nodes 22 and 24 (7 tiles), with 26 28 and 27 (12 tiles).
+  const int64_t longest = std::min<int64_t>((int64_t)p.max_blocks * p.block_size, kAttnMaxLen);
+  const int64_t row_tiles = (int64_t)p.nreq * p.n_kv * ((max_rows + kAttnRows - 1) / kAttnRows);
+  const bool few = SEE == kSeeTree && row_tiles < kMaxCount && row_tiles * ((longest + 63) / 64) <= (int64_t)10 * s->sm_count * AttnCfg<D, FP8>::kCtasPerSm;
+  const bool chunks = kChunks && max_rows > min_rows && !few;
   const bool rows = !chunks || p.nreq > 1;
   c.min_rows = rows ? min_rows : 0;
   p.max_rows = chunks ? c.min_rows : 0x7fffffff;
@@ -529,7 +535,7 @@ ms_status memstore_accept(memstore_t* s, const int32_t* parents, const int32_t* 
     MS_CUDA(s, launch_dependent(accept_walk_kernel, dim3((unsigned)((nreq + kWalkWarps - 1) / kWalkWarps)), dim3(kWalkWarps * 32), 0, st, p));
     s->kernels_launched++;
   }
-  const int64_t columns = (int64_t)c.n_layers * 2 * c.n_kv_heads * p.row_chunks;
+  const int64_t columns = (int64_t)(c.n_layers + 1) / 2 * c.n_kv_heads * p.row_chunks;
   const int64_t items = (columns + kMoveThreads - 1) / kMoveThreads * nreq;
   MS_CUDA(s, launch_dependent(accept_move_kernel, dim3(1u + (unsigned)std::min<int64_t>(items, (int64_t)s->sm_count * kMoveCtasPerSm)), dim3(kMoveThreads), 0, st, p));
   s->kernels_launched++;
@@ -572,7 +578,7 @@ ms_status memstore_summarize_blocks(memstore_t* s, int32_t layer, const int32_t*
   // blocks that the call can touch at most: a request's new tokens begin and end inside a block
   const int64_t blocks = q_start ? n_tokens / cache->block_size + 2 * (int64_t)nreq : (int64_t)nreq * max_blocks;
   const int64_t ctas = (blocks * c.n_kv_heads + kSummaryThreads / 32 - 1) / (kSummaryThreads / 32);
-  const dim3 grid((unsigned)std::min<int64_t>(ctas, (int64_t)s->sm_count * kSummaryCtasPerSm));
+  const dim3 grid((unsigned)std::min<int64_t>(ctas, (int64_t)s->sm_count * (fp8 ? kSummaryCtasPerSm<true> : kSummaryCtasPerSm<false>)));
   void (*kernel)(SummaryParams) = nullptr;
   switch (c.head_dim) {
     case 16: kernel = fp8 ? summarize_kernel<16, true> : summarize_kernel<16, false>; break;

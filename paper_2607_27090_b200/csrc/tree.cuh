@@ -217,10 +217,11 @@ __device__ __forceinline__ void accept_trim(const AcceptParams& p, int64_t* s_wa
   if (threadIdx.x == 0) *p.out_n_taken = (int32_t)(taken - returned);
 }
 
-// Moves the accepted nodes' rows to their places behind the context, and returns blocks (block 0).  A thread has one 16-byte column
-// (layer, K or V, head, piece) of a request and takes the accepted nodes in order, kMoveBatch loads before their stores: path[j] >= j,
-// so no row is written before it has been read.  Bound: HBM for many requests, the chain of look-ups for one.
-constexpr int kMoveBatch = 4;
+// Moves the accepted nodes' rows to their places behind the context, and returns blocks (block 0).  A thread has the same 16 bytes of a head's row in K and V
+// of two layers and takes the accepted nodes in order, kMoveBatch rows' loads before their stores: path[j] >= j, so no row is written before
+// it has been read.  Bound: HBM for many requests, the chain of look-ups (accepted, path, table) for one; with one column a thread, which
+// looks up as much for a quarter of the bytes, 90 requests take 13.7 us instead of 9.6.
+constexpr int kMoveBatch = 2;
 constexpr int kMoveCtasPerSm = 8;
 __global__ void __launch_bounds__(kMoveThreads) accept_move_kernel(const AcceptParams p) {
   __shared__ int64_t s_warp[32];
@@ -230,42 +231,49 @@ __global__ void __launch_bounds__(kMoveThreads) accept_move_kernel(const AcceptP
     if (p.free_blocks) accept_trim(p, s_warp);
     return;
   }
-  const int per_layer = 2 * p.n_kv * p.row_chunks;
-  const int64_t columns = (int64_t)p.n_layers * per_layer, pieces = (columns + kMoveThreads - 1) / kMoveThreads;
+  const int per_pair = p.n_kv * p.row_chunks;
+  const int64_t columns = (int64_t)(p.n_layers + 1) / 2 * per_pair, pieces = (columns + kMoveThreads - 1) / kMoveThreads;
   for (int64_t item = blockIdx.x - 1; item < pieces * p.nreq; item += gridDim.x - 1) {
     const int64_t r = item / pieces, column = (item - r * pieces) * kMoveThreads + threadIdx.x;
     const int a = p.n_accepted[r];
     if (a <= 1 || column >= columns) continue;
     const int32_t q0 = p.q_start[r], start = p.out_lens[r] - a;
-    const int layer = (int)(column / per_layer), c = (int)(column - (int64_t)layer * per_layer);
-    const int head = (c / p.row_chunks) % p.n_kv;
-    uint8_t* base = (c >= p.n_kv * p.row_chunks ? p.v_cache : p.k_cache) + layer * p.layer_stride + head * p.head_stride + (c % p.row_chunks) * 16;
+    const int layer = 2 * (int)(column / per_pair), c = (int)(column % per_pair), head = c / p.row_chunks;
+    const int64_t at = layer * p.layer_stride + head * p.head_stride + (c % p.row_chunks) * 16;
+    const bool two = layer + 1 < p.n_layers;
+    uint8_t* const base[4] = {p.k_cache + at, p.v_cache + at, p.k_cache + at + p.layer_stride, p.v_cache + at + p.layer_stride};
     const int32_t* table = p.tables + r * p.max_blocks;
-    auto place = [&](int32_t pos) -> uint8_t* {
+    auto place = [&](int32_t pos) -> int64_t {
       const int b = pos / p.block_size;
       const int32_t blk = b < p.max_blocks ? table[b] : -1;
-      return blk >= 0 && blk < p.num_blocks ? base + blk * p.block_stride + (pos - b * p.block_size) * p.token_stride : nullptr;
+      return blk >= 0 && blk < p.num_blocks ? blk * p.block_stride + (pos - b * p.block_size) * p.token_stride : -1;
     };
     for (int i0 = 1; i0 < a; i0 += kMoveBatch) {
-      uint4 x[kMoveBatch];
-      uint8_t* to[kMoveBatch];
+      uint4 x[kMoveBatch][4];
+      int64_t to[kMoveBatch];
 #pragma unroll
       for (int j = 0; j < kMoveBatch; ++j) {
         const int i = i0 + j;
         const int from = i < a ? p.path[q0 + i] : i;
-        to[j] = nullptr;
+        to[j] = -1;
         if (from != i) {
-          const uint8_t* src = place(start + from);
+          const int64_t src = place(start + from);
           to[j] = place(start + i);
-          if (src && to[j])
-            x[j] = *reinterpret_cast<const uint4*>(src);
-          else
-            to[j] = nullptr;
+          if (src < 0) to[j] = -1;
+          if (to[j] >= 0) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (e < 2 || two) x[j][e] = *reinterpret_cast<const uint4*>(base[e] + src);
+          }
         }
       }
 #pragma unroll
       for (int j = 0; j < kMoveBatch; ++j)
-        if (to[j]) *reinterpret_cast<uint4*>(to[j]) = x[j];
+        if (to[j] >= 0) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (e < 2 || two) *reinterpret_cast<uint4*>(base[e] + to[j]) = x[j][e];
+        }
     }
   }
 }

@@ -804,15 +804,19 @@ class MemStore:
             (ints,) = self._empty(stream, ((T + 4 * nreq + 1,), i32))
             path, a, said, lens, status, taken = ints.split_with_sizes((T, nreq, nreq, nreq, nreq, 1))
             out = Accepted(path, a, said, lens, None if n_taken is None else taken, status)
+            at = ints.data_ptr()
+            a, n = at + 4 * T, 4 * nreq
+            outs = (at, a, a + n, a + 2 * n, None if n_taken is None else a + 4 * n, a + 3 * n)
+        else:
+            outs = (ptr(out.path, i32, "out.path", (T,)), ptr(out.n_accepted, i32, "out.n_accepted", (nreq,)),
+                    ptr(out.next_tokens, i32, "out.next_tokens", (nreq,)), ptr(out.seq_lens, i32, "out.seq_lens", (nreq,)),
+                    None if n_taken is None else ptr(out.n_taken, i32, "out.n_taken", (1,)), ptr(out.status, i32, "out.status", (nreq,)))  # fmt: skip
         self._check(self._lib.memstore_accept(
             self._h, ptr(parents, i32, "parents", (T,)), ptr(tokens, i32, "tokens", (T,)), ptr(choices, i32, "choices", (T,)),
             ptr(positions, i32, "positions", (T,)), T, ptr(q_start, i32, "q_start", (nreq + 1,)), ptr(seq_lens, i32, "seq_lens", (nreq,)), nreq,
             ptr(block_tables, i32, "block_tables"), block_tables.shape[1], self._paged(cache),
             None if free_blocks is None else ptr(free_blocks, i32, "free_blocks"), 0 if free_blocks is None else free_blocks.numel(),
-            None if n_taken is None else ptr(n_taken, i32, "n_taken", (1,)), ptr(out.path, i32, "out.path", (T,)),
-            ptr(out.n_accepted, i32, "out.n_accepted", (nreq,)), ptr(out.next_tokens, i32, "out.next_tokens", (nreq,)),
-            ptr(out.seq_lens, i32, "out.seq_lens", (nreq,)), None if n_taken is None else ptr(out.n_taken, i32, "out.n_taken", (1,)),
-            ptr(out.status, i32, "out.status", (nreq,)), self._raw_stream(stream)))  # fmt: skip
+            None if n_taken is None else ptr(n_taken, i32, "n_taken", (1,)), *outs, self._raw_stream(stream)))  # fmt: skip
         return out
 
     # -- selected blocks -----------------------------------------------------------------------------

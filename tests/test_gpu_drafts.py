@@ -91,8 +91,14 @@ def test_plan_reports_what_it_refuses():
 
 
 # ------------------------------------------------------------------------------------------------ attention
-def check_tree(ms, cache, q, q_start, lens, tables, mask, layer=0, scale=0.0, max_q_len=0, want_status=None, **kw):
+def check_tree(ms, cache, q, q_start, lens, tables, mask, layer=0, scale=0.0, max_q_len=0, want_status=None, wide=True, **kw):
+    """Against the definition; with ``wide`` once more with tables of many more columns, which steers the call to the kernel for long contexts."""
     T, hq, d = q.shape
+    if wide:
+        pad = torch.full((tables.shape[0], 40000 // cache.block_size + 1000), -1, dtype=torch.int32, device=DEV)
+        few = torch.tensor([st & 4 for st in want_status or []]).any().item()
+        if not few:
+            check_tree(ms, cache, q, q_start, lens, torch.cat([tables, pad], 1), mask, layer, scale, max_q_len, want_status, False, **kw)
     out = torch.full((T, hq, d), 9.0, dtype=torch.bfloat16, device=DEV)
     lse = torch.full((T, hq), 9.0, device=DEV)
     status = i32([-5] * len(lens))
@@ -283,7 +289,7 @@ def test_tree_attention_holes_strides_and_refusals():
 
 def test_tree_attention_reports_a_wait_that_ran_out_and_works_again():
     rng = random.Random(2)
-    tables, nb = paged(rng, [900], 16)
+    tables, nb = paged(rng, [900], 16, width_extra=8000)  # (as wide as for a long context, which steers the call to the kernel that waits)
     cache, gen = fill_cache(1, nb, 16, 2, 128, False, "NHD", 2)
     ms = store(2, 128)
     q = torch.randn((60, 8, 128), generator=gen, device=DEV).to(torch.bfloat16)
