@@ -16,12 +16,12 @@
 // columns and are the A operand of the second product, whose accumulator stays in TMEM for the whole unit.
 //   warps 0-7, 8-15  queries (scaled to fp16 for an 8-bit cache), weights and epilogue of rows 0-127, 128-255: two threads share a row,
 //                    64 of the tile's keys each (16 warps: a single warp per scheduler cannot keep the exponentials' unit busy)
-//   warp 22          loads: K and V tiles of 128 keys through a ring of 5 buffers, gathered through the block table by tensor copies of a block
+//   warps 22, 23     loads: K and V tiles of 128 keys through a ring of 5 buffers, gathered through the block table by tensor copies of a block
 //                    each (block sizes that divide 128, from 8 on, and multiples of 128)
 //   warps 16-19      work on tiles between their copy and the tensor cores: codes of an 8-bit cache become fp16, exactly; V tiles at the causal border
 //                    lose what is not finite.  For other block sizes they do the loads too, with cp.async
 //   warp 20          TMEM allocation, tcgen05.mma issue by one elected lane
-//   warp 21          walks the CTA's share of the line and describes its units to the other roles (warp 23 completes the warpgroup)
+//   warp 21          walks the CTA's share of the line and describes its units to the other roles
 // Work split: as in attend.cuh, the tiles of all units (causal: only as many as a unit's last row sees) form one line of which every
 // CTA takes an equal share, so 64 units on 148 SMs balance as well as 6400.  Starting and ending a unit costs as much as a few of its
 // tiles, so each unit takes kChunkUnitCost places more on the line.  Places for that, and the time of a call (32/8 heads of 128,
@@ -411,7 +411,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
     }
     for (int i = 0; i < kChunkUnits; ++i) {
       mbar_init(&u_full[i], 1);
-      mbar_init(&u_empty[i], tensor_copies ? 22 : 21);  // every warp of the other roles
+      mbar_init(&u_empty[i], tensor_copies ? 23 : 21);  // every warp of the other roles
     }
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -461,10 +461,11 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
     regs_down<kChunkRegsLoads>();
     const int w = warp - 16, lt = tid - 16 * 32;
     constexpr int kRowPieces = D * (FP8 ? 1 : 2) / 16;  // 16-byte pieces of a cache row; as many as a thread takes of a tile
-    // the four warps meet once per tile of an 8-bit cache, so they leave together
+    // Codes lie where the numbers of later rows go (head_dim 64: of other warps' rows, so the four warps meet once per tile and leave together) or
+    // those of their own row (128: eight lanes of one warp).
     auto together = [&](bool fine) {
       fine = __all_sync(0xffffffffu, fine);
-      return FP8 ? !loaders_any(!fine) : fine;
+      return FP8 && D == 64 ? !loaders_any(!fine) : fine;
     };
     bool ok = true;
     int stage = 0, mask_at = 0;
@@ -490,7 +491,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
 #pragma unroll
                 for (int i = 0; i < kRowPieces; ++i) x[i] = *reinterpret_cast<const uint4*>(tile + C::kRawAt + (i * 128 + lt) * 16);
               }
-              ok = together(ok);  // (everybody's codes have been read: they lie where the numbers go)
+              ok = together(ok);  // (everybody's codes have been read)
               if (!ok) break;
 #pragma unroll
               for (int i = 0; i < kRowPieces; ++i) {
@@ -773,13 +774,17 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
         }
         if (u.nt < 0) break;
       }
-    } else if (warp == 22 && tensor_copies) {
-      // ---------------------------------------------------------------- tensor copies: K, V, K, V ..., as far ahead as there are stages
+    } else if (warp >= 22 && tensor_copies) {
+      // ---------------------------------------------------------------- tensor copies, as far ahead as there are stages: K by warp 22, V by warp 23
+      // (a warp issues one in fifty nanoseconds, and a tile of 16-key blocks with head_dim 128 is 32 of them: with one warp for both the tiles of
+      // long contexts take 1.68 us, 1.50 with two)
       // A lane copies a block (or 128 keys of one): rows of 128 bytes, swizzled as the tensor cores take them, or the codes of an 8-bit cache.  Keys
       // whose block the table does not name are copied from outside the cache, which gives zeros.
       bool ok = !c.mute_producer;
-      if (lane < 2) asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(lane ? &v_map : &k_map)) : "memory");
-      int stage = 0, mask_at = 0;
+      const int kv = warp - 22;
+      const CUtensorMap* map = kv ? &v_map : &k_map;
+      if (lane == 0) asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(map)) : "memory");
+      int stage = kv, mask_at = 0;
       uint32_t ph = 1;
       const int pages = kChunkKeys >> c.page_shift;
       for (int n = 0; ok; ++n) {
@@ -797,38 +802,36 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
         for (int t = u.t0; ok && t < t_end; ++t) {
           const int32_t blk = nxt >= 0 && nxt < p.num_blocks ? nxt : -1;
           nxt = entry_of(t + 1);
-          const uint32_t named = __ballot_sync(0xffffffffu, blk >= 0);
+          if (kv == 0) {
+            const uint32_t named = __ballot_sync(0xffffffffu, blk >= 0);
 #pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            const int key = w * 32 + lane;
-            const uint32_t there = __ballot_sync(0xffffffffu, ((named >> (key >> c.page_shift)) & 1u) && t * kChunkKeys + key < u.key_end);
-            if (lane == w) s_masks[mask_at * 4 + w] = there;
+            for (int w = 0; w < 4; ++w) {
+              const int key = w * 32 + lane;
+              const uint32_t there = __ballot_sync(0xffffffffu, ((named >> (key >> c.page_shift)) & 1u) && t * kChunkKeys + key < u.key_end);
+              if (lane == w) s_masks[mask_at * 4 + w] = there;
+            }
+            if (++mask_at == kChunkMaskRing) mask_at = 0;
+            __syncwarp();
+          }
+          const bool raw = FP8 || (kv && t * kChunkKeys + kChunkKeys - 1 > u.lim_min);
+          ok = __all_sync(0xffffffffu, chunk_wait(&kv_empty[stage], ph, abort_flag, limit));
+          if (!ok) break;
+          uint64_t* bar = raw ? &raw_full[stage] : &kv_full[stage];
+          if (lane == 0) {
+            mbar_arrive_expect_tx(bar, C::kCopyBytes);
+            if (!raw) mbar_arrive_n<3>(bar);  // (in the loading warps' place)
           }
           __syncwarp();
-          const int in_page = attn_in_page(p, key_of(t));
-          const bool causal = t * kChunkKeys + kChunkKeys - 1 > u.lim_min;
-          for (int kv = 0; kv < 2; ++kv) {
-            ok = __all_sync(0xffffffffu, chunk_wait(&kv_empty[stage], ph, abort_flag, limit));
-            if (!ok) break;
-            const bool raw = FP8 || (kv && causal);
-            uint64_t* bar = raw ? &raw_full[stage] : &kv_full[stage];
-            if (lane == 0) {
-              mbar_arrive_expect_tx(bar, C::kCopyBytes);
-              if (!raw) mbar_arrive_n<3>(bar);  // (in the loading warps' place)
-            }
-            __syncwarp();
-            if (lane < pages) {
-              const CUtensorMap* map = kv ? &v_map : &k_map;
-              uint8_t* dst = ring + stage * C::kTileBytes + C::kRawAt + ((lane << c.page_shift) * (FP8 ? D : 128));
+          if (lane < pages) {
+            uint8_t* dst = ring + stage * C::kTileBytes + C::kRawAt + ((lane << c.page_shift) * (FP8 ? D : 128));
 #pragma unroll
-              for (int b = 0; b < (FP8 ? 1 : C::kHalves); ++b) tma_load_4d(dst + b * 16384, map, b * 64, in_page, u.kvh, blk, bar);
-            }
-            if (++stage == C::kStages) {
-              stage = 0;
-              ph ^= 1u;
-            }
+            for (int b = 0; b < (FP8 ? 1 : C::kHalves); ++b) tma_load_4d(dst + b * 16384, map, b * 64, attn_in_page(p, key_of(t)), u.kvh, blk, bar);
           }
-          if (++mask_at == kChunkMaskRing) mask_at = 0;
+          stage += 2;
+          if (stage >= C::kStages) {
+            stage -= C::kStages;
+            ph ^= 1u;
+          }
         }
       }
       __syncwarp();
