@@ -520,7 +520,8 @@ size_t memstore_attend_workspace(memstore_t* store);
  * Several guesses of the tokens that follow are checked in one pass over the cache.  The new tokens of a request are then the nodes of
  * a tree: node 0 is the token that is certain, node i > 0 hangs on a node before it (parent in [0, i - 1]) and stands for one guess of the
  * token after that node.  Their keys and values lie in the cache one after another in node order (memstore_grow_blocks gives the slots),
- * whatever their positions.  A step: memstore_grow_blocks, memstore_plan_tree, then per layer memstore_append (at the tree's positions) and
+ * whatever their positions.  What is said above of the serving step's calls (scratch, devices, captures, limits of counts) holds here and for
+ * selected blocks too.  A step: memstore_grow_blocks, memstore_plan_tree, then per layer memstore_append (at the tree's positions) and
  * memstore_attend_tree, and when the model has said what follows each node, memstore_accept.
  */
 
@@ -649,7 +650,7 @@ typedef struct {
   int64_t kernels_launched; /* kernels of this library enqueued so far */
   int64_t arena_bytes, embedding_bytes;
   int64_t host_kv_tokens_used;
-  int64_t kernel_timeouts; /* 1 if a bounded wait inside the tensor-core scoring kernel or the chunk kernel of memstore_attend ever
+  int64_t kernel_timeouts; /* 1 if a bounded wait inside the tensor-core scoring kernel or the chunk kernel of memstore_attend and memstore_attend_tree ever
                               ran out (results of that call are invalid) */
   int64_t filter_fixups;   /* queries of the tensor-core retrieve path that were re-scanned exactly because the filter's margin
                               check failed (more groups within rounding of the k-th score than the margin keeps) */

@@ -734,7 +734,7 @@ class MemStore:
                 (out,) = self._empty(stream, ((T, n_q, self.head_dim), torch.bfloat16))
             ho = _Heads(out.data_ptr(), n_q * self.head_dim, self.head_dim)
         if out_lse is None and want_lse:
-            (out_lse,) = self._empty(stream, ((T, n_q), torch.float32))
+            out_lse = q.new_empty((T, n_q), dtype=torch.float32) if stream is None else self._empty(stream, ((T, n_q), torch.float32))[0]
         raw = self._raw_stream(stream)
         if workspace is None:
             workspace = self._workspace(raw, stream)
@@ -798,10 +798,15 @@ class MemStore:
             raise ValueError(f"block_tables must have shape ({nreq}, max_blocks), got {tuple(block_tables.shape)}")
         if (free_blocks is None) != (n_taken is None):
             raise ValueError("free_blocks and n_taken go together")
-        if cache.k.shape[0] < self.n_layers:
-            raise ValueError(f"the cache has {cache.k.shape[0]} layers, the store {self.n_layers}")
+        # (the one call that writes every layer: the description must not reach behind the tensors' memory)
+        last = (self.n_layers - 1) * cache.layer_stride + (cache.num_blocks - 1) * cache.block_stride + (cache.block_size - 1) * cache.token_stride
+        last += (self.n_kv_heads - 1) * cache.head_stride + self.head_dim
+        for x in (cache.k, cache.v):
+            if (x.storage_offset() + last) * x.element_size() > x.untyped_storage().nbytes():
+                raise ValueError(f"the cache is smaller than its description with the store's {self.n_layers} layers")
         if out is None:
-            (ints,) = self._empty(stream, ((T + 4 * nreq + 1,), i32))
+            n = T + 4 * nreq + 1
+            ints = seq_lens.new_empty(n, dtype=i32) if stream is None else self._empty(stream, ((n,), i32))[0]
             path, a, said, lens, status, taken = ints.split_with_sizes((T, nreq, nreq, nreq, nreq, 1))
             out = Accepted(path, a, said, lens, None if n_taken is None else taken, status)
             at = ints.data_ptr()
