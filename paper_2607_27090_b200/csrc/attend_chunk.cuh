@@ -89,7 +89,14 @@ struct ChunkParams {
   int mute_producer;
   int tensor_copies;  // tiles come by tensor copies, a block (or 128 keys of it) each
   int page_shift;     // log2 of the keys of such a copy
+  int unit_cost;      // of trees, see chunk_unit_cost
 };
+
+// Places on the line for a unit's set-up and end.
+template <int SEE>
+__device__ __forceinline__ int chunk_unit_cost(const ChunkParams& c) {
+  return SEE == kSeeTree ? c.unit_cost : kChunkUnitCost;
+}
 
 // The row tiles of a request one after another: token and query head of the group of the tile's first row.
 struct ChunkWalk {
@@ -117,7 +124,7 @@ __device__ __forceinline__ int64_t chunk_head_cost(const ChunkParams& c, const A
   int64_t s = 0;
   ChunkWalk w;
   const int n = chunk_row_tiles(q);
-  for (int rt = 0; rt < n; ++rt, w.step(c)) s += chunk_tiles<SEE>(c.a, q, w) + kChunkUnitCost;
+  for (int rt = 0; rt < n; ++rt, w.step(c)) s += chunk_tiles<SEE>(c.a, q, w) + chunk_unit_cost<SEE>(c);
   return s;
 }
 template <int SEE>
@@ -140,7 +147,7 @@ struct __align__(16) ChunkUnit {
   int32_t whole;            // all tiles of the unit are here
 };
 
-// A unit, and the place on it where a CTA's share begins (the first kChunkUnitCost places stand for its set-up, then come its tiles).
+// A unit, and the place on it where a CTA's share begins (the first chunk_unit_cost() places stand for its set-up, then come its tiles).
 struct ChunkSeg {
   int r, kvh, rt, tiles, pos;
   ChunkWalk w;
@@ -160,8 +167,8 @@ __device__ __forceinline__ bool chunk_locate(const ChunkParams& c, const AttnLin
   seg->w = ChunkWalk();
   for (;;) {
     seg->tiles = chunk_tiles<SEE>(c.a, seg->q, seg->w);
-    if (rem < seg->tiles + kChunkUnitCost) break;
-    rem -= seg->tiles + kChunkUnitCost;
+    if (rem < seg->tiles + chunk_unit_cost<SEE>(c)) break;
+    rem -= seg->tiles + chunk_unit_cost<SEE>(c);
     ++seg->rt;
     seg->w.step(c);
   }
@@ -735,9 +742,9 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
           begin = off;
           pos = seg.pos;
           tiles = seg.tiles;
-          const int here = (int)min((int64_t)(tiles + kChunkUnitCost - pos), off_end - off);  // places of this CTA on the unit
-          u.t0 = max(0, pos - kChunkUnitCost);
-          u.t1 = max(0, pos + here - kChunkUnitCost);
+          const int here = (int)min((int64_t)(tiles + chunk_unit_cost<SEE>(c) - pos), off_end - off);  // places of this CTA on the unit
+          u.t0 = max(0, pos - chunk_unit_cost<SEE>(c));
+          u.t1 = max(0, pos + here - chunk_unit_cost<SEE>(c));
           if (u.t1 > u.t0) {
             u.rows = min(kChunkRows, seg.q.rows - seg.rt * kChunkRows);
             u.req = seg.r;
@@ -758,7 +765,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
           cut.c_last = -1;
           if (u.nt >= 0 && u.t0 != 0 && share >= u.t0) {  // the border before this CTA cuts the unit, and is the first that does
             int64_t rem;
-            cut.c_last = (int)attn_div(begin - pos + tiles + kChunkUnitCost - 1, share, &rem);
+            cut.c_last = (int)attn_div(begin - pos + tiles + chunk_unit_cost<SEE>(c) - 1, share, &rem);
             cut.rows = u.rows;
             cut.tok0 = u.tok0;
             cut.sub0 = u.sub0;

@@ -272,6 +272,9 @@ static ms_status attend_launch(memstore* s, ChunkParams& c, int64_t max_rows, cu
   c.min_rows = rows ? min_rows : 0;
   p.max_rows = chunks ? c.min_rows : 0x7fffffff;
   if (!chunks || !rows) p.gate = nullptr;  // (with both kernels there is a unit, so a join kernel too, which clears the word)
+  // A tree's units cost more to begin and end (the halves meet) and their tiles less: eight places where units outnumber CTAs.  40 requests, 17 - 61 nodes
+  // behind 700 - 9,000 tokens: four places 298 us (8-bit cache 301), eight 272 (283), ten 275 (290), sixteen 293 (311); one request of 8,000 with 64 nodes 32, 34, 34, 32.
+  c.unit_cost = (int64_t)p.n_kv * p.nreq >= s->sm_count ? 8 : kChunkUnitCost;
   c.step_tok = kChunkRows / p.group;
   c.step_sub = kChunkRows % p.group;
   const int64_t all_rows = (int64_t)p.n_tokens * p.group;
