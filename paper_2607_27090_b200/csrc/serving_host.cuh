@@ -684,11 +684,11 @@ ms_status memstore_select_blocks(memstore_t* s, const ms_heads* q, int32_t n_q_h
   lc.stream = (cudaStream_t)stream;
   lc.attrs = attr;
   lc.numAttrs = 2;
-  for (;; parts /= 2) {  // a cluster that the device cannot hold at once with this much shared memory: halve it
+  for (;; parts /= 2) {  // clusters that the device cannot hold at once (15 of eight CTAs fit its groups of SMs): halve them
     attr[1].val.clusterDim.x = parts;
     lc.gridDim = dim3((unsigned)(units * parts));
     int n_clusters = 0;
-    if (parts == 1 || (cudaOccupancyMaxActiveClusters(&n_clusters, kernel, &lc) == cudaSuccess && n_clusters > 0)) break;
+    if (parts == 1 || (cudaOccupancyMaxActiveClusters(&n_clusters, kernel, &lc) == cudaSuccess && n_clusters >= units)) break;
     (void)cudaGetLastError();
   }
   MS_CUDA(s, cudaLaunchKernelEx(&lc, kernel, p));
