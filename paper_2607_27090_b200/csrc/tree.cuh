@@ -151,7 +151,7 @@ __global__ void __launch_bounds__(kWalkWarps * 32) accept_walk_kernel(const Acce
     bool no_table = false, no_block = false;
     auto look = [&](int32_t pos) {
       const int b = pos / p.block_size;
-      if (b >= p.max_blocks) {
+      if (pos < 0 || b >= p.max_blocks) {
         no_table = true;
       } else {
         const int32_t x = p.tables[r * p.max_blocks + b];
@@ -160,7 +160,7 @@ __global__ void __launch_bounds__(kWalkWarps * 32) accept_walk_kernel(const Acce
     };
     for (int i = lane; i < a; i += 32) {
       const int from = __ldcg(p.path + q0 + i);
-      if (from != i) {
+      if (from > i) {
         look(start + from);
         look(start + i);
       }
@@ -245,7 +245,7 @@ __global__ void __launch_bounds__(kMoveThreads) accept_move_kernel(const AcceptP
     const int32_t* table = p.tables + r * p.max_blocks;
     auto place = [&](int32_t pos) -> int64_t {
       const int b = pos / p.block_size;
-      const int32_t blk = b < p.max_blocks ? table[b] : -1;
+      const int32_t blk = pos >= 0 && b < p.max_blocks ? table[b] : -1;
       return blk >= 0 && blk < p.num_blocks ? blk * p.block_stride + (pos - b * p.block_size) * p.token_stride : -1;
     };
     for (int i0 = 1; i0 < a; i0 += kMoveBatch) {
@@ -256,7 +256,7 @@ __global__ void __launch_bounds__(kMoveThreads) accept_move_kernel(const AcceptP
         const int i = i0 + j;
         const int from = i < a ? p.path[q0 + i] : i;
         to[j] = -1;
-        if (from != i) {
+        if (from > i) {  // (less only where another request's rows overlap these: nothing outside the cache may be read then either)
           const int64_t src = place(start + from);
           to[j] = place(start + i);
           if (src < 0) to[j] = -1;

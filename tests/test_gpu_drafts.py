@@ -446,6 +446,25 @@ def test_accept_long_chains_and_whole_trees():
         assert want["a"] == [(n + 1) // 2]
 
 
+def test_accept_stays_inside_the_cache_where_rows_of_requests_overlap():
+    """Two requests that share rows write their paths over one another's; no row is then read from a place in front of the cache's first."""
+    ms, bs, n = store(1, 64, 1), 4, 10003
+    row = bs * 64
+    memory = torch.full((2, 10 * row), 3.0, dtype=torch.bfloat16, device=DEV)  # the cache is blocks 1 to 8 of this
+    kv = memory[:, row : 9 * row]
+    kv[:] = torch.arange(8 * bs, device=DEV).repeat_interleave(64).to(torch.bfloat16)
+    cache = PagedCache(kv[0], kv[1], 8 * row, row, 64, 64, 8, bs)
+    before = memory.clone()
+    # request 0: rows 0 - 4, a chain that is accepted whole; request 2: from row 3 on, its root alone is accepted, after a look at all its nodes
+    parents, tokens, choices, positions = np.zeros(n, np.int32), np.ones(n, np.int32), np.full(n, 9, np.int32), np.full(n, -1, np.int32)
+    parents[:5], tokens[:5], choices[:5] = [-1, 0, 1, 2, 3], range(50, 55), range(51, 56)
+    positions[0], positions[3] = 0, 100
+    got = ms.accept(i32(parents), i32(tokens), i32(choices), i32(positions), i32([0, 5, 3, n]), i32([5, 7, 100 + n - 3]), i32([[0, 1], [2, 3], [4, 5]]), cache)
+    torch.cuda.synchronize()
+    assert got.n_accepted.tolist() == [5, 0, 1] and got.seq_lens.tolist() == [5, 7, 101] and got.status.tolist()[1] == M.REQ_BAD_LENGTH
+    assert torch.equal(memory, before)
+
+
 def test_accept_reports_what_it_refuses():
     rng = random.Random(10)
     sizes, starts = [12, 9, 20, 7, 15, 30, 11], [30, 31, 5, 0, 16, 3, 9]
